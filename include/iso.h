@@ -63,7 +63,11 @@
  * (iso_optimizer_step, iso_optimizer_step_muon) and
  * the spectral diagnostics of Sec. 3 (iso_spectral_diagnostics,
  * iso_spectrum_interpolate, iso_transport_ratios) and the mean squared
- * spectral error of App. G (iso_spectral_error).
+ * spectral error of App. G (iso_spectral_error).  The gradients that the
+ * optimizer steps take come from iso_embed_lookup / iso_embed_grad (an
+ * embedding and its gradient) and from 8-bit activation checkpoints:
+ * iso_ckpt_pack, iso_ckpt_unpack, iso_ckpt_gate_grad, iso_ckpt_weight_grad;
+ * their conventions stand with them.
  */
 #ifndef ISO_H
 #define ISO_H
@@ -85,7 +89,8 @@ typedef enum iso_status {
   ISO_ERR_NONFINITE = 4,
   ISO_ERR_HIP = 5,
   ISO_ERR_UNSUPPORTED = 6,
-  ISO_ERR_INTERNAL = 7     /* a kernel met counts that cannot occur; outputs invalid */
+  ISO_ERR_INTERNAL = 7,    /* a kernel met counts that cannot occur; outputs invalid */
+  ISO_ERR_INDEX = 8        /* a token id outside the vocabulary                        */
 } iso_status;
 
 /* The enumerations name the values of plain int parameters and fields: the library checks
@@ -451,6 +456,145 @@ typedef struct iso_factors {
 iso_status iso_blockdiag_project_factors(const iso_tensor* t, int n_t, int K, int dt, int rank, double alpha,
                                          const iso_factors* factors, float* const* delta_hat, void* ws,
                                          size_t ws_bytes, void* stream);
+
+/* ==== gradients for the optimizer steps ==========================================================
+ *
+ * G_W of iso_frame (rows x cols row-major, the step's storage type) is what a backward pass leaves for
+ * a weight matrix.  The calls below make it for an embedding and for linear layers, the latter from
+ * activations kept in 8 bits between the forward and the backward pass.
+ *
+ *  - Weights and weight gradients are contiguous; activation matrices (tokens x features) have a row
+ *    stride ld >= features, in elements, so that they may be column ranges of a wider buffer.  Any
+ *    stride is taken; rows that stay 16-byte aligned are read and written 16 bytes at a time.
+ *  - Pointers are device memory, 16-byte aligned, except the ids (their own size).  Outputs must not
+ *    overlap inputs unless said so.
+ *  - All calls are asynchronous on `stream`, allocate nothing, copy nothing from the host and may be
+ *    captured into a graph.  Argument errors are returned before anything is queued.  Tables are
+ *    read before the call returns.
+ *  - Sums are held in binary32 and rounded once to the output type (nearest even).  They are formed in
+ *    a fixed order: results are bit-identical across runs.
+ *  - Non-finite values propagate as in IEEE arithmetic; they are no error here.
+ */
+
+typedef enum iso_id_type { ISO_I32 = 0, ISO_I64 = 1 } iso_id_type;
+
+/* A pad_id that no token has. */
+#define ISO_NO_PAD INT64_MIN
+
+#define ISO_EMBED_MAX_VOCAB (1 << 20)
+
+/* An embedding and the tokens of one pass through it.  Which pointers are read depends on the call. */
+typedef struct iso_embed {
+  const void* ids;       /* tokens ids, of id_type                                                   */
+  int32_t id_type;       /* an iso_id_type                                                           */
+  int64_t tokens;        /* 0 <= tokens < 2^31                                                       */
+  int64_t vocab, dim;    /* the table is vocab x dim; vocab <= ISO_EMBED_MAX_VOCAB                   */
+  int64_t pad_id;        /* tokens with this id are padding (it need not lie in the table)           */
+  double scale;          /* finite                                                                   */
+  const void* table;     /* lookup: W, vocab x dim                                                   */
+  void* x;               /* tokens x dim: written by the lookup, dX for the gradient                 */
+  int64_t ld_x;          /* row stride of x                                                          */
+  void* grad;            /* gradient: G, vocab x dim                                                 */
+} iso_embed;
+
+/* Bytes of workspace for either call on these sizes (0 on bad arguments); 256-byte aligned. */
+size_t iso_workspace_size_embed(const iso_embed* e);
+
+/*
+ * iso_embed_lookup -- x_i = round(scale * W[id_i]) for every token i (the
+ * product in binary32), +0 in every column where id_i == pad_id.  table and x
+ * are of type dt.  An id that is neither pad_id nor in [0, vocab) is reported
+ * by iso_read_device_status (ISO_ERR_INDEX); its row of x is zero.
+ */
+iso_status iso_embed_lookup(const iso_embed* e, int dt, void* ws, size_t ws_bytes, void* stream);
+
+/*
+ * iso_embed_grad -- the lookup's gradient: G[v] = round(scale * sum of dX_i over
+ * the tokens i with id_i = v), the sum in binary32 over the tokens sorted by id,
+ * in token order in runs of 32 whose sums are added in order.  Padding (and an id
+ * outside the vocabulary, reported as above) adds nothing, whatever its row of
+ * dX holds.  dX (e->x) is of type dt, G of type dt_grad.
+ * accumulate = 0: every row of G is written (zero where no token has the id);
+ * accumulate = 1: G[v] = round(G[v] + scale * sum) in place, and rows that no
+ * token has are neither read nor written.
+ */
+iso_status iso_embed_grad(const iso_embed* e, int dt, int dt_grad, int accumulate, void* ws, size_t ws_bytes,
+                          void* stream);
+
+/*
+ * 8-bit activation checkpoint of a rows x cols matrix (rows = tokens).  Columns
+ * are padded to ld = iso_ckpt_ld(cols), a multiple of ISO_CKPT_GROUP; the values
+ * of a group of 32 columns in a row share a power of two:
+ *   2^k the least with max |x| <= 127 * 2^k and k >= -126,
+ *   q = x / 2^k rounded to the nearest integer, ties to even  (|q| <= 127),
+ * so a value is off by at most 2^(k-1) <= max|x| / 127 of its group (for k = 122,
+ * reached above 127 * 2^121 only, |q| is held at 63, off by at most 2^122: 64 *
+ * 2^122 would come back infinite).  q holds rows x ld
+ * int8 values (zeros in the padding), e holds rows x ld/32 bytes k + 127 (1 for
+ * a group of zeros).  A group that holds a NaN or an infinity is kept as
+ * e = 255, q = 0 and comes back as NaN in all its columns.  The stored values q 2^k are
+ * exact in bf16 and in fp32: everything computed from them is computed from
+ * the same numbers in both types.
+ */
+#define ISO_CKPT_GROUP 32
+
+typedef struct iso_ckpt {
+  int8_t* q;             /* rows x iso_ckpt_ld(cols)                                                 */
+  uint8_t* e;            /* rows x iso_ckpt_ld(cols) / 32                                            */
+  int64_t rows, cols;
+  void* x;               /* pack: the matrix to keep; unpack: where it is written back               */
+  int64_t ld_x;          /* row stride of x                                                          */
+} iso_ckpt;
+
+/* Columns of q for a matrix of `cols` columns: the next multiple of 32 (-1 for cols < 0). */
+int64_t iso_ckpt_ld(int64_t cols);
+
+/* iso_ckpt_pack / iso_ckpt_unpack -- a table of n matrices of type dt to 8 bits and back. */
+iso_status iso_ckpt_pack(const iso_ckpt* c, int n, int dt, void* stream);
+iso_status iso_ckpt_unpack(const iso_ckpt* c, int n, int dt, void* stream);
+
+/*
+ * iso_ckpt_gate_grad -- the backward pass of a gated activation h = silu(g) * u
+ * (silu(g) = g s, s = 1 / (1 + exp(-g))) from the checkpoints of g and u and the gradient dh:
+ *   dgate = dh u s (1 + g (1 - s)),   dup = dh g s,
+ * in binary32, rounded once.  gate and up have the same rows and cols (their x
+ * is not used); dh, dgate and dup are rows x cols of type dt with row stride
+ * ld; dgate or dup may be dh itself.
+ */
+typedef struct iso_gate_grad {
+  iso_ckpt gate, up;
+  const void* dh;
+  void* dgate;
+  void* dup;
+  int64_t ld;
+} iso_gate_grad;
+
+iso_status iso_ckpt_gate_grad(const iso_gate_grad* g, int n, int dt, void* stream);
+
+/*
+ * iso_ckpt_weight_grad -- G_W of a table of linear layers y = W x (W: rows x cols,
+ * x: cols features of every token) from the 8-bit checkpoint of x:
+ *   G = round([G +] sum over the tokens t of dy_t x_t^T),
+ * the sum in binary32.  in.rows is the number of tokens and in.cols the columns
+ * of W (in.x is not used); dy is tokens x rows of type dt with row stride ld_dy;
+ * grad is rows x cols of type dt_grad.  accumulate = 1 adds to what grad holds.
+ * No tokens: a zero gradient (accumulate: unchanged).  Layers of one call that
+ * share a checkpoint (q-k-v, gate-up) share the work on it.  Products are exact:
+ * x is exact in bf16, and an fp32 dy is taken in three bf16 parts.
+ */
+typedef struct iso_weight_grad {
+  iso_ckpt in;
+  const void* dy;
+  int64_t ld_dy;
+  void* grad;
+  int64_t rows;
+} iso_weight_grad;
+
+/* Bytes of workspace of a table (0 on bad arguments); 256-byte aligned. */
+size_t iso_workspace_size_weight_grad(const iso_weight_grad* g, int n, int dt);
+
+iso_status iso_ckpt_weight_grad(const iso_weight_grad* g, int n, int dt, int dt_grad, int accumulate, void* ws,
+                                size_t ws_bytes, void* stream);
 
 /* round(n * num / den), halves rounded up, in exact integer arithmetic; -1 on bad arguments. */
 int64_t iso_k_from_density(int64_t n, int64_t num, int64_t den);

@@ -9,7 +9,7 @@ from dataclasses import dataclass, field
 from typing import List, Optional, Sequence
 
 from . import _lib
-from ._lib import (BF16, F32, MERGE_RAM, MERGE_TA, MERGE_TIES, OP_BLOCKDIAG, OP_MERGE, OP_SIGN, OP_TOPK,
+from ._lib import (BF16, CKPT_GROUP, F32, MERGE_RAM, MERGE_TA, MERGE_TIES, OP_BLOCKDIAG, OP_MERGE, OP_SIGN, OP_TOPK,
                    OP_UPDATE_APPLY, OP_UPDATE_FUSED, OP_UPDATE_FUSED_SELECT, OP_UPDATE_ORTHO, OP_UPDATE_SPECTRAL,
                    UPDATE_APPLY, UPDATE_FUSED, UPDATE_ORTHO, UPDATE_SPECTRAL, IsoSelectDesc)
 
@@ -223,6 +223,155 @@ def iso_optimizer_step_muon(frames, dtype, lr, momentum=0.95, weight_decay=0.0, 
     rc = _lib.load().iso_optimizer_step_muon(_frames(frames), len(frames), dtype, ctypes.byref(o), wp, wb,
                                              _stream(stream))
     _check(rc, "iso_optimizer_step_muon")
+
+
+# ---- gradients for the optimizer steps: embeddings, 8-bit activation checkpoints ----------------------------------
+
+
+@dataclass
+class Embed:
+    """An embedding and the tokens of one pass: int32 or int64 ids, the table (vocab x dim, lookup), x (tokens x dim with row
+    stride ld_x, dim if None: written by the lookup, dX for the gradient), grad (vocab x dim, gradient).  Tokens with
+    id pad_id are padding (None: there is none)."""
+    ids: object
+    tokens: int
+    vocab: int
+    dim: int
+    x: object
+    table: Optional[object] = None
+    grad: Optional[object] = None
+    scale: float = 1.0
+    pad_id: Optional[int] = None
+    ld_x: Optional[int] = None
+    id_type: Optional[int] = None      # I32 or I64; None: from ids.dtype
+
+
+def _embed(e: Embed):
+    wide = e.id_type if e.id_type is not None else _id_type(e.ids)
+    return _lib.IsoEmbed(_ptr(e.ids), wide, e.tokens, e.vocab, e.dim, _lib.NO_PAD if e.pad_id is None else e.pad_id,
+                         e.scale, _ptr(e.table), _ptr(e.x), e.dim if e.ld_x is None else e.ld_x, _ptr(e.grad))
+
+
+def _id_type(ids):
+    size = {"torch.int32": _lib.I32, "torch.int64": _lib.I64}.get(str(getattr(ids, "dtype", None)))
+    if size is None:
+        raise TypeError("ids are an int32 or int64 tensor (or give id_type)")
+    return size
+
+
+def _bytes(n, device):
+    import torch
+    ws = torch.empty(n + 256, dtype=torch.uint8, device=device)
+    off = (-ws.data_ptr()) % 256
+    return ws[off:off + n]
+
+
+def embed_workspace(e: Embed, device="cuda"):
+    """Workspace for iso_embed_lookup and iso_embed_grad on these sizes."""
+    n = _lib.load().iso_workspace_size_embed(ctypes.byref(_embed(e)))
+    if n == 0:
+        raise ValueError("bad embedding sizes")
+    return _bytes(n, device)
+
+
+def iso_embed_lookup(e: Embed, dtype, ws=None, stream=None):
+    wp, wb = _ws(ws)
+    rc = _lib.load().iso_embed_lookup(ctypes.byref(_embed(e)), dtype, wp, wb, _stream(stream))
+    _check(rc, "iso_embed_lookup")
+
+
+def iso_embed_grad(e: Embed, dtype, grad_dtype, accumulate=False, ws=None, stream=None):
+    wp, wb = _ws(ws)
+    rc = _lib.load().iso_embed_grad(ctypes.byref(_embed(e)), dtype, grad_dtype, 1 if accumulate else 0, wp, wb,
+                                    _stream(stream))
+    _check(rc, "iso_embed_grad")
+
+
+@dataclass
+class Ckpt:
+    """An activation matrix of rows x cols kept in 8 bits: q (int8, rows x iso_ckpt_ld(cols)) and e (uint8, a byte per 32
+    columns).  x is the matrix itself (row stride ld_x, cols if None), read by iso_ckpt_pack, written by iso_ckpt_unpack."""
+    rows: int
+    cols: int
+    q: object
+    e: object
+    x: Optional[object] = None
+    ld_x: Optional[int] = None
+
+
+def _ckpt(c: Ckpt):
+    return _lib.IsoCkpt(_ptr(c.q), _ptr(c.e), c.rows, c.cols, _ptr(c.x), c.cols if c.ld_x is None else c.ld_x)
+
+
+def iso_ckpt_ld(cols):
+    return _lib.load().iso_ckpt_ld(cols)
+
+
+def ckpt_buffers(rows, cols, device="cuda"):
+    """(q, e) buffers of a checkpoint of a rows x cols matrix."""
+    import torch
+    ld = iso_ckpt_ld(cols)
+    return (torch.empty(rows, ld, dtype=torch.int8, device=device),
+            torch.empty(rows, ld // CKPT_GROUP, dtype=torch.uint8, device=device))
+
+
+def iso_ckpt_pack(ckpts: Sequence[Ckpt], dtype, stream=None):
+    arr = (_lib.IsoCkpt * max(1, len(ckpts)))(*[_ckpt(c) for c in ckpts])
+    _check(_lib.load().iso_ckpt_pack(arr, len(ckpts), dtype, _stream(stream)), "iso_ckpt_pack")
+
+
+def iso_ckpt_unpack(ckpts: Sequence[Ckpt], dtype, stream=None):
+    arr = (_lib.IsoCkpt * max(1, len(ckpts)))(*[_ckpt(c) for c in ckpts])
+    _check(_lib.load().iso_ckpt_unpack(arr, len(ckpts), dtype, _stream(stream)), "iso_ckpt_unpack")
+
+
+@dataclass
+class GateGrad:
+    """Backward pass of h = silu(gate) * up: checkpoints of gate and up, dh, and where dgate and dup go (row stride ld)."""
+    gate: Ckpt
+    up: Ckpt
+    dh: object
+    dgate: object
+    dup: object
+    ld: Optional[int] = None
+
+
+def iso_ckpt_gate_grad(gates: Sequence[GateGrad], dtype, stream=None):
+    arr = (_lib.IsoGateGrad * max(1, len(gates)))(*[
+        _lib.IsoGateGrad(_ckpt(g.gate), _ckpt(g.up), _ptr(g.dh), _ptr(g.dgate), _ptr(g.dup),
+                         g.gate.cols if g.ld is None else g.ld) for g in gates])
+    _check(_lib.load().iso_ckpt_gate_grad(arr, len(gates), dtype, _stream(stream)), "iso_ckpt_gate_grad")
+
+
+@dataclass
+class WeightGrad:
+    """One linear layer's weight gradient: the checkpoint of its input (tokens x cols), dy (tokens x rows, row stride ld_dy)
+    and grad (rows x cols)."""
+    ckpt: Ckpt
+    dy: object
+    grad: object
+    rows: int
+    ld_dy: Optional[int] = None
+
+
+def _weight_grads(jobs):
+    return (_lib.IsoWeightGrad * max(1, len(jobs)))(*[
+        _lib.IsoWeightGrad(_ckpt(j.ckpt), _ptr(j.dy), j.rows if j.ld_dy is None else j.ld_dy, _ptr(j.grad), j.rows)
+        for j in jobs])
+
+
+def weight_grad_workspace(jobs: Sequence[WeightGrad], dtype, device="cuda"):
+    n = _lib.load().iso_workspace_size_weight_grad(_weight_grads(jobs), len(jobs), dtype)
+    if n == 0:
+        raise ValueError("bad table of layers")
+    return _bytes(n, device)
+
+
+def iso_ckpt_weight_grad(jobs: Sequence[WeightGrad], dtype, grad_dtype, accumulate=False, ws=None, stream=None):
+    wp, wb = _ws(ws)
+    rc = _lib.load().iso_ckpt_weight_grad(_weight_grads(jobs), len(jobs), dtype, grad_dtype, 1 if accumulate else 0, wp,
+                                          wb, _stream(stream))
+    _check(rc, "iso_ckpt_weight_grad")
 
 
 def iso_spectral_diagnostics(entries, dtype, out, ws=None, stream=None):

@@ -10,7 +10,10 @@ BUILD = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "libiso.so")
 
 SOURCES = ["iso_abi.cpp", "iso_select.hip", "iso_merge.hip", "iso_fused.hip", "iso_spectral.hip", "iso_tsv.hip",
-           "iso_noalloc.hip", "iso_ortho.hip"]
+           "iso_noalloc.hip", "iso_ortho.hip", "iso_grad_abi.cpp", "iso_embed.hip", "iso_ckpt.hip", "iso_wgrad.hip"]
+
+# the C ABI layers: argument checks and host-side planning (what the sanitized build instruments)
+HOST_SOURCES = ["iso_abi.cpp", "iso_grad_abi.cpp"]
 
 HIPFLAGS = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC",
@@ -56,7 +59,7 @@ def build(verbose=False, jobs=8):
     return LIB
 
 
-# Host-side sanitizer build of the C ABI layer: iso_abi.cpp (argument checks, workspace
+# Host-side sanitizer build of the C ABI layers: HOST_SOURCES (argument checks, workspace
 # planning, table building) instrumented with AddressSanitizer and UndefinedBehaviorSanitizer,
 # linked with the uninstrumented kernel objects of build().  The sanitizer runtime is not linked
 # in: it is preloaded into the host process (asan_runtime() below), which the CPU test of the
@@ -77,21 +80,23 @@ def asan_runtime():
 
 
 def build_host_sanitized(verbose=False):
-    """Builds SANITIZED_LIB from the objects of build() (which must have run) and a sanitized
-    iso_abi.cpp; returns its path, or None when the toolchain has no ASan runtime."""
+    """Builds SANITIZED_LIB from the objects of build() (which must have run) and sanitized
+    HOST_SOURCES; returns its path, or None when the toolchain has no ASan runtime."""
     if asan_runtime() is None:
         return None
-    obj = os.path.join(BUILD, "iso_abi_hostsan.o")
-    cmd = (["hipcc"] + HIPFLAGS
-           + ["-Xarch_host", "-fsanitize=address", "-Xarch_host", "-fsanitize=undefined",
-              "-Xarch_host", "-fno-sanitize-recover=all", "-Xarch_host", "-fno-omit-frame-pointer", "-g",
-              "-c", os.path.join(CSRC, "iso_abi.cpp"), "-o", obj])
-    if verbose:
-        print(" ".join(cmd), flush=True)
-    r = subprocess.run(cmd, capture_output=True, text=True)
-    if r.returncode != 0:
-        raise RuntimeError(f"compile failed: iso_abi.cpp (sanitized)\n{r.stdout}\n{r.stderr}")
-    objs = [obj] + [os.path.join(BUILD, os.path.splitext(s)[0] + ".o") for s in SOURCES if s != "iso_abi.cpp"]
+    objs = [os.path.join(BUILD, os.path.splitext(s)[0] + ".o") for s in SOURCES if s not in HOST_SOURCES]
+    for src in HOST_SOURCES:
+        obj = os.path.join(BUILD, os.path.splitext(src)[0] + "_hostsan.o")
+        cmd = (["hipcc"] + HIPFLAGS
+               + ["-Xarch_host", "-fsanitize=address", "-Xarch_host", "-fsanitize=undefined",
+                  "-Xarch_host", "-fno-sanitize-recover=all", "-Xarch_host", "-fno-omit-frame-pointer", "-g",
+                  "-c", os.path.join(CSRC, src), "-o", obj])
+        if verbose:
+            print(" ".join(cmd), flush=True)
+        r = subprocess.run(cmd, capture_output=True, text=True)
+        if r.returncode != 0:
+            raise RuntimeError(f"compile failed: {src} (sanitized)\n{r.stdout}\n{r.stderr}")
+        objs.append(obj)
     tmp = SANITIZED_LIB + ".tmp"
     cmd = ["hipcc", "--offload-arch=gfx950", "-shared", "-fPIC", "-o", tmp] + objs
     if verbose:

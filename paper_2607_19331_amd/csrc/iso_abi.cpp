@@ -904,6 +904,7 @@ iso_status iso_read_device_status(const void* ws, void* stream) {
   if (hipMemcpy(&flags, ws, sizeof flags, hipMemcpyDeviceToHost) != hipSuccess) return ISO_ERR_HIP;
   if (flags & kStatusInternal) return ISO_ERR_INTERNAL;
   if (flags & kStatusNonFinite) return ISO_ERR_NONFINITE;
+  if (flags & kStatusIndex) return ISO_ERR_INDEX;
   return ISO_OK;
 }
 
@@ -958,6 +959,7 @@ const char* iso_status_string(int s) {
     case ISO_ERR_HIP: return "HIP runtime error";
     case ISO_ERR_UNSUPPORTED: return "unsupported shape or option";
     case ISO_ERR_INTERNAL: return "internal consistency check failed";
+    case ISO_ERR_INDEX: return "token id outside the vocabulary";
   }
   return "unknown status";
 }

@@ -14,6 +14,7 @@ namespace iso {
 constexpr size_t kStatusBytes = 256;
 constexpr uint32_t kStatusNonFinite = 1u;
 constexpr uint32_t kStatusInternal = 2u;   // a kernel found counts that cannot occur; results invalid
+constexpr uint32_t kStatusIndex = 4u;      // a token id outside the vocabulary
 
 inline size_t align_up(size_t x, size_t a) { return (x + a - 1) / a * a; }
 
