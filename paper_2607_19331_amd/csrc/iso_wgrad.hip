@@ -2,122 +2,584 @@
 //
 // X is exact in bf16, so the products of a bf16 dY are exact and bf16 matrix instructions with binary32 accumulators
 // lose nothing but the sum's own rounding; a binary32 dY is the sum of three bf16 parts of 8 bits each (cut, not
-// rounded: every remainder is exact), which gives three products with the same X.
+// rounded: every remainder is exact), which makes it three products with the same X, added least part first.
+//
+// A call is up to three launches per 16 layers.  k_wgrad_prep brings operands into the form that the product reads,
+// bf16 rows aligned to 16 bytes: X always (once per checkpoint, however many layers share it), dY where it is fp32 or
+// its stride is odd.  k_wgrad forms 256 x 256 tiles of all layers.  k_wgrad_join adds up tiles whose tokens were split.
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
 #include <algorithm>
+#include <vector>
 
 #include "iso.h"
 #include "iso_device.h"
 #include "iso_grad.h"
 #include "iso_grad_device.h"
-#include "iso_kernels.h"
 
 namespace iso {
 
 namespace {
 
-typedef __bf16 bf16x8_t __attribute__((ext_vector_type(8)));
+constexpr int kLayers = 16;          // layers a launch
+constexpr int kTile = 256;           // a workgroup's tile of G
+constexpr int kStep = 32;            // tokens of a step
+constexpr int kStages = 4;           // steps in LDS
+constexpr int kStageBytes = 2 * kStep * kTile * 2;
+constexpr int kUnits = 256;          // workgroups that run at once: one a CU
+constexpr int64_t kMaxStride = 1 << 25;   // 32 rows of it stay within 32-bit offsets
 
-struct Job {
-  const int8_t* q;
-  const uint8_t* e;
-  const void* dy;
-  void* grad;
-  int64_t tokens, ld_dy, ld_q;
-  int32_t rows, cols;
+// ---- operand preparation -------------------------------------------------------------------------------------------
+
+struct Prep {
+  const void* src;        // q, or dY
+  const uint8_t* e;       // exponents of q; null for dY
+  uint16_t* dst;
+  int64_t rows, ld;       // rows and row stride of the source
+  int64_t part;           // rows of a part of the destination (rows rounded up to whole steps); 0 for X
+  uint32_t cols, per_row; // columns of the source; groups of eight in a destination row
+  uint32_t block0;
 };
 
-constexpr int kTile = 64, kStep = 32, kLd = kStep + 8;
+struct PrepTable {
+  Prep p[2 * kLayers];
+  int n;
+  uint32_t blocks;
+  uint32_t* status;
+};
 
-// One 64 x 64 tile of G a workgroup, four waves of 32 x 32; a step of 32 tokens is staged in LDS token-innermost.
-template <int DT, int DTG, bool ADD>
-__global__ void __launch_bounds__(256) k_wgrad(Job a) {
-  constexpr int kParts = DT == ISO_F32 ? 3 : 1;
-  __shared__ uint16_t A[kParts][kTile][kLd], B[kTile][kLd];
-  const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
-  const int64_t across = (a.cols + kTile - 1) / kTile;
-  const int64_t m0 = blockIdx.x / across * kTile, n0 = blockIdx.x % across * kTile;
-  const int wm = (wave >> 1) * 32, wn = (wave & 1) * 32;
-  f32x4_t acc[2][2] = {};
-  for (int64_t t0 = 0; t0 < a.tokens; t0 += kStep) {
-    __syncthreads();
-    for (int i = tid; i < kTile * kStep; i += 256) {
-      const int c = i & 63, t = i >> 6;
-      const int64_t tok = t0 + t, m = m0 + c, n = n0 + c;
-      uint32_t y = 0, x = 0;
-      if (tok < a.tokens && m < a.rows) y = elem_bits<DT>(a.dy, tok * a.ld_dy + m);
-      if (tok < a.tokens && n < a.cols)
-        x = bits_from_f32((float)a.q[tok * a.ld_q + n] * f32_from_bits((uint32_t)a.e[(tok * a.ld_q + n) >> 5] << 23));
-      B[c][t] = (uint16_t)(x >> 16);
-      if constexpr (DT == ISO_BF16) {
-        A[0][c][t] = (uint16_t)y;
-      } else {
-        const bool finite = (y & 0x7F800000u) != 0x7F800000u;
-        float r = f32_from_bits(y);
-        uint32_t hi = y & 0xFFFF0000u;
-        if (!finite && (y & 0x7FFFFFu)) hi |= 0x400000u;   // a NaN stays one
-        r = finite ? r - f32_from_bits(hi) : 0.0f;
-        const uint32_t mid = bits_from_f32(r) & 0xFFFF0000u;
-        r -= f32_from_bits(mid);
-        A[0][c][t] = (uint16_t)(hi >> 16);
-        A[1][c][t] = (uint16_t)(mid >> 16);
-        A[2][c][t] = (uint16_t)(bits_from_f32(r) >> 16);
+// Eight columns of one row a thread.  X: q 2^k, whose upper 16 bits are the whole value.  dY: its bf16 parts, least
+// first, rows up to a whole step zero (X has none there, and 0 times what lies there may be NaN).
+template <int DT>
+__device__ __forceinline__ void prep_block(const PrepTable& T, uint32_t b) {
+  int j = 0;
+  while (j + 1 < T.n && b >= T.p[j + 1].block0) ++j;
+  const Prep& a = T.p[j];
+  const int64_t block = b - a.block0, base = block * 256, r0 = base / a.per_row;
+  const uint32_t c = (uint32_t)(base - r0 * a.per_row) + threadIdx.x, d = c / a.per_row;
+  const int64_t row = r0 + d;
+  const uint32_t col = (c - d * a.per_row) * 8;
+  auto put = [&](int64_t at, const uint32_t* w) {
+    *(gmem((u32x4_t*)(a.dst + at * a.per_row * 8 + col))) = u32x4_t{w[0], w[1], w[2], w[3]};
+  };
+  if (a.e != nullptr) {
+    if (row >= a.rows) return;
+    const int64_t at = row * a.ld + col;
+    const u32x2_t q = *gmem((const u32x2_t*)((const int8_t*)a.src + at));
+    const float s = f32_from_bits((uint32_t)gmem(a.e)[at >> 5] << 23);
+    const uint32_t u[2] = {q.x ^ 0x80808080u, q.y ^ 0x80808080u};
+    uint32_t w[4];
+#pragma unroll
+    for (int h = 0; h < 4; ++h) {
+      const uint32_t v = u[h >> 1] >> (16 * (h & 1));
+      const uint32_t lo = bits_from_f32(((float)(v & 0xFFu) - 128.0f) * s);
+      const uint32_t hi = bits_from_f32(((float)((v >> 8) & 0xFFu) - 128.0f) * s);
+      w[h] = lo >> 16 | (hi & 0xFFFF0000u);
+    }
+    put(row, w);
+    return;
+  }
+  if (row >= a.part) return;
+  uint32_t y[8];
+#pragma unroll
+  for (int h = 0; h < 8; ++h) {
+    y[h] = 0;
+    if (row < a.rows && col + h < a.cols) y[h] = elem_bits<DT>(a.src, row * a.ld + col + h);
+  }
+  uint32_t w[4];
+  if constexpr (DT == ISO_BF16) {
+#pragma unroll
+    for (int h = 0; h < 4; ++h) w[h] = y[2 * h] | y[2 * h + 1] << 16;
+    put(row, w);
+  } else {
+    uint32_t p[3][8];
+#pragma unroll
+    for (int h = 0; h < 8; ++h) {
+      const bool finite = (y[h] & 0x7F800000u) != 0x7F800000u;
+      uint32_t hi = y[h] & 0xFFFF0000u;
+      if (!finite && (y[h] & 0x7FFFFFu)) hi |= 0x400000u;   // a NaN stays one
+      float r = finite ? f32_from_bits(y[h]) - f32_from_bits(hi) : 0.0f;
+      const uint32_t mid = bits_from_f32(r) & 0xFFFF0000u;
+      r -= f32_from_bits(mid);
+      p[2][h] = hi, p[1][h] = mid, p[0][h] = bits_from_f32(r);
+    }
+#pragma unroll
+    for (int part = 0; part < 3; ++part) {
+#pragma unroll
+      for (int h = 0; h < 4; ++h) w[h] = p[part][2 * h] >> 16 | (p[part][2 * h + 1] & 0xFFFF0000u);
+      put(part * a.part + row, w);
+    }
+  }
+}
+
+template <int DT>
+__global__ void __launch_bounds__(256) k_wgrad_prep(PrepTable T) {
+  if (blockIdx.x == 0 && threadIdx.x == 0) *T.status = 0;
+  for (uint32_t b = blockIdx.x; b < T.blocks; b += gridDim.x) prep_block<DT>(T, b);
+}
+
+// ---- the product ---------------------------------------------------------------------------------------------------
+
+struct Layer {
+  const uint8_t* y;            // bf16 dY and X, token rows
+  const uint8_t* x;
+  void* g;
+  int64_t y_ld, x_ld;          // row strides, bytes
+  int64_t y_bytes, x_bytes;    // bytes from the first element to past the last (dY: of all its parts)
+  int32_t rows, cols;          // of G
+  int32_t across;              // tiles of a tile row
+  int32_t steps, parts;        // steps of a part of dY
+  uint32_t tile0;
+};
+
+struct LayerTable {
+  Layer l[kLayers];
+  int n;
+  uint32_t tiles;     // of all layers
+  uint32_t whole;     // tiles one workgroup does alone; the others' tokens are split `split` ways
+  uint32_t split;
+  float* part;        // their partial sums, kTile * kTile a piece, (tile, piece) in order
+};
+
+typedef __attribute__((address_space(3))) uint8_t lds_u8;
+typedef short s16x4_t __attribute__((ext_vector_type(4)));
+typedef __attribute__((address_space(3))) s16x4_t* lds_frag;
+typedef __bf16 bf16x8_t __attribute__((ext_vector_type(8)));
+typedef float f32x16_t __attribute__((ext_vector_type(16)));
+
+// Descriptor of a buffer of `left` bytes: reads past its end give zeros.
+__device__ __forceinline__ u32x4_t buffer_of(const uint8_t* p, int64_t left) {
+  const uint64_t a = (uint64_t)p;
+  const uint32_t n = left <= 0 ? 0u : left > 0xFFFFFFF0ll ? 0xFFFFFFF0u : (uint32_t)left;
+  return u32x4_t{(uint32_t)a, (uint32_t)(a >> 32) & 0xFFFFu, n, 0x00027000u};
+}
+
+// 16 bytes a lane from the buffer into LDS, the wave's 1024 bytes one after another from byte `lds` on.  An instruction
+// of its own because the compiler waits for every such load before the next LDS read, whatever that reads; k_wgrad
+// counts them itself.  It has no destination register; m0 needs one instruction between its write and its use.
+#pragma clang diagnostic push
+#pragma clang diagnostic ignored "-Winline-asm"   // m0 among the clobbers
+__device__ __forceinline__ void load_lds(u32x4_t buffer, uint32_t lds, uint32_t offset) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(lds), "v"(offset), "s"(buffer)
+               : "m0");
+}
+#pragma clang diagnostic pop
+
+// 32 rows of 128 columns (132 floats apart in LDS) to G from row m, column n on, by one wave.  Rows whose length keeps
+// vectors aligned go 16 bytes a lane, others one element a lane with the lanes along the row.
+typedef __attribute__((address_space(3))) f32x4_t* lds_f32x4;
+typedef __attribute__((address_space(3))) float* lds_f32;
+
+constexpr int kRowBytes = 132 * 4;
+
+template <int DTG, bool ADD>
+__device__ __forceinline__ void write_rows(const Layer& a, int m, int n, uint32_t lds, int lane) {
+  constexpr int V = Fmt<DTG>::kPerVec, kLanes = 128 / V, kRows = 64 / kLanes;
+  if (a.cols % V == 0) {
+    const int row = lane / kLanes, c = lane % kLanes * V;
+    if (n + c >= a.cols) return;
+#pragma unroll 8
+    for (int h = 0; h < 32; h += kRows) {
+      if (m + h + row >= a.rows) continue;
+      const int64_t at = (int64_t)(m + h + row) * a.cols + n + c;
+      float v[V];
+#pragma unroll
+      for (int j = 0; j < V; j += 4) {
+        const f32x4_t x = *(lds_f32x4)(uintptr_t)(lds + (h + row) * kRowBytes + (c + j) * 4);
+        v[j] = x.x, v[j + 1] = x.y, v[j + 2] = x.z, v[j + 3] = x.w;
+      }
+      if constexpr (ADD) {
+        float old[V];
+        load_elems<DTG, V>(a.g, at, old);
+#pragma unroll
+        for (int j = 0; j < V; ++j) v[j] += old[j];
+      }
+      store_elems<DTG, V>(a.g, at, v);
+    }
+  } else {
+#pragma unroll 2
+    for (int h = 0; h < 32; ++h) {
+      if (m + h >= a.rows) break;
+#pragma unroll
+      for (int k = 0; k < 2; ++k) {
+        const int c = k * 64 + lane;
+        if (n + c >= a.cols) continue;
+        const int64_t at = (int64_t)(m + h) * a.cols + n + c;
+        float v = *(lds_f32)(uintptr_t)(lds + h * kRowBytes + c * 4);
+        if constexpr (ADD) {
+          float old;
+          load_elems<DTG, 1>(a.g, at, &old);
+          v += old;
+        }
+        store_elems<DTG, 1>(a.g, at, &v);
       }
     }
-    __syncthreads();
-    const int k = (lane >> 4) * 8, r = lane & 15;
-    bf16x8_t b[2];
-#pragma unroll
-    for (int j = 0; j < 2; ++j) b[j] = *(const bf16x8_t*)&B[wn + 16 * j + r][k];
-#pragma unroll
-    for (int p = kParts - 1; p >= 0; --p)
-#pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        const bf16x8_t x = *(const bf16x8_t*)&A[p][wm + 16 * i + r][k];
-#pragma unroll
-        for (int j = 0; j < 2; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x, b[j], acc[i][j], 0, 0, 0);
-      }
   }
+}
+
+template <int DTG>
+__device__ __forceinline__ void put4(void* g, int64_t at, const float* v, int left, bool aligned, bool add) {
+  float o[4] = {v[0], v[1], v[2], v[3]};
+  if (aligned) {
+    if (left <= 0) return;
+    if (add) {
+      float old[4];
+      load_elems<DTG, 4>(g, at, old);
 #pragma unroll
-  for (int i = 0; i < 2; ++i)
+      for (int h = 0; h < 4; ++h) o[h] += old[h];
+    }
+    store_elems<DTG, 4>(g, at, o);
+  } else {
 #pragma unroll
-    for (int j = 0; j < 2; ++j)
-#pragma unroll
-      for (int h = 0; h < 4; ++h) {
-        const int64_t m = m0 + wm + 16 * i + (lane >> 4) * 4 + h, n = n0 + wn + 16 * j + (lane & 15);
-        if (m >= a.rows || n >= a.cols) continue;
-        float g = acc[i][j][h];
-        if constexpr (ADD) {
-          float o;
-          load_elems<DTG, 1>(a.grad, m * a.cols + n, &o);
-          g += o;
-        }
-        store_elems<DTG, 1>(a.grad, m * a.cols + n, &g);
+    for (int h = 0; h < 4; ++h) {
+      if (h >= left) continue;
+      if (add) {
+        float old;
+        load_elems<DTG, 1>(g, at + h, &old);
+        o[h] += old;
       }
+      store_elems<DTG, 1>(g, at + h, o + h);
+    }
+  }
+}
+
+__device__ __forceinline__ int layer_of(const LayerTable& T, uint32_t tile) {
+  int j = 0;
+  while (j + 1 < T.n && tile >= T.l[j + 1].tile0) ++j;
+  return j;
+}
+
+// Origin of a layer's tile: bands of eight tile rows, walked down their columns, so that the 32 tiles an XCD works on
+// at once are 8 x 4 and share 12 panels in its L2.
+__device__ __forceinline__ void tile_origin(const Layer& a, uint32_t tile, int& m0, int& n0) {
+  const int t = (int)(tile - a.tile0), down = (a.rows + kTile - 1) / kTile;
+  const int band = t / (8 * a.across), r0 = band * 8, h = min(8, down - r0), in = t - r0 * a.across;
+  m0 = (r0 + in % h) * kTile;
+  n0 = in / h * kTile;
+}
+
+// Consecutive pieces of [0, n) for the workgroups of one XCD (workgroup b runs on XCD b % 8).
+__device__ __forceinline__ uint32_t by_xcd(uint32_t b, uint32_t n) {
+  const uint32_t x = b & 7u, each = n >> 3, more = n & 7u;
+  return x * each + min(x, more) + (b >> 3);
+}
+
+// One 256 x 256 tile of G (or a share of its tokens) a workgroup of four waves, each with 128 x 128 of it in 256
+// accumulator registers a lane.
+//   Steps of 32 tokens go from memory straight into LDS, four stages deep (two 16 KiB panels each, token rows of 512
+// bytes); both operands have their tokens along the slow dimension, so fragments come through the transposing LDS read,
+// 16 lanes a 4 token x 16 column block.  The four 64-byte pieces that the first (or second) half of a wave reads at once
+// come from four successive token rows; piece c of row t lies at c ^ (t & 3), which puts the four into different quarters
+// of the 64 banks (no conflicts counted), while 64 bytes of memory stay together.
+//   The loop is laid out by hand, one LDS read or load between two matrix instructions: fragments of the next half step
+// are read, and loads issued, under the 16 products of the current one.  At the middle of a step all its fragments are in
+// registers: one barrier there frees its stage and vouches for the next.
+//   Bound by the power that matrix products of full entropy take (the clock falls to about 1.9 GHz) and the loads' issue.
+template <int DTG, bool ADD>
+__global__ void __launch_bounds__(256, 1) k_wgrad(LayerTable T) {
+  extern __shared__ __attribute__((aligned(1024))) uint8_t smem[];
+  const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
+  uint32_t tile, piece = 0, pieces = 1;
+  if (blockIdx.x < T.whole) {
+    tile = by_xcd(blockIdx.x, T.whole);
+  } else {
+    const uint32_t rest = T.tiles - T.whole, u = by_xcd(blockIdx.x - T.whole, rest * T.split);
+    pieces = T.split;
+    piece = u / rest;
+    tile = T.whole + u - piece * rest;
+  }
+  const Layer& a = T.l[layer_of(T, tile)];
+  int m0, n0;
+  tile_origin(a, tile, m0, n0);
+  const int all = a.steps * a.parts;
+  const int first = (int)((int64_t)all * piece / pieces), last = (int)((int64_t)all * (piece + 1) / pieces);
+  const int steps = last - first;
+
+  // loads: 16-byte column c of token row 8 j + row
+  const int row = 2 * w + (lane >> 5), c = lane & 31;
+  const uint32_t col = (uint32_t)(((c >> 2) ^ (row & 3)) * 64 + (c & 3) * 16);
+  uint32_t vy[4], vx[4];
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    vy[j] = (uint32_t)(row + 8 * j) * (uint32_t)a.y_ld + col;
+    vx[j] = (uint32_t)(row + 8 * j) * (uint32_t)a.x_ld + col;
+  }
+  const uint8_t* const x_base = a.x + 2 * (int64_t)n0;
+  const int64_t x_left0 = a.x_bytes - 2 * (int64_t)n0, y_step = kStep * a.y_ld, x_step = kStep * a.x_ld;
+  int x_at = a.steps > 0 ? first % a.steps : 0;
+  const uint8_t *yp = a.y + 2 * (int64_t)m0 + first * y_step, *xp = x_base + x_at * x_step;
+  int64_t y_left = a.y_bytes - 2 * (int64_t)m0 - first * y_step, x_left = x_left0 - x_at * x_step;
+  int to_load = steps;
+  u32x4_t yb, xb;
+  auto next = [&] {   // descriptors of the next step's panels; empty past the last
+    yb = buffer_of(yp, to_load > 0 ? y_left : 0);
+    xb = buffer_of(xp, to_load > 0 ? x_left : 0);
+    --to_load;
+    yp += y_step, y_left -= y_step, xp += x_step, x_left -= x_step;
+    if (++x_at == a.steps) x_at = 0, xp = x_base, x_left = x_left0;
+  };
+  const uint32_t lds0 = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(lds_u8*)smem);
+  auto load = [&](int j, int stage) {
+    const uint32_t to = lds0 + stage * kStageBytes + w * 1024;
+    if (j < 4) load_lds(yb, to + j * 4096, vy[j]);
+    else load_lds(xb, to + kStageBytes / 2 + (j - 4) * 4096, vx[j - 4]);
+  };
+
+  // fragments f of 32 columns: lane's token rows (lane / 32) * 8 ..., columns lane % 32
+  const int g = lane >> 4, i = lane & 15;
+  uint32_t ay[4], ax[4];
+#pragma unroll
+  for (int f = 0; f < 4; ++f) {
+    const uint32_t at = lds0 + ((g >> 1) * 8 + (i >> 2)) * 512 + (f ^ (i >> 2)) * 64 + (g & 1) * 32 + (i & 3) * 8;
+    ay[f] = at + (w >> 1) * 256;
+    ax[f] = at + (w & 1) * 256 + kStageBytes / 2;
+  }
+  struct Frag {
+    s16x4_t h[2];
+  };
+  Frag fx[2][4], fy[2][4];
+  auto read = [&](int set, int q, uint32_t offset) {   // piece q of 16: x0 y0 y1 y2 y3 x1 x2 x3, two halves each
+    const int n = q >> 1, h = q & 1;
+    const uint32_t at = (n == 0 ? ax[0] : n < 5 ? ay[n - 1] : ax[n - 4]) + offset + h * 2048;
+    const s16x4_t v = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_frag)(uintptr_t)at);
+    if (n == 0) fx[set][0].h[h] = v;
+    else if (n < 5) fy[set][n - 1].h[h] = v;
+    else fx[set][n - 4].h[h] = v;
+  };
+  f32x16_t acc[4][4];
+#pragma unroll
+  for (int p = 0; p < 4; ++p)
+#pragma unroll
+    for (int q = 0; q < 4; ++q) acc[p][q] = 0.0f;
+  auto multiply = [&](int set, int q) {
+    acc[q >> 2][q & 3] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, fx[set][q >> 2]),
+                                                                 __builtin_bit_cast(bf16x8_t, fy[set][q & 3]),
+                                                                 acc[q >> 2][q & 3], 0, 0, 0);
+  };
+
+  // the last stage's X panel is loaded in the first step
+  for (int s = 0; s < kStages; ++s) {
+    next();
+#pragma unroll
+    for (int j = 0; j < 8; ++j)
+      if (s < kStages - 1 || j < 4) load(j, s);
+  }
+  asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" ::"n"((kStages - 2) * 8 + 4) : "memory");
+#pragma unroll
+  for (int q = 0; q < 16; ++q) read(0, q, 0);
+  int stage = 0, before = kStages - 1;
+  for (int t = 0; t < steps; ++t) {
+    const int after = stage + 1 == kStages ? 0 : stage + 1;
+#pragma unroll
+    for (int q = 0; q < 16; ++q) {
+      read(1, q, stage * kStageBytes + 8192);
+      multiply(0, q);
+      if ((q & 3) == 1) load(4 + (q >> 2), before);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+    next();
+    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"((kStages - 2) * 8) : "memory");
+    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+    for (int q = 0; q < 16; ++q) {
+      read(0, q, after * kStageBytes);
+      multiply(1, q);
+      if ((q & 3) == 1) load(q >> 2, stage);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+    before = stage;
+    stage = after;
+  }
+  asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");   // no load may reach LDS after the workgroup's end
+
+  // a lane holds four consecutive columns of a row in every four registers
+  if (pieces > 1) {
+    float* const out = T.part + ((int64_t)(tile - T.whole) * pieces + piece) * (kTile * kTile) + w * (128 * 128);
+#pragma unroll
+    for (int q = 0; q < 4; ++q)
+#pragma unroll
+      for (int p = 0; p < 4; ++p)
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+          store_elems<ISO_F32, 4>(out, ((q * 4 + p) * 4 + r) * 256 + lane * 4, (const float*)&acc[p][q] + 4 * r);
+    return;
+  }
+  // through LDS, 32 rows of the wave's 128 x 128 at a time, so that memory sees whole rows
+  asm volatile("s_barrier" ::: "memory");   // every wave is past its last fragment
+  const uint32_t own = lds0 + w * (32 * kRowBytes);
+  const int mw = m0 + (w >> 1) * 128, nw = n0 + (w & 1) * 128;
+#pragma unroll
+  for (int q = 0; q < 4; ++q) {
+#pragma unroll
+    for (int p = 0; p < 4; ++p)
+#pragma unroll
+      for (int r = 0; r < 4; ++r)
+        *(lds_f32x4)(uintptr_t)(own + (lane & 31) * kRowBytes + (p * 32 + r * 8 + (lane >> 5) * 4) * 4) =
+            f32x4_t{acc[p][q][4 * r], acc[p][q][4 * r + 1], acc[p][q][4 * r + 2], acc[p][q][4 * r + 3]};
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    write_rows<DTG, ADD>(a, mw + q * 32, nw, own, lane);
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+  }
+}
+
+// Adds up the pieces of the split tiles, in order: a thread four columns of a row, 64 workgroups a tile.
+template <int DTG, bool ADD>
+__global__ void __launch_bounds__(256) k_wgrad_join(LayerTable T) {
+  const uint32_t r = blockIdx.x >> 6, tile = T.whole + r;
+  const Layer& a = T.l[layer_of(T, tile)];
+  int m0, n0;
+  tile_origin(a, tile, m0, n0);
+  const int at = (int)(blockIdx.x & 63u) * 1024 + threadIdx.x * 4;
+  const float* const in = T.part + (int64_t)r * T.split * (kTile * kTile) + at;
+  const int w = at >> 14, q = (at >> 12) & 3, p = (at >> 10) & 3, h = (at >> 8) & 3, lane = (at >> 2) & 63;
+  const int m = m0 + (w >> 1) * 128 + q * 32 + (lane & 31);
+  const int n = n0 + (w & 1) * 128 + p * 32 + h * 8 + (lane >> 5) * 4;
+  if (m >= a.rows || n >= a.cols) return;
+  float sum[4] = {};
+  for (uint32_t s = 0; s < T.split; ++s) {
+    float v[4];
+    load_elems<ISO_F32, 4>(in, (int64_t)s * (kTile * kTile), v);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) sum[j] += v[j];
+  }
+  put4<DTG>(a.g, (int64_t)m * a.cols + n, sum, a.cols - n, (a.cols & 3) == 0, ADD);
+}
+
+// ---- host ----------------------------------------------------------------------------------------------------------
+
+// What up to 16 layers take: the tables of their launches, with workspace offsets in place of pointers until bound.
+struct Plan {
+  PrepTable prep{};
+  LayerTable layers{};
+  size_t total = 0;
+};
+
+bool direct(const iso_weight_grad& x, int dt) { return dt == ISO_BF16 && x.ld_dy % 8 == 0 && x.ld_dy <= kMaxStride; }
+
+int64_t whole_steps(int64_t tokens) { return (tokens + kStep - 1) / kStep * kStep; }
+
+// Pieces that the tiles past the last full round of workgroups are split into: the fewest microseconds of
+// a round of `steps` / s steps (0.45 us each), and where s > 1 of writing and adding up the pieces (8 us for the launch,
+// 0.1 us for each piece of 256 KiB).
+uint32_t pieces_for(uint32_t rest, int steps) {
+  uint32_t best = 1;
+  double least = 0.45 * steps;
+  for (uint32_t s = 2; s <= kUnits / std::max(rest, 1u) && s <= (uint32_t)steps; ++s) {
+    const double t = 0.45 * ((steps + s - 1) / s) + 8.0 + 0.1 * rest * s;
+    if (t < least) least = t, best = s;
+  }
+  return best;
+}
+
+Plan plan_layers(const iso_weight_grad* g, int n, int dt, bool accumulate, uint8_t* ws) {
+  Plan P;
+  size_t at = kStatusBytes;
+  auto region = [&](size_t bytes) {
+    const size_t o = at;
+    at = align_up(at + bytes, 256);
+    return ws + o;
+  };
+  const int parts = dt == ISO_F32 ? 3 : 1;
+  struct Kept {
+    const iso_ckpt* c;
+    const uint8_t* x;
+  };
+  std::vector<Kept> kept;
+  std::vector<Layer> layers;
+  auto add_prep = [&](Prep p, int64_t rows) {
+    p.block0 = P.prep.blocks;
+    P.prep.blocks += (uint32_t)((rows * p.per_row + 255) / 256);
+    P.prep.p[P.prep.n++] = p;
+  };
+  for (int j = 0; j < n; ++j) {
+    const iso_weight_grad& x = g[j];
+    const int64_t t = x.in.rows;
+    if (x.rows == 0 || x.in.cols == 0 || (t == 0 && accumulate)) continue;
+    Layer l{};
+    l.g = x.grad;
+    l.rows = (int32_t)x.rows, l.cols = (int32_t)x.in.cols;
+    l.across = (l.cols + kTile - 1) / kTile;
+    l.steps = (int32_t)(whole_steps(t) / kStep);
+    l.parts = parts;
+    const int64_t ld = ckpt_ld(x.in.cols);
+    l.x_ld = 2 * ld, l.x_bytes = 2 * t * ld;
+    if (t > 0) {
+      for (const Kept& k : kept)
+        if (x.in.q != nullptr && k.c->q == x.in.q && k.c->e == x.in.e && k.c->rows == t && k.c->cols == x.in.cols) l.x = k.x;
+      if (l.x == nullptr) {
+        uint8_t* const to = region(2 * (size_t)(t * ld));
+        add_prep(Prep{x.in.q, x.in.e, (uint16_t*)to, t, ld, 0, (uint32_t)ld, (uint32_t)(ld / 8), 0}, t);
+        kept.push_back(Kept{&x.in, to});
+        l.x = to;
+      }
+      if (direct(x, dt)) {
+        l.y = (const uint8_t*)x.dy;
+        l.y_ld = 2 * x.ld_dy;
+        l.y_bytes = (int64_t)align_up(2 * (size_t)((t - 1) * x.ld_dy + x.rows), 16);
+      } else {
+        const int64_t per = (x.rows + 7) / 8, part = whole_steps(t);
+        uint8_t* const to = region(2 * (size_t)(parts * part * per * 8));
+        add_prep(Prep{x.dy, nullptr, (uint16_t*)to, t, x.ld_dy, part, (uint32_t)x.rows, (uint32_t)per, 0}, part);
+        l.y = to;
+        l.y_ld = 16 * per;
+        l.y_bytes = 16 * parts * part * per;
+      }
+    }
+    layers.push_back(l);
+  }
+  // long sums first: the tiles past the last full round, which may be split, are then the shortest
+  std::stable_sort(layers.begin(), layers.end(), [](const Layer& a, const Layer& b) { return a.steps > b.steps; });
+  LayerTable& L = P.layers;
+  for (Layer& l : layers) {
+    l.tile0 = L.tiles;
+    L.tiles += (uint32_t)((l.rows + kTile - 1) / kTile * l.across);
+    L.l[L.n++] = l;
+  }
+  L.whole = L.tiles / kUnits * kUnits;
+  L.split = 1;
+  if (L.tiles > L.whole) {
+    int steps = 0;
+    for (const Layer& l : layers)
+      if (l.tile0 + (uint32_t)((l.rows + kTile - 1) / kTile * l.across) > L.whole) steps = std::max(steps, l.steps * l.parts);
+    L.split = pieces_for(L.tiles - L.whole, steps);
+    if (L.split == 1) L.whole = L.tiles;
+  }
+  L.part = (float*)region(sizeof(float) * kTile * kTile * (size_t)(L.tiles - L.whole) * L.split);
+  P.prep.status = (uint32_t*)ws;
+  P.total = at;
+  return P;
+}
+
+template <int DTG, bool ADD>
+void launch(const LayerTable& L, hipStream_t s) {
+  const uint32_t rest = L.tiles - L.whole;
+  k_wgrad<DTG, ADD><<<L.whole + rest * L.split, 256, kStages * kStageBytes, s>>>(L);
+  if (rest > 0) k_wgrad_join<DTG, ADD><<<rest * 64, 256, 0, s>>>(L);
 }
 
 }  // namespace
 
-size_t weight_grad_workspace_bytes(const iso_weight_grad*, int, int) { return kStatusBytes; }
+size_t weight_grad_workspace_bytes(const iso_weight_grad* g, int n, int dt) {
+  size_t most = kStatusBytes;
+  for (int j = 0; j < n; j += kLayers) most = std::max(most, plan_layers(g + j, std::min(kLayers, n - j), dt, false, nullptr).total);
+  return most;
+}
 
-hipError_t run_weight_grad(const iso_weight_grad* g, int n, int dt, int dt_grad, bool accumulate, uint8_t* ws,
-                           hipStream_t s) {
-  const hipError_t e = fill_u32((uint32_t*)ws, kStatusBytes / 4, 0u, s);
-  if (e != hipSuccess) return e;
-  for (int j = 0; j < n; ++j) {
-    const iso_weight_grad& x = g[j];
-    if (x.rows == 0 || x.in.cols == 0) continue;
-    const Job a{x.in.q, x.in.e, x.dy, x.grad, x.in.rows, x.ld_dy, ckpt_ld(x.in.cols), (int32_t)x.rows, (int32_t)x.in.cols};
-    const unsigned grid = (unsigned)(((x.in.cols + kTile - 1) / kTile) * ((x.rows + kTile - 1) / kTile));
-    auto go = [&](auto k) { k<<<grid, 256, 0, s>>>(a); };
-    if (dt == ISO_BF16 && dt_grad == ISO_BF16) accumulate ? go(k_wgrad<ISO_BF16, ISO_BF16, true>) : go(k_wgrad<ISO_BF16, ISO_BF16, false>);
-    else if (dt == ISO_BF16) accumulate ? go(k_wgrad<ISO_BF16, ISO_F32, true>) : go(k_wgrad<ISO_BF16, ISO_F32, false>);
-    else if (dt_grad == ISO_BF16) accumulate ? go(k_wgrad<ISO_F32, ISO_BF16, true>) : go(k_wgrad<ISO_F32, ISO_BF16, false>);
-    else accumulate ? go(k_wgrad<ISO_F32, ISO_F32, true>) : go(k_wgrad<ISO_F32, ISO_F32, false>);
+hipError_t run_weight_grad(const iso_weight_grad* g, int n, int dt, int dt_grad, bool accumulate, uint8_t* ws, hipStream_t s) {
+  for (int j = 0; j < n || j == 0; j += kLayers) {
+    const Plan P = plan_layers(g + j, std::min(kLayers, n - j), dt, accumulate, ws);
+    const unsigned grid = std::min(std::max(P.prep.blocks, 1u), 1u << 22);
+    if (dt == ISO_BF16) k_wgrad_prep<ISO_BF16><<<grid, 256, 0, s>>>(P.prep);
+    else k_wgrad_prep<ISO_F32><<<grid, 256, 0, s>>>(P.prep);
+    if (P.layers.tiles > 0) {
+      if (dt_grad == ISO_BF16) accumulate ? launch<ISO_BF16, true>(P.layers, s) : launch<ISO_BF16, false>(P.layers, s);
+      else accumulate ? launch<ISO_F32, true>(P.layers, s) : launch<ISO_F32, false>(P.layers, s);
+    }
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
   }
-  return hipGetLastError();
+  return hipSuccess;
 }
 
 }  // namespace iso
