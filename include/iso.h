@@ -510,10 +510,10 @@ iso_status iso_embed_lookup(const iso_embed* e, int dt, void* ws, size_t ws_byte
 
 /*
  * iso_embed_grad -- the lookup's gradient: G[v] = round(scale * sum of dX_i over
- * the tokens i with id_i = v), the sum in binary32 over the tokens sorted by id,
- * in token order in runs of 32 whose sums are added in order.  Padding (and an id
- * outside the vocabulary, reported as above) adds nothing, whatever its row of
- * dX holds.  dX (e->x) is of type dt, G of type dt_grad.
+ * the tokens i with id_i = v), the sum in binary32 over the tokens sorted by id
+ * (in token order up to 32 of them; more in runs of 32 whose sums are added).
+ * Padding (and an id outside the vocabulary, reported as above) adds nothing,
+ * whatever its row of dX holds.  dX (e->x) is of type dt, G of type dt_grad.
  * accumulate = 0: every row of G is written (zero where no token has the id);
  * accumulate = 1: G[v] = round(G[v] + scale * sum) in place, and rows that no
  * token has are neither read nor written.

@@ -21,7 +21,7 @@ namespace {
 
 // Workgroups of a launch over `n` pieces of work, which the kernels walk in strides of the grid (a launch holds fewer
 // than 2^32 threads).
-unsigned grid_for(int64_t n) { return (unsigned)std::min<int64_t>(std::max<int64_t>(n, 1), 1 << 23); }
+unsigned grid_for(int64_t n) { return (unsigned)std::min<int64_t>(std::max<int64_t>(n, 1), 1 << 22); }
 
 struct Ids {
   const void* p;
@@ -39,13 +39,13 @@ __device__ __forceinline__ int32_t row_of(const Ids& ids, int64_t t) {
 
 // ---- lookup --------------------------------------------------------------------------------------------------------
 
-constexpr int kLookupItems = 4;   // 16-byte vectors (or elements) a thread
+constexpr int kLookupItems = 4;   // 16-byte vectors a thread
 constexpr int kLookupBlock = 256 * kLookupItems;
 
 // Workgroup 0 looks at every id and writes the status word, so that the call is one launch: nothing has to be
 // cleared before the others find a bad id.  The others copy 1024 vectors each, numbered through tokens and columns:
 // a thread's four ids, and then its four vectors, are in flight together.
-template <int DT, bool VEC>
+template <int DT>
 __global__ void __launch_bounds__(256) k_embed_lookup(Ids ids, const void* __restrict__ table, void* __restrict__ x,
                                                       int64_t tokens, int64_t dim, int64_t ld_x, float scale,
                                                       uint32_t* status) {
@@ -60,49 +60,44 @@ __global__ void __launch_bounds__(256) k_embed_lookup(Ids ids, const void* __res
     if (threadIdx.x == 0) *status = any ? kStatusIndex : 0u;
     return;
   }
-  constexpr int V = VEC ? Fmt<DT>::kPerVec : 1;
-  const uint32_t per_row = (uint32_t)(dim / V);
+  constexpr int V = kVec<DT>;
+  const uint32_t per_row = (uint32_t)((dim + V - 1) / V);
   const int64_t items = tokens * per_row, step = (int64_t)(gridDim.x - 1) * kLookupBlock;
   for (int64_t base = (int64_t)(blockIdx.x - 1) * kLookupBlock; base < items; base += step) {
     const int64_t t0 = base / per_row;
     const uint32_t c0 = (uint32_t)(base - t0 * per_row);
-    int64_t tok[kLookupItems];
-    uint32_t col[kLookupItems];
+    int64_t tok[kLookupItems], col[kLookupItems];
     int32_t row[kLookupItems];
 #pragma unroll
     for (int q = 0; q < kLookupItems; ++q) {
       const uint32_t r = c0 + q * 256 + threadIdx.x, d = r / per_row;
       tok[q] = t0 + d;
-      col[q] = r - d * per_row;
+      col[q] = (int64_t)(r - d * per_row) * V;
       row[q] = tok[q] < tokens ? row_of(ids, tok[q]) : -1;
     }
-    float v[kLookupItems][V];
+    u32x4_t w[kLookupItems];
 #pragma unroll
     for (int q = 0; q < kLookupItems; ++q) {
-#pragma unroll
-      for (int j = 0; j < V; ++j) v[q][j] = 0.0f;
-      if (row[q] >= 0) load_elems<DT, V>(table, (int64_t)row[q] * dim + (int64_t)col[q] * V, v[q]);
+      w[q] = u32x4_t{0, 0, 0, 0};
+      if (row[q] >= 0) w[q] = load_raw<DT>(table, row[q] * dim + col[q], dim - col[q]);
     }
 #pragma unroll
     for (int q = 0; q < kLookupItems; ++q) {
       if (tok[q] >= tokens) continue;
-      if (row[q] >= 0) {
+      float v[V];
+      unpack_raw<DT>(w[q], v);
 #pragma unroll
-        for (int j = 0; j < V; ++j) v[q][j] *= scale;
-      }
-      store_elems<DT, V>(x, tok[q] * ld_x + (int64_t)col[q] * V, v[q]);
+      for (int j = 0; j < V; ++j) v[j] = row[q] >= 0 ? v[j] * scale : 0.0f;
+      store_elems<DT, V>(x, tok[q] * ld_x + col[q], v, dim - col[q]);
     }
   }
 }
 
-// ---- gradient: the sort --------------------------------------------------------------------------------------------
+// ---- gradient: shared pieces ---------------------------------------------------------------------------------------
 
-constexpr int kMaxBuckets = 512;
-constexpr int kMaxTiles = 64;
-constexpr int kMinTile = 1024;
-constexpr int kRun = 32;          // tokens of one partial sum
-constexpr int kSlotSpan = 16;     // an id with m > kRun tokens from sorted position p on owns slots p/16 ...:
-                                  // ceil(m/32) <= floor(m/16) of them, so no two ids share one
+// The tokens of an id are added in runs of kRun, whose sums are then added in order.
+constexpr int kRun = 32;
+constexpr int kFlight = 8;     // rows whose loads are in flight together
 
 // Lanes of the wave whose key equals this lane's (of those with `on`), by one ballot per key bit.
 __device__ __forceinline__ uint64_t peers(uint32_t key, int bits, bool on) {
@@ -114,374 +109,590 @@ __device__ __forceinline__ uint64_t peers(uint32_t key, int bits, bool on) {
   return m;
 }
 
-// Counts per (tile, bucket); tokens outside the vocabulary are noted per tile, no slot is taken yet.
-__global__ void __launch_bounds__(256) k_embed_count(Ids ids, int64_t tokens, int64_t tile, int shift, int buckets,
+// Where the tokens of the wave's lanes go, each with the counter `key` of its next place (one counter per key and wave):
+// equal keys take successive places in lane order, and their counter moves past them.  Every lane calls it.
+__device__ __forceinline__ uint32_t take_places(uint32_t* counters, uint32_t key, int bits, bool on) {
+  const uint64_t m = peers(key, bits, on);
+  const int lane = threadIdx.x & 63, lead = on ? __ffsll((unsigned long long)m) - 1 : lane;
+  uint32_t at = 0;
+  if (on && lane == lead) at = atomicAdd(&counters[key], (uint32_t)__popcll(m));
+  return (uint32_t)__shfl((int)at, lead) + __popcll(m & ((1ull << lane) - 1));
+}
+
+// Sum of `value` over the threads before this one, and the workgroup's total; WAVES waves, scratch of as many words.
+template <int WAVES>
+__device__ __forceinline__ uint32_t scan_block(uint32_t value, uint32_t* scratch, uint32_t& total) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  uint32_t sum = value;
+#pragma unroll
+  for (int d = 1; d < 64; d <<= 1) {
+    const uint32_t v = (uint32_t)__shfl_up((int)sum, d);
+    if (lane >= d) sum += v;
+  }
+  if (lane == 63) scratch[wave] = sum;
+  __syncthreads();
+  uint32_t before = 0;
+  total = 0;
+#pragma unroll
+  for (int w = 0; w < WAVES; ++w) {
+    const uint32_t v = scratch[w];
+    if (w < wave) before += v;
+    total += v;
+  }
+  __syncthreads();
+  return before + sum - value;
+}
+
+struct Rows {
+  const void* x;
+  void* grad;
+  int64_t dim, ld_x;
+  float scale;
+};
+
+// acc += the rows of dX of up to 64 tokens (lane l holds the l-th) for this lane's columns, in order.
+template <int DT>
+__device__ __forceinline__ void add_rows(const Rows& a, uint32_t mine, uint32_t count, int64_t col, float* acc) {
+  const int64_t left = a.dim - col;
+  const uint32_t m = __builtin_amdgcn_readfirstlane(count);
+  for (uint32_t q = 0; q < m; q += kFlight) {
+    u32x4_t w[kFlight];
+#pragma unroll
+    for (int h = 0; h < kFlight; ++h)
+      if (q + h < m) {
+        const int64_t row = (int64_t)(uint32_t)__builtin_amdgcn_readlane((int)mine, (int)(q + h)) * a.ld_x;
+        if (left > 0) w[h] = load_raw<DT>(a.x, row + col, left);
+      }
+#pragma unroll
+    for (int h = 0; h < kFlight; ++h)
+      if (q + h < m) {
+        float v[kVec<DT>];
+        unpack_raw<DT>(w[h], v);
+#pragma unroll
+        for (int j = 0; j < kVec<DT>; ++j) acc[j] += v[j];
+      }
+  }
+}
+
+template <int DT, int DTG, bool ADD>
+__device__ __forceinline__ void finish_row(const Rows& a, int64_t v, int64_t col, const float* acc) {
+  constexpr int V = kVec<DT>;
+  if (col >= a.dim) return;
+  float g[V];
+  if constexpr (ADD) load_elems<DTG, V>(a.grad, v * a.dim + col, g, a.dim - col);
+#pragma unroll
+  for (int j = 0; j < V; ++j) g[j] = ADD ? g[j] + a.scale * acc[j] : a.scale * acc[j];
+  store_elems<DTG, V>(a.grad, v * a.dim + col, g, a.dim - col);
+}
+
+// Ids are dealt to 1 << log2 buckets by their low bits, which spreads the frequent ones (low ids, in most vocabularies);
+// id v is local id v >> log2 of bucket v & mask.
+struct Buckets {
+  int log2;
+  int32_t width;     // local ids of a bucket
+  int bits;          // of a local id
+};
+
+// Zeros over the gradient, one vector a thread in memory order: written so, memory takes 6.9 TB/s on a 1.1 GB
+// gradient, against 5 to 6 where threads write several vectors or waves follow the rows.
+struct Fill {
+  void* p;
+  int64_t vectors;     // of 16 bytes
+  int32_t tail;        // 2-byte words after the last vector
+};
+
+__device__ __forceinline__ void fill_zeros(const Fill& f, uint32_t block, uint32_t blocks) {
+  for (int64_t v = (int64_t)block * 256 + threadIdx.x; v < f.vectors; v += (int64_t)blocks * 256)
+    gmem((u32x4_t*)f.p)[v] = u32x4_t{0, 0, 0, 0};
+  if (block == 0 && (int)threadIdx.x < f.tail) gmem((uint16_t*)f.p)[f.vectors * 8 + threadIdx.x] = 0;
+}
+
+// ---- gradient: few tokens, one launch ------------------------------------------------------------------------------
+
+// Up to 4096 tokens of a 151936 x 1536 table are added in 24 us this way and in 38 by the launches below (2048: 18 and 35);
+// 4096 tokens of one id, the worst case, in 98 and 44.
+constexpr int kFewTokens = 4096;
+constexpr int kFewWaves = 8;
+constexpr int kFewWidth = 512;   // local ids of a bucket, at most
+
+// A workgroup per bucket and column block: it reads all ids (eight a thread at most), keeps its own, sorts them in LDS and
+// writes its rows that have tokens, with `zeros` the others too.  Ids with more than kRun tokens are done last, a run a wave.
+template <int DT, int DTG, bool ADD>
+__global__ void __launch_bounds__(64 * kFewWaves) k_embed_few(Ids ids, int tokens, Buckets B, int64_t blocks, Rows a,
+                                                              bool zeros, uint32_t* status) {
+  constexpr int V = kVec<DT>, kThreads = 64 * kFewWaves, kIds = kFewTokens / kThreads, kCols = 64 * V;
+  constexpr int kEach = kFewWidth / kThreads;
+  __shared__ union {
+    uint32_t cnt[kFewWaves][kFewWidth];   // per wave and local id: the next place in perm
+    float part[kFewWaves][kCols];
+  } u;
+  __shared__ uint16_t perm[kFewTokens];
+  __shared__ uint16_t start[kFewWidth], count[kFewWidth];
+  __shared__ uint16_t some[kFewWidth], many[kFewTokens / kRun];   // local ids with up to kRun tokens, and with more
+  __shared__ uint32_t scratch[kFewWaves], n_some, n_many;
+  const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
+  const uint32_t bucket = (uint32_t)(blockIdx.x / blocks);
+  const int64_t col = (int64_t)(blockIdx.x - bucket * blocks) * kCols + lane * V;
+  const uint32_t mask = (1u << B.log2) - 1;
+  if (tid == 0) n_some = n_many = 0;
+  for (int q = tid; q < kFewWaves * kFewWidth; q += kThreads) (&u.cnt[0][0])[q] = 0;
+  // each wave takes successive tokens
+  const int per = (tokens + kThreads - 1) / kThreads * 64, t0 = wave * per + lane;
+  int32_t row[kIds];
+#pragma unroll
+  for (int k = 0; k < kIds; ++k) {
+    row[k] = -1;
+    if (64 * k < per && t0 + 64 * k < tokens) row[k] = row_of(ids, t0 + 64 * k);
+  }
+  bool bad = false;
+  int mine = 0;
+#pragma unroll
+  for (int k = 0; k < kIds; ++k) {
+    bad |= row[k] == -2;
+    row[k] = row[k] >= 0 && ((uint32_t)row[k] & mask) == bucket ? row[k] >> B.log2 : -1;
+    mine += row[k] >= 0;
+  }
+  const bool any = __syncthreads_or(mine);
+  if (blockIdx.x == 0) {
+    const bool wrong = __syncthreads_or(bad);
+    if (tid == 0) *status = wrong ? kStatusIndex : 0u;
+  }
+  if (any) {
+#pragma unroll
+    for (int k = 0; k < kIds; ++k)
+      if (row[k] >= 0) atomicAdd(&u.cnt[wave][row[k]], 1u);
+    __syncthreads();
+    uint32_t c[kEach][kFewWaves], n[kEach], sum = 0, total;
+#pragma unroll
+    for (int h = 0; h < kEach; ++h) {
+      n[h] = 0;
+#pragma unroll
+      for (int w = 0; w < kFewWaves; ++w) n[h] += c[h][w] = u.cnt[w][tid * kEach + h];
+      sum += n[h];
+    }
+    uint32_t at = scan_block<kFewWaves>(sum, scratch, total);
+#pragma unroll
+    for (int h = 0; h < kEach; ++h) {
+      const int q = tid * kEach + h;
+      start[q] = (uint16_t)at;
+      count[q] = (uint16_t)n[h];
+      // in any order: each is done by itself
+      if (n[h] > kRun) many[atomicAdd(&n_many, 1u)] = (uint16_t)q;
+      else if (n[h] > 0) some[atomicAdd(&n_some, 1u)] = (uint16_t)q;
+#pragma unroll
+      for (int w = 0; w < kFewWaves; ++w) {
+        u.cnt[w][q] = at;
+        at += c[h][w];
+      }
+    }
+    __syncthreads();
+#pragma unroll
+    for (int k = 0; k < kIds; ++k) {
+      if (__ballot(row[k] >= 0) == 0) continue;
+      const uint32_t to = take_places(u.cnt[wave], row[k] >= 0 ? row[k] : 0, B.bits, row[k] >= 0);
+      if (row[k] >= 0) perm[to] = (uint16_t)(t0 + 64 * k);
+    }
+    __syncthreads();
+  }
+  if (zeros) {
+    const float zero[V] = {};
+    for (int q = wave; q < B.width; q += kFewWaves) {
+      const int64_t v = ((int64_t)q << B.log2) + bucket;
+      if (v < ids.vocab && (!any || count[q] == 0)) finish_row<DT, DTG, false>(a, v, col, zero);
+    }
+  }
+  if (!any) return;
+  const uint32_t few = n_some, hot = n_many;
+  for (uint32_t h = wave; h < few; h += kFewWaves) {
+    const uint32_t q = some[h], m = count[q];
+    float acc[V] = {};
+    add_rows<DT>(a, (uint32_t)lane < m ? perm[start[q] + lane] : 0u, m, col, acc);
+    finish_row<DT, DTG, ADD>(a, ((int64_t)q << B.log2) + bucket, col, acc);
+  }
+  for (uint32_t h = 0; h < hot; ++h) {
+    const uint32_t q = many[h], s = start[q], e = s + count[q];
+    float out[V] = {};
+    for (uint32_t r0 = s; r0 < e; r0 += kRun * kFewWaves) {
+      __syncthreads();
+      const uint32_t r = r0 + wave * kRun, m = r < e ? min(e - r, (uint32_t)kRun) : 0u;
+      if (m > 0) {
+        float acc[V] = {};
+        add_rows<DT>(a, (uint32_t)lane < m ? perm[r + lane] : 0u, m, col, acc);
+#pragma unroll
+        for (int j = 0; j < V; ++j) u.part[wave][j * 64 + lane] = acc[j];
+      }
+      __syncthreads();
+      if (wave == 0)
+        for (int w = 0; w < kFewWaves && r0 + w * kRun < e; ++w)
+#pragma unroll
+          for (int j = 0; j < V; ++j) out[j] += u.part[w][j * 64 + lane];
+    }
+    if (wave == 0) finish_row<DT, DTG, ADD>(a, ((int64_t)q << B.log2) + bucket, col, out);
+  }
+}
+
+__global__ void __launch_bounds__(256) k_embed_fill(Fill f) { fill_zeros(f, blockIdx.x, gridDim.x); }
+
+// ---- gradient: many tokens -----------------------------------------------------------------------------------------
+//
+// Count (with further workgroups that write the gradient's zeros), scatter into buckets, sort each bucket, partial sums of
+// frequent ids, rows.  32768 tokens into 152064 x 3584 in bf16: 274 us, of which the zeros take 150 (1.09 GB), the sort's
+// latencies 20, the reads of dX and the rows that have tokens the rest; their bytes alone would take 209.  Spreading the zeros
+// over the first four launches, under whose latencies they would hide, gained nothing (270 to 280 us).
+
+constexpr int kMaxTiles = 64;
+constexpr int kMinTile = 1024;
+constexpr int kMaxBuckets = 512;
+constexpr int kMaxWidth = ISO_EMBED_MAX_VOCAB / kMaxBuckets;
+
+// Distinct ids and the runs of frequent ones, appended bucket by bucket in any order (each is worked on by itself).
+struct Lists {
+  uint32_t* n;       // ids, runs, frequent ids
+  uint4* ids;        // id, first sorted position, tokens (at most kRun)
+  uint2* runs;       // first sorted position, tokens
+  uint4* many;       // id with more than kRun tokens, its first run, its runs
+};
+
+// Tokens per (tile, bucket); tokens outside the vocabulary are noted per tile, the lists are empty yet.
+__global__ void __launch_bounds__(256) k_embed_count(Ids ids, int64_t tokens, int64_t tile, int tiles, Buckets B,
                                                      uint32_t* __restrict__ hist, uint32_t* __restrict__ bad,
-                                                     int32_t* __restrict__ task, int64_t slots) {
+                                                     uint32_t* __restrict__ listed, Fill f) {
+  if (blockIdx.x >= tiles) return fill_zeros(f, blockIdx.x - tiles, gridDim.x - tiles);
   __shared__ uint32_t h[kMaxBuckets];
   __shared__ uint32_t any;
+  const int buckets = 1 << B.log2;
   for (int b = threadIdx.x; b < buckets; b += 256) h[b] = 0;
   if (threadIdx.x == 0) any = 0;
+  if (blockIdx.x == 0 && threadIdx.x < 3) listed[threadIdx.x] = 0;
   __syncthreads();
   const int64_t t0 = blockIdx.x * tile, t1 = min(tokens, t0 + tile);
   for (int64_t t = t0 + threadIdx.x; t < t1; t += 256) {
     const int32_t r = row_of(ids, t);
-    if (r >= 0) atomicAdd(&h[r >> shift], 1u);
+    if (r >= 0) atomicAdd(&h[r & (buckets - 1)], 1u);
     if (r == -2) any = 1;
   }
   __syncthreads();
   for (int b = threadIdx.x; b < buckets; b += 256) hist[(int64_t)blockIdx.x * buckets + b] = h[b];
   if (threadIdx.x == 0) bad[blockIdx.x] = any;
-  for (int64_t q = (int64_t)blockIdx.x * 256 + threadIdx.x; q < slots; q += (int64_t)gridDim.x * 256) task[q] = -1;
 }
 
-// Stable scatter of (id, token) into buckets.  Each workgroup adds up the counts before its tile itself (at most
-// 64 x 512 of them), each wave owns a contiguous part of the tile and ranks equal buckets by ballots.
-__global__ void __launch_bounds__(256) k_embed_scatter(Ids ids, int64_t tokens, int64_t tile, int shift, int buckets,
-                                                       int bits, const uint32_t* __restrict__ hist,
+// Stable scatter of (local id, token) into buckets.  Each workgroup adds up the counts before its tile itself (at most
+// 64 x 512 of them), each wave owns a contiguous part of the tile.
+__global__ void __launch_bounds__(512) k_embed_scatter(Ids ids, int64_t tokens, int64_t tile, int tiles, Buckets B,
+                                                       const uint32_t* __restrict__ hist,
                                                        const uint32_t* __restrict__ bad, uint32_t* __restrict__ bucket0,
                                                        uint2* __restrict__ pairs, uint32_t* status) {
-  __shared__ uint32_t cnt[4][kMaxBuckets];
-  __shared__ uint32_t scan[256];
-  const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, tiles = gridDim.x;
-  uint32_t total[2], before[2];
-#pragma unroll
-  for (int h = 0; h < 2; ++h) {
-    const int b = 2 * tid + h;
-    total[h] = before[h] = 0;
-    if (b < buckets) {
-      for (int w = 0; w < tiles; ++w) {
-        const uint32_t c = hist[(int64_t)w * buckets + b];
-        if (w < (int)blockIdx.x) before[h] += c;
-        total[h] += c;
-      }
+  __shared__ uint32_t cnt[8][kMaxBuckets];
+  __shared__ uint32_t scratch[8];
+  const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, buckets = 1 << B.log2;
+  for (int b = tid; b < 8 * kMaxBuckets; b += 512) (&cnt[0][0])[b] = 0;
+  uint32_t total = 0, before = 0, all;
+  if (tid < buckets) {
+#pragma unroll 8
+    for (int w = 0; w < tiles; ++w) {
+      const uint32_t c = hist[w * buckets + tid];
+      before += w < (int)blockIdx.x ? c : 0u;
+      total += c;
     }
   }
-  scan[tid] = total[0] + total[1];
-  for (int b = tid; b < 4 * kMaxBuckets; b += 256) (&cnt[0][0])[b] = 0;
   __syncthreads();
-  for (int d = 1; d < 256; d <<= 1) {
-    const uint32_t v = tid >= d ? scan[tid - d] : 0;
-    __syncthreads();
-    scan[tid] += v;
-    __syncthreads();
-  }
-  const int64_t t0 = blockIdx.x * tile, per = (tile + 3) / 4;
-  const int64_t w0 = min(min(tokens, t0 + tile), t0 + wave * per), w1 = min(min(tokens, t0 + tile), w0 + per);
+  const int64_t t0 = blockIdx.x * tile, t1 = min(tokens, t0 + tile), per = (tile + 511) / 512 * 64;
+  const int64_t w0 = min(t1, t0 + wave * per), w1 = min(t1, w0 + per);
   for (int64_t t = w0 + lane; t < w1; t += 64) {
     const int32_t r = row_of(ids, t);
-    if (r >= 0) atomicAdd(&cnt[wave][r >> shift], 1u);
+    if (r >= 0) atomicAdd(&cnt[wave][r & (buckets - 1)], 1u);
   }
-  __syncthreads();
-  const uint32_t first = scan[tid] - total[0] - total[1];
+  const uint32_t first = scan_block<8>(total, scratch, all);
+  if (tid < buckets) {
+    if (blockIdx.x == 0) bucket0[tid] = first;
+    uint32_t at = first + before;
 #pragma unroll
-  for (int h = 0; h < 2; ++h) {
-    const int b = 2 * tid + h;
-    const uint32_t s = first + (h ? total[0] : 0);
-    if (b < buckets) {
-      if (blockIdx.x == 0) bucket0[b] = s;
-      uint32_t at = s + before[h];
-      for (int w = 0; w < 4; ++w) {
-        const uint32_t c = cnt[w][b];
-        cnt[w][b] = at;
-        at += c;
-      }
+    for (int w = 0; w < 8; ++w) {
+      const uint32_t c = cnt[w][tid];
+      cnt[w][tid] = at;
+      at += c;
     }
   }
-  if (blockIdx.x == 0 && tid == 255) bucket0[buckets] = scan[255];
-  if (blockIdx.x == 0 && tid == 0) {
-    uint32_t any = 0;
-    for (int w = 0; w < tiles; ++w) any |= bad[w];
-    *status = any ? kStatusIndex : 0u;
+  if (blockIdx.x == 0) {
+    if (tid == 0) bucket0[buckets] = all;
+    const bool any = __syncthreads_or(tid < tiles && bad[tid] != 0);
+    if (tid == 0) *status = any ? kStatusIndex : 0u;
   }
   __syncthreads();
   for (int64_t t = w0; t < w1; t += 64) {
     const int32_t r = t + lane < w1 ? row_of(ids, t + lane) : -1;
-    const uint32_t b = r >= 0 ? (uint32_t)r >> shift : 0u;
-    const uint64_t m = peers(b, bits, r >= 0);
-    if (r >= 0) {
-      const int lead = __ffsll((unsigned long long)m) - 1;
-      uint32_t at = 0;
-      if (lane == lead) at = atomicAdd(&cnt[wave][b], (uint32_t)__popcll(m));
-      at = (uint32_t)__shfl((int)at, lead) + __popcll(m & ((1ull << lane) - 1));
-      pairs[at] = make_uint2((uint32_t)r, (uint32_t)(t + lane));
-    }
+    const uint32_t at = take_places(cnt[wave], r >= 0 ? r & (buckets - 1) : 0, B.log2, r >= 0);
+    if (r >= 0) pairs[at] = make_uint2((uint32_t)r >> B.log2, (uint32_t)(t + lane));
   }
 }
 
-// One workgroup per bucket: stable counting sort by the id's low bits.  Writes the sorted tokens and their ids, the
-// first sorted position of every id of the bucket's range, and the slots of ids with more than kRun tokens.
-// Dynamic LDS: 8 waves x (1 << shift) counters.
-__global__ void __launch_bounds__(512) k_embed_bucket(int64_t vocab, int shift, int buckets,
-                                                      const uint32_t* __restrict__ bucket0,
-                                                      const uint2* __restrict__ pairs, uint32_t* __restrict__ perm,
-                                                      uint32_t* __restrict__ sid, uint32_t* __restrict__ start,
-                                                      int32_t* __restrict__ task) {
+// One workgroup per bucket: stable counting sort by local id.  Writes the sorted tokens and appends to the lists.
+// Dynamic LDS: 8 waves x width counters.
+__global__ void __launch_bounds__(512) k_embed_bucket(Buckets B, const uint32_t* __restrict__ bucket0,
+                                                      const uint2* __restrict__ pairs, uint32_t* __restrict__ perm, Lists l) {
   extern __shared__ uint32_t cnt[];
-  __shared__ uint32_t scan[512];
-  const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
-  const int width = 1 << shift;
-  const uint32_t s = bucket0[blockIdx.x], e = bucket0[blockIdx.x + 1], n = e - s;
+  __shared__ uint32_t scratch[8], n_ids, n_runs, n_many;
+  const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, width = B.width;
+  const uint32_t s = bucket0[blockIdx.x], n = bucket0[blockIdx.x + 1] - s;
+  if (n == 0) return;
   for (int q = tid; q < 8 * width; q += 512) cnt[q] = 0;
+  if (tid == 0) n_ids = n_runs = n_many = 0;
   __syncthreads();
-  const uint32_t per = (n + 7) / 8;
+  const uint32_t per = (n + 511) / 512 * 64;
   const uint32_t w0 = min(n, wave * per), w1 = min(n, w0 + per);
-  for (uint32_t q = w0 + lane; q < w1; q += 64) atomicAdd(&cnt[wave * width + (pairs[s + q].x & (width - 1))], 1u);
+  for (uint32_t q = w0 + lane; q < w1; q += 64) atomicAdd(&cnt[wave * width + pairs[s + q].x], 1u);
   __syncthreads();
-  // ids of this thread: `each` in a row (width <= 2048: at most four)
-  const int each = (width + 511) / 512, id0 = tid * each;
-  uint32_t own[4], sum = 0;
+  constexpr int kChunks = kMaxWidth / 512;
+  uint32_t base = s, first[kChunks], many[kChunks], id_at[kChunks], run_at[kChunks];
 #pragma unroll
-  for (int q = 0; q < 4; ++q) {
-    own[q] = 0;
-    if (q < each && id0 + q < width) {
-      for (int w = 0; w < 8; ++w) own[q] += cnt[w * width + id0 + q];
-      sum += own[q];
+  for (int k = 0; k < kChunks; ++k) {
+    many[k] = 0;
+    if (k * 512 >= width) continue;
+    const int q = k * 512 + tid;
+    uint32_t c[8], all;
+#pragma unroll
+    for (int w = 0; w < 8; ++w) {
+      c[w] = q < width ? cnt[w * width + q] : 0;
+      many[k] += c[w];
     }
-  }
-  scan[tid] = sum;
-  __syncthreads();
-  for (int d = 1; d < 512; d <<= 1) {
-    const uint32_t v = tid >= d ? scan[tid - d] : 0;
-    __syncthreads();
-    scan[tid] += v;
-    __syncthreads();
-  }
-  uint32_t at = s + scan[tid] - sum;
+    uint32_t at = first[k] = base + scan_block<8>(many[k], scratch, all);
+    if (many[k] > 0) id_at[k] = atomicAdd(many[k] > kRun ? &n_many : &n_ids, 1u);
+    if (many[k] > kRun) run_at[k] = atomicAdd(&n_runs, (many[k] + kRun - 1) / kRun);
+    if (q < width) {
 #pragma unroll
-  for (int q = 0; q < 4; ++q) {
-    if (q < each && id0 + q < width) {
-      const int64_t v = ((int64_t)blockIdx.x << shift) + id0 + q;
-      if (v < vocab) start[v] = at;
-      if (own[q] > kRun)
-        for (uint32_t c = 0; c * kRun < own[q]; ++c) task[at / kSlotSpan + c] = (int32_t)v;
       for (int w = 0; w < 8; ++w) {
-        const uint32_t c = cnt[w * width + id0 + q];
-        cnt[w * width + id0 + q] = at;
-        at += c;
+        cnt[w * width + q] = at;
+        at += c[w];
       }
     }
+    base += all;
   }
-  if (blockIdx.x == buckets - 1 && tid == 0) start[vocab] = e;
   __syncthreads();
+  if (tid == 0) {
+    n_ids = atomicAdd(&l.n[0], n_ids);
+    if (n_many > 0) {
+      n_runs = atomicAdd(&l.n[1], n_runs);
+      n_many = atomicAdd(&l.n[2], n_many);
+    }
+  }
   for (uint32_t q = w0; q < w1; q += 64) {
     const bool on = q + lane < w1;
     const uint2 p = on ? pairs[s + q + lane] : make_uint2(0, 0);
-    const uint32_t b = p.x & (width - 1);
-    const uint64_t m = peers(b, shift, on);
-    if (on) {
-      const int lead = __ffsll((unsigned long long)m) - 1;
-      uint32_t to = 0;
-      if (lane == lead) to = atomicAdd(&cnt[wave * width + b], (uint32_t)__popcll(m));
-      to = (uint32_t)__shfl((int)to, lead) + __popcll(m & ((1ull << lane) - 1));
-      perm[to] = p.y;
-      sid[to] = p.x;
-    }
+    const uint32_t to = take_places(cnt + wave * width, p.x, B.bits, on);
+    if (on) perm[to] = p.y;
   }
-}
-
-// ---- gradient: the sums --------------------------------------------------------------------------------------------
-
-constexpr int kRowVecs = 4;   // vectors a lane holds of its wave's columns
-
-struct RowArgs {
-  const uint32_t* perm;
-  const uint32_t* sid;
-  const uint32_t* start;
-  const int32_t* task;
-  const void* x;
-  float* part;
-  void* grad;
-  int64_t rows, dim, ld_x;   // rows: vocab, sorted positions or slots, whichever the launch walks
-  int64_t blocks;            // column blocks of a row
-  int64_t vocab;
-  float scale;
-};
-
-// Sum of dX over the sorted positions [s, e), at most 64 of them, for this lane's columns: in order, four rows' loads
-// in flight.
-template <int DT, int V>
-__device__ __forceinline__ void sum_rows(const RowArgs& a, uint32_t s, uint32_t e, int64_t col, float acc[kRowVecs][V]) {
-  const int lane = threadIdx.x & 63;
-  const uint32_t m = e - s;
-  const uint32_t mine = (uint32_t)lane < m ? a.perm[s + lane] : 0u;
-  uint32_t q = 0;
-  for (; q + 4 <= m; q += 4) {
-    float v[4][kRowVecs][V];
+  __syncthreads();
 #pragma unroll
-    for (int h = 0; h < 4; ++h) {
-      const int64_t row = (int64_t)(uint32_t)__builtin_amdgcn_readlane(mine, q + h) * a.ld_x;
-#pragma unroll
-      for (int u = 0; u < kRowVecs; ++u)
-        if (col + u * 64 * V < a.dim) load_elems<DT, V>(a.x, row + col + u * 64 * V, v[h][u]);
-    }
-#pragma unroll
-    for (int h = 0; h < 4; ++h)
-#pragma unroll
-      for (int u = 0; u < kRowVecs; ++u)
-#pragma unroll
-        for (int j = 0; j < V; ++j) acc[u][j] += v[h][u][j];
-  }
-  for (; q < m; ++q) {
-    const int64_t row = (int64_t)(uint32_t)__builtin_amdgcn_readlane(mine, q) * a.ld_x;
-#pragma unroll
-    for (int u = 0; u < kRowVecs; ++u) {
-      if (col + u * 64 * V >= a.dim) continue;
-      float v[V];
-      load_elems<DT, V>(a.x, row + col + u * 64 * V, v);
-#pragma unroll
-      for (int j = 0; j < V; ++j) acc[u][j] += v[j];
-    }
-  }
-}
-
-// Partial sums of ids with more than kRun tokens, a wave per slot and column block.
-template <int DT, int V>
-__global__ void __launch_bounds__(256) k_embed_parts(RowArgs a) {
-  const int64_t items = a.rows * a.blocks;
-  for (int64_t item = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6); item < items; item += (int64_t)gridDim.x * 4) {
-    const int64_t slot = item / a.blocks;
-    const int32_t v = a.task[slot];
-    if (v < 0) continue;
-    const uint32_t s = a.start[v], e = a.start[v + 1];
-    const uint32_t p = s + (uint32_t)(slot - s / kSlotSpan) * kRun;
-    const int64_t col = (item - slot * a.blocks) * (64 * kRowVecs * V) + (threadIdx.x & 63) * V;
-    float acc[kRowVecs][V] = {};
-    sum_rows<DT, V>(a, p, min(e, p + kRun), col, acc);
-#pragma unroll
-    for (int u = 0; u < kRowVecs; ++u)
-      if (col + u * 64 * V < a.dim) store_elems<ISO_F32, V>(a.part, slot * a.dim + col + u * 64 * V, acc[u]);
-  }
-}
-
-// One row of the gradient a wave and column block.  ADD = false walks the whole vocabulary (a row without tokens is
-// zeros), ADD = true the sorted positions, of which the first of each id does the id's row.
-template <int DT, int DTG, int V, bool ADD>
-__global__ void __launch_bounds__(256) k_embed_rows(RowArgs a) {
-  const int64_t units = ADD ? a.start[a.vocab] : a.rows;   // padding is not sorted
-  const int64_t items = units * a.blocks;
-  for (int64_t item = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6); item < items; item += (int64_t)gridDim.x * 4) {
-    const int64_t unit = item / a.blocks;
-    const int64_t col = (item - unit * a.blocks) * (64 * kRowVecs * V) + (threadIdx.x & 63) * V;
-    const int64_t v = ADD ? a.sid[unit] : unit;
-    const uint32_t s = a.start[v], e = a.start[v + 1];
-    if (ADD && s != (uint32_t)unit) continue;
-    float acc[kRowVecs][V] = {};
-    if (e - s <= kRun) {
-      sum_rows<DT, V>(a, s, e, col, acc);
+  for (int k = 0; k < kChunks; ++k) {
+    if (many[k] == 0) continue;
+    const uint32_t v = ((uint32_t)(k * 512 + tid) << B.log2) + blockIdx.x;
+    if (many[k] > kRun) {
+      const uint32_t run0 = n_runs + run_at[k], runs = (many[k] + kRun - 1) / kRun;
+      for (uint32_t p = 0; p < runs; ++p)
+        l.runs[run0 + p] = make_uint2(first[k] + p * kRun, min((uint32_t)kRun, many[k] - p * kRun));
+      l.many[n_many + id_at[k]] = make_uint4(v, run0, runs, 0);
     } else {
-      const int64_t slot0 = s / kSlotSpan, parts = (e - s + kRun - 1) / kRun;
-      for (int64_t c = 0; c < parts; ++c)
+      l.ids[n_ids + id_at[k]] = make_uint4(v, first[k], many[k], 0);
+    }
+  }
+}
+
+// Partial sums of ids with more than kRun tokens, a wave per run and column block.
+template <int DT>
+__global__ void __launch_bounds__(256) k_embed_parts(const uint32_t* __restrict__ perm, Lists l, Rows a, int64_t blocks,
+                                                     float* __restrict__ part) {
+  constexpr int V = kVec<DT>;
+  const int lane = threadIdx.x & 63;
+  const int64_t items = (int64_t)l.n[1] * blocks;
+  for (int64_t item = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6); item < items; item += (int64_t)gridDim.x * 4) {
+    const int64_t run = item / blocks;
+    const uint2 r = l.runs[run];
+    const int64_t col = (item - run * blocks) * (64 * V) + lane * V;
+    float acc[V] = {};
+    add_rows<DT>(a, (uint32_t)lane < r.y ? perm[r.x + lane] : 0u, r.y, col, acc);
+    if (col < a.dim) store_elems<ISO_F32, V>(part, run * a.dim + col, acc, a.dim - col);
+  }
+}
+
+// The gradient's rows that have tokens.  Frequent ids first, a workgroup a column block: its waves add up a quarter of the
+// id's runs each, in order, and then the quarters.  The others take a wave a column block; a wave has the list's entry after
+// next and the next one's tokens under way while it adds the current rows, so that it waits for one memory access a row
+// block instead of three.
+template <int DT, int DTG, bool ADD>
+__global__ void __launch_bounds__(256) k_embed_rows(const uint32_t* __restrict__ perm, Lists l, Rows a, int64_t blocks,
+                                                    const float* __restrict__ part) {
+  constexpr int V = kVec<DT>, kSums = 2;
+  __shared__ float quarter[4][V][64];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int64_t many = (int64_t)l.n[2] * blocks, items = (int64_t)l.n[0] * blocks;
+  for (int64_t b = blockIdx.x; b < many; b += gridDim.x) {
+    const int64_t unit = b / blocks;
+    const uint4 id = l.many[unit];
+    const int64_t col = (b - unit * blocks) * (64 * V) + lane * V;
+    const uint32_t each = (id.z + 3) / 4, r0 = min(id.z, wave * each), r1 = min(id.z, r0 + each);
+    float acc[V] = {};
+    for (uint32_t r = r0; r < r1; r += kSums) {
+      float p[kSums][V];
 #pragma unroll
-        for (int u = 0; u < kRowVecs; ++u) {
-          if (col + u * 64 * V >= a.dim) continue;
-          float p[V];
-          load_elems<ISO_F32, V>(a.part, (slot0 + c) * a.dim + col + u * 64 * V, p);
+      for (int h = 0; h < kSums; ++h)
+        if (r + h < r1) load_elems<ISO_F32, V>(part, (int64_t)(id.y + r + h) * a.dim + col, p[h], a.dim - col);
 #pragma unroll
-          for (int j = 0; j < V; ++j) acc[u][j] += p[j];
+      for (int h = 0; h < kSums; ++h)
+        if (r + h < r1) {
+#pragma unroll
+          for (int j = 0; j < V; ++j) acc[j] += p[h][j];
         }
     }
 #pragma unroll
-    for (int u = 0; u < kRowVecs; ++u) {
-      if (col + u * 64 * V >= a.dim) continue;
-      const int64_t at = v * a.dim + col + u * 64 * V;
-      float g[V];
-      if constexpr (ADD) load_elems<DTG, V>(a.grad, at, g);
+    for (int j = 0; j < V; ++j) quarter[wave][j][lane] = acc[j];
+    __syncthreads();
+    if (wave == 0) {
 #pragma unroll
-      for (int j = 0; j < V; ++j) g[j] = ADD ? g[j] + a.scale * acc[u][j] : a.scale * acc[u][j];
-      store_elems<DTG, V, !ADD>(a.grad, at, g);
+      for (int j = 0; j < V; ++j) acc[j] = ((quarter[0][j][lane] + quarter[1][j][lane]) + quarter[2][j][lane]) + quarter[3][j][lane];
+      finish_row<DT, DTG, ADD>(a, id.x, col, acc);
     }
+    __syncthreads();
+  }
+  const int64_t stride = (int64_t)gridDim.x * 4;
+  int64_t item = (int64_t)blockIdx.x * 4 + wave;
+  auto entry = [&](int64_t at) { return at < items ? l.ids[at / blocks] : make_uint4(0, 0, 0, 0); };
+  auto tokens = [&](const uint4& id) { return (uint32_t)lane < id.z ? perm[id.y + lane] : 0u; };
+  uint4 now = entry(item), next = entry(item + stride);
+  uint32_t mine = tokens(now);
+  for (; item < items; item += stride) {
+    const uint4 after = entry(item + 2 * stride);
+    const uint32_t theirs = tokens(next);
+    const int64_t col = (item - item / blocks * blocks) * (64 * V) + lane * V;
+    float acc[V] = {};
+    add_rows<DT>(a, mine, now.z, col, acc);
+    finish_row<DT, DTG, ADD>(a, now.x, col, acc);
+    now = next, next = after, mine = theirs;
   }
 }
 
-template <int DT, int DTG, int V>
-hipError_t launch_rows(RowArgs a, int64_t vocab, int64_t tokens, int64_t slots, bool accumulate, hipStream_t s) {
-  a.blocks = (a.dim + 64 * kRowVecs * V - 1) / (64 * kRowVecs * V);
-  a.vocab = vocab;
-  if (slots > 0) {
-    a.rows = slots;
-    k_embed_parts<DT, V><<<grid_for((slots * a.blocks + 3) / 4), 256, 0, s>>>(a);
-  }
-  a.rows = accumulate ? tokens : vocab;
-  const unsigned grid = grid_for((a.rows * a.blocks + 3) / 4);
-  if (accumulate) k_embed_rows<DT, DTG, V, true><<<grid, 256, 0, s>>>(a);
-  else k_embed_rows<DT, DTG, V, false><<<grid, 256, 0, s>>>(a);
-  return hipGetLastError();
+// ---- host ----------------------------------------------------------------------------------------------------------
+
+int log2_up(int64_t n) {
+  int b = 0;
+  while ((1ll << b) < n) ++b;
+  return b;
+}
+
+Buckets buckets_of(int64_t vocab, int log2) {
+  Buckets B;
+  B.log2 = log2;
+  B.width = (int32_t)((vocab + (1ll << log2) - 1) >> log2);
+  B.bits = log2_up(B.width);
+  return B;
 }
 
 Ids ids_of(const iso_embed& e) {
   return Ids{e.ids, e.id_type == ISO_I64, e.pad_id != ISO_NO_PAD, e.pad_id, e.vocab};
 }
 
-template <int DT, bool VEC>
-void launch_lookup(const iso_embed& e, uint8_t* ws, hipStream_t s) {
-  constexpr int V = VEC ? Fmt<DT>::kPerVec : 1;
-  const int64_t items = e.tokens * (e.dim / V);
-  const unsigned grid = 1 + grid_for((items + kLookupBlock - 1) / kLookupBlock);
-  k_embed_lookup<DT, VEC><<<grid, 256, 0, s>>>(ids_of(e), e.table, e.x, e.tokens, e.dim, e.ld_x, (float)e.scale,
-                                               (uint32_t*)ws);
+Fill zeros_of(const iso_embed& e, int dt_grad) {
+  const int64_t words = e.vocab * e.dim * (dt_grad == ISO_BF16 ? 1 : 2);
+  return Fill{e.grad, words / 8, (int32_t)(words % 8)};
+}
+unsigned grid_of(const Fill& f) { return grid_for((f.vectors + 255) / 256); }
+
+// Gradients from 64 MiB on are cleared by a launch of their own at the rate of fill_zeros, smaller ones by the workgroups
+// that hold the ids, whose writes are slower (5.0 against 6.9 TB/s) but need no second launch (4 us).
+constexpr int64_t kOwnFill = 64ll << 20;
+
+template <int DT, int DTG, bool ADD>
+hipError_t grad_few(const iso_embed& e, const Rows& a, uint8_t* ws, hipStream_t s) {
+  // 512 buckets, or as many as the vocabulary takes to leave at most 512 ids in each
+  const Buckets B = buckets_of(e.vocab, std::max(std::min(9, log2_up(e.vocab)), log2_up((e.vocab + kFewWidth - 1) / kFewWidth)));
+  const int64_t blocks = (e.dim + 64 * kVec<DT> - 1) / (64 * kVec<DT>);
+  const bool fill = !ADD && e.vocab * e.dim * (DTG == ISO_BF16 ? 2 : 4) >= kOwnFill;
+  if (fill) {
+    const Fill f = zeros_of(e, DTG);
+    k_embed_fill<<<grid_of(f), 256, 0, s>>>(f);
+  }
+  k_embed_few<DT, DTG, ADD><<<(unsigned)(blocks << B.log2), 64 * kFewWaves, 0, s>>>(ids_of(e), (int)e.tokens, B, blocks, a,
+                                                                                    !ADD && !fill, (uint32_t*)ws);
+  return hipGetLastError();
+}
+
+template <int DT, int DTG, bool ADD>
+hipError_t grad_many(const iso_embed& e, const Rows& a, uint8_t* ws, hipStream_t s) {
+  const EmbedPlan P = embed_plan(e.tokens, e.vocab, e.dim);
+  const Ids ids = ids_of(e);
+  const Buckets B = buckets_of(e.vocab, std::min(9, log2_up(e.vocab)));
+  const unsigned tiles = (unsigned)P.tiles, buckets = 1u << B.log2;
+  const Lists l{(uint32_t*)(ws + P.listed), (uint4*)(ws + P.ids), (uint2*)(ws + P.runs), (uint4*)(ws + P.many)};
+  uint32_t* const perm = (uint32_t*)(ws + P.perm);
+  uint2* const pairs = (uint2*)(ws + P.pairs);
+  float* const part = (float*)(ws + P.part);
+  const Fill f = zeros_of(e, DTG);
+  k_embed_count<<<tiles + (ADD ? 0 : grid_of(f)), 256, 0, s>>>(ids, e.tokens, P.tile, tiles, B, (uint32_t*)(ws + P.hist),
+                                                               (uint32_t*)(ws + P.bad), l.n, f);
+  k_embed_scatter<<<tiles, 512, 0, s>>>(ids, e.tokens, P.tile, tiles, B, (const uint32_t*)(ws + P.hist),
+                                        (const uint32_t*)(ws + P.bad), (uint32_t*)(ws + P.bucket0), pairs, (uint32_t*)ws);
+  k_embed_bucket<<<buckets, 512, sizeof(uint32_t) * 8 * (size_t)B.width, s>>>(B, (const uint32_t*)(ws + P.bucket0), pairs,
+                                                                            perm, l);
+  const hipError_t err = hipGetLastError();
+  if (err != hipSuccess) return err;
+  const int64_t blocks = (e.dim + 64 * kVec<DT> - 1) / (64 * kVec<DT>);
+  k_embed_parts<DT><<<(unsigned)std::min<int64_t>((P.most_runs * blocks + 3) / 4, 2048), 256, 0, s>>>(perm, l, a, blocks, part);
+  const int64_t most = (std::min(e.tokens, e.vocab) * blocks + 3) / 4;
+  k_embed_rows<DT, DTG, ADD><<<(unsigned)std::min<int64_t>(most, 2048), 256, 0, s>>>(perm, l, a, blocks, part);
+  return hipGetLastError();
+}
+
+template <int DT, int DTG, bool ADD>
+hipError_t grad(const iso_embed& e, uint8_t* ws, hipStream_t s) {
+  const Rows a{e.x, e.grad, e.dim, e.ld_x, (float)e.scale};
+  return e.tokens <= kFewTokens ? grad_few<DT, DTG, ADD>(e, a, ws, s) : grad_many<DT, DTG, ADD>(e, a, ws, s);
 }
 
 }  // namespace
 
 EmbedPlan embed_plan(int64_t tokens, int64_t vocab, int64_t dim) {
   EmbedPlan P;
-  while (((vocab - 1) >> P.shift) >= kMaxBuckets) ++P.shift;
-  P.buckets = (int)((vocab - 1) >> P.shift) + 1;
+  P.total = kStatusBytes;
+  if (tokens <= kFewTokens) return P;
+  const size_t buckets = (size_t)1 << std::min(9, log2_up(vocab));
   P.tile = std::max<int64_t>(kMinTile, (tokens + kMaxTiles - 1) / kMaxTiles);
-  P.tiles = std::max<int64_t>(1, (tokens + P.tile - 1) / P.tile);
-  P.slots = tokens > kRun ? tokens / kSlotSpan + 1 : 0;
-  size_t at = kStatusBytes;
+  P.tiles = (tokens + P.tile - 1) / P.tile;
+  P.most_runs = tokens / (kRun / 2) + 1;   // an id with m > kRun tokens has ceil(m / kRun) <= m / (kRun / 2)
   auto region = [&](size_t bytes) {
-    const size_t o = at;
-    at = align_up(at + bytes, 256);
+    const size_t o = P.total;
+    P.total = align_up(P.total + bytes, 256);
     return o;
   };
   P.bad = region(sizeof(uint32_t) * P.tiles);
-  P.hist = region(sizeof(uint32_t) * P.tiles * P.buckets);
-  P.bucket0 = region(sizeof(uint32_t) * (P.buckets + 1));
+  P.hist = region(sizeof(uint32_t) * P.tiles * buckets);
+  P.bucket0 = region(sizeof(uint32_t) * (buckets + 1));
   P.pairs = region(sizeof(uint2) * tokens);
   P.perm = region(sizeof(uint32_t) * tokens);
-  P.sid = region(sizeof(uint32_t) * tokens);
-  P.start = region(sizeof(uint32_t) * (vocab + 1));
-  P.task = region(sizeof(int32_t) * P.slots);
-  P.part = region(sizeof(float) * P.slots * dim);
-  P.total = at;
+  P.listed = region(sizeof(uint32_t) * 3);
+  P.ids = region(sizeof(uint4) * std::min(tokens, vocab));
+  P.runs = region(sizeof(uint2) * P.most_runs);
+  P.many = region(sizeof(uint4) * (tokens / kRun + 1));
+  P.part = region(sizeof(float) * P.most_runs * dim);
   return P;
 }
 
 hipError_t run_embed_lookup(const iso_embed& e, int dt, uint8_t* ws, hipStream_t s) {
-  const bool vec = vector_rows(e.dim, e.ld_x, dt == ISO_BF16 ? 8 : 4);
-  if (dt == ISO_BF16) vec ? launch_lookup<ISO_BF16, true>(e, ws, s) : launch_lookup<ISO_BF16, false>(e, ws, s);
-  else vec ? launch_lookup<ISO_F32, true>(e, ws, s) : launch_lookup<ISO_F32, false>(e, ws, s);
+  const int v = dt == ISO_BF16 ? kVec<ISO_BF16> : kVec<ISO_F32>;
+  const int64_t items = e.tokens * ((e.dim + v - 1) / v);
+  const unsigned grid = 1 + grid_for((items + kLookupBlock - 1) / kLookupBlock);
+  auto go = [&](auto k) {
+    k<<<grid, 256, 0, s>>>(ids_of(e), e.table, e.x, e.tokens, e.dim, e.ld_x, (float)e.scale, (uint32_t*)ws);
+  };
+  dt == ISO_BF16 ? go(k_embed_lookup<ISO_BF16>) : go(k_embed_lookup<ISO_F32>);
   return hipGetLastError();
 }
 
 hipError_t run_embed_grad(const iso_embed& e, int dt, int dt_grad, bool accumulate, uint8_t* ws, hipStream_t s) {
-  const EmbedPlan P = embed_plan(e.tokens, e.vocab, e.dim);
-  const Ids ids = ids_of(e);
-  uint32_t* const start = (uint32_t*)(ws + P.start);
-  k_embed_count<<<(unsigned)P.tiles, 256, 0, s>>>(ids, e.tokens, P.tile, P.shift, P.buckets, (uint32_t*)(ws + P.hist),
-                                                  (uint32_t*)(ws + P.bad), (int32_t*)(ws + P.task), P.slots);
-  int bits = 0;
-  while ((1 << bits) < P.buckets) ++bits;
-  k_embed_scatter<<<(unsigned)P.tiles, 256, 0, s>>>(ids, e.tokens, P.tile, P.shift, P.buckets, bits,
-                                                    (const uint32_t*)(ws + P.hist), (const uint32_t*)(ws + P.bad),
-                                                    (uint32_t*)(ws + P.bucket0), (uint2*)(ws + P.pairs), (uint32_t*)ws);
-  k_embed_bucket<<<(unsigned)P.buckets, 512, sizeof(uint32_t) * 8 * ((size_t)1 << P.shift), s>>>(
-      e.vocab, P.shift, P.buckets, (const uint32_t*)(ws + P.bucket0), (const uint2*)(ws + P.pairs),
-      (uint32_t*)(ws + P.perm), (uint32_t*)(ws + P.sid), start, (int32_t*)(ws + P.task));
-  hipError_t err = hipGetLastError();
-  if (err != hipSuccess) return err;
-  RowArgs a{(const uint32_t*)(ws + P.perm), (const uint32_t*)(ws + P.sid), start, (const int32_t*)(ws + P.task),
-            e.x, (float*)(ws + P.part), e.grad, 0, e.dim, e.ld_x, 0, 0, (float)e.scale};
-  auto go = [&](auto f) { return f(a, e.vocab, e.tokens, P.slots, accumulate, s); };
-  const bool vec = vector_rows(e.dim, e.ld_x, dt == ISO_BF16 ? 8 : 4);
+  auto go = [&](auto f) { return f(e, ws, s); };
   if (dt == ISO_BF16 && dt_grad == ISO_BF16)
-    return go(vec ? launch_rows<ISO_BF16, ISO_BF16, 8> : launch_rows<ISO_BF16, ISO_BF16, 1>);
-  if (dt == ISO_BF16) return go(vec ? launch_rows<ISO_BF16, ISO_F32, 8> : launch_rows<ISO_BF16, ISO_F32, 1>);
-  if (dt_grad == ISO_BF16) return go(vec ? launch_rows<ISO_F32, ISO_BF16, 4> : launch_rows<ISO_F32, ISO_BF16, 1>);
-  return go(vec ? launch_rows<ISO_F32, ISO_F32, 4> : launch_rows<ISO_F32, ISO_F32, 1>);
+    return go(accumulate ? grad<ISO_BF16, ISO_BF16, true> : grad<ISO_BF16, ISO_BF16, false>);
+  if (dt == ISO_BF16) return go(accumulate ? grad<ISO_BF16, ISO_F32, true> : grad<ISO_BF16, ISO_F32, false>);
+  if (dt_grad == ISO_BF16) return go(accumulate ? grad<ISO_F32, ISO_BF16, true> : grad<ISO_F32, ISO_BF16, false>);
+  return go(accumulate ? grad<ISO_F32, ISO_F32, true> : grad<ISO_F32, ISO_F32, false>);
 }
 
 }  // namespace iso

@@ -10,12 +10,11 @@
 
 namespace iso {
 
-// What a call needs without its pointers' contents; offsets are into the workspace.
+// Workspace regions of the embedding's gradient (many tokens; few take the status block alone).
 struct EmbedPlan {
-  int shift = 0, buckets = 0;      // bucket of an id: id >> shift
   int64_t tiles = 0, tile = 0;     // tokens are counted and scattered by tiles of `tile`
-  int64_t slots = 0;               // partial sums of ids with many tokens
-  size_t bad = 0, hist = 0, bucket0 = 0, pairs = 0, perm = 0, sid = 0, start = 0, task = 0, part = 0, total = 0;
+  int64_t most_runs = 0;           // partial sums of ids with many tokens
+  size_t bad = 0, hist = 0, bucket0 = 0, pairs = 0, perm = 0, listed = 0, ids = 0, runs = 0, many = 0, part = 0, total = 0;
 };
 
 EmbedPlan embed_plan(int64_t tokens, int64_t vocab, int64_t dim);

@@ -16,10 +16,10 @@ bool aligned16(const void* p) { return ((uintptr_t)p & 15u) == 0; }
 bool is_dtype(int dt) { return dt == ISO_F32 || dt == ISO_BF16; }
 bool is_flag(int v) { return v == 0 || v == 1; }
 
-// Limits of one matrix, its padding and stride included: a launch of a workgroup per 4096 elements holds fewer than
+// Limits of one matrix, its padding and stride included: a launch of a workgroup per 2048 elements holds fewer than
 // 2^32 threads.
 constexpr int64_t kMaxDim = 1 << 24;
-constexpr int64_t kMaxElems = 1ll << 35;
+constexpr int64_t kMaxElems = 1ll << 34;
 bool too_large(int64_t rows, int64_t ld) { return rows > 0 && ld > kMaxElems / rows; }
 
 iso_status check_ptr(const void* p) {

@@ -166,81 +166,33 @@ __device__ __forceinline__ void load_lds(u32x4_t buffer, uint32_t lds, uint32_t 
 }
 #pragma clang diagnostic pop
 
-// 32 rows of 128 columns (132 floats apart in LDS) to G from row m, column n on, by one wave.  Rows whose length keeps
-// vectors aligned go 16 bytes a lane, others one element a lane with the lanes along the row.
 typedef __attribute__((address_space(3))) f32x4_t* lds_f32x4;
-typedef __attribute__((address_space(3))) float* lds_f32;
 
 constexpr int kRowBytes = 132 * 4;
 
+// 32 rows of 128 columns (132 floats apart in LDS) to G from row m, column n on, by one wave, 16 bytes a lane.
 template <int DTG, bool ADD>
 __device__ __forceinline__ void write_rows(const Layer& a, int m, int n, uint32_t lds, int lane) {
-  constexpr int V = Fmt<DTG>::kPerVec, kLanes = 128 / V, kRows = 64 / kLanes;
-  if (a.cols % V == 0) {
-    const int row = lane / kLanes, c = lane % kLanes * V;
-    if (n + c >= a.cols) return;
+  constexpr int V = kVec<DTG>, kLanes = 128 / V, kRows = 64 / kLanes;
+  const int row = lane / kLanes, c = lane % kLanes * V, left = a.cols - n - c;
+  if (left <= 0) return;
 #pragma unroll 8
-    for (int h = 0; h < 32; h += kRows) {
-      if (m + h + row >= a.rows) continue;
-      const int64_t at = (int64_t)(m + h + row) * a.cols + n + c;
-      float v[V];
+  for (int h = 0; h < 32; h += kRows) {
+    if (m + h + row >= a.rows) continue;
+    const int64_t at = (int64_t)(m + h + row) * a.cols + n + c;
+    float v[V];
 #pragma unroll
-      for (int j = 0; j < V; j += 4) {
-        const f32x4_t x = *(lds_f32x4)(uintptr_t)(lds + (h + row) * kRowBytes + (c + j) * 4);
-        v[j] = x.x, v[j + 1] = x.y, v[j + 2] = x.z, v[j + 3] = x.w;
-      }
-      if constexpr (ADD) {
-        float old[V];
-        load_elems<DTG, V>(a.g, at, old);
-#pragma unroll
-        for (int j = 0; j < V; ++j) v[j] += old[j];
-      }
-      store_elems<DTG, V>(a.g, at, v);
+    for (int j = 0; j < V; j += 4) {
+      const f32x4_t x = *(lds_f32x4)(uintptr_t)(lds + (h + row) * kRowBytes + (c + j) * 4);
+      v[j] = x.x, v[j + 1] = x.y, v[j + 2] = x.z, v[j + 3] = x.w;
     }
-  } else {
-#pragma unroll 2
-    for (int h = 0; h < 32; ++h) {
-      if (m + h >= a.rows) break;
+    if constexpr (ADD) {
+      float old[V];
+      load_elems<DTG, V>(a.g, at, old, left);
 #pragma unroll
-      for (int k = 0; k < 2; ++k) {
-        const int c = k * 64 + lane;
-        if (n + c >= a.cols) continue;
-        const int64_t at = (int64_t)(m + h) * a.cols + n + c;
-        float v = *(lds_f32)(uintptr_t)(lds + h * kRowBytes + c * 4);
-        if constexpr (ADD) {
-          float old;
-          load_elems<DTG, 1>(a.g, at, &old);
-          v += old;
-        }
-        store_elems<DTG, 1>(a.g, at, &v);
-      }
+      for (int j = 0; j < V; ++j) v[j] += old[j];
     }
-  }
-}
-
-template <int DTG>
-__device__ __forceinline__ void put4(void* g, int64_t at, const float* v, int left, bool aligned, bool add) {
-  float o[4] = {v[0], v[1], v[2], v[3]};
-  if (aligned) {
-    if (left <= 0) return;
-    if (add) {
-      float old[4];
-      load_elems<DTG, 4>(g, at, old);
-#pragma unroll
-      for (int h = 0; h < 4; ++h) o[h] += old[h];
-    }
-    store_elems<DTG, 4>(g, at, o);
-  } else {
-#pragma unroll
-    for (int h = 0; h < 4; ++h) {
-      if (h >= left) continue;
-      if (add) {
-        float old;
-        load_elems<DTG, 1>(g, at + h, &old);
-        o[h] += old;
-      }
-      store_elems<DTG, 1>(g, at + h, o + h);
-    }
+    store_elems<DTG, V>(a.g, at, v, left);
   }
 }
 
@@ -443,7 +395,14 @@ __global__ void __launch_bounds__(256) k_wgrad_join(LayerTable T) {
 #pragma unroll
     for (int j = 0; j < 4; ++j) sum[j] += v[j];
   }
-  put4<DTG>(a.g, (int64_t)m * a.cols + n, sum, a.cols - n, (a.cols & 3) == 0, ADD);
+  const int64_t to = (int64_t)m * a.cols + n;
+  if constexpr (ADD) {
+    float old[4];
+    load_elems<DTG, 4>(a.g, to, old, a.cols - n);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) sum[j] += old[j];
+  }
+  store_elems<DTG, 4>(a.g, to, sum, a.cols - n);
 }
 
 // ---- host ----------------------------------------------------------------------------------------------------------

@@ -58,8 +58,10 @@ def test_embed_more_refusals():
     assert L.iso_embed_grad(None, iso.BF16, iso.F32, 0, WS, 1 << 30, None) == _lib.ERR_INVALID_ARG
     assert grad(embed(), dtg=7) == _lib.ERR_INVALID_ARG
     assert grad(embed(), acc=2) == _lib.ERR_INVALID_ARG
-    need = L.iso_workspace_size_embed(ctypes.byref(iso._embed(embed())))
-    assert need > 256 and grad(embed(), ws_bytes=need - 1) == _lib.ERR_WORKSPACE
+    for n in (8, 10000):
+        need = L.iso_workspace_size_embed(ctypes.byref(iso._embed(embed(tokens=n))))
+        assert need >= 256 and grad(embed(tokens=n), ws_bytes=need - 1) == _lib.ERR_WORKSPACE
+    assert need > 10000 * 4
     assert L.iso_workspace_size_embed(None) == 0
     assert L.iso_workspace_size_embed(ctypes.byref(iso._embed(embed(vocab=-3)))) == 0
     with pytest.raises(TypeError):
