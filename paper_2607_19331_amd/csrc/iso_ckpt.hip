@@ -95,7 +95,7 @@ __device__ __forceinline__ void stored8(uint2 q, uint32_t e, float v[8]) {
   for (int j = 0; j < 8; ++j) v[j] = ((float)((w[j / 4] >> (8 * (j & 3))) & 0xFFu) - 128.0f) * s;
 }
 
-template <int DT>
+template <int DT, bool STREAM>
 __global__ void __launch_bounds__(256) k_ckpt_pack(CkptTable T) {
   const int j = table_entry(T);
   const CkptArg& a = T.t[j];
@@ -131,12 +131,13 @@ __global__ void __launch_bounds__(256) k_ckpt_pack(CkptTable T) {
     if (p[i].row >= a.rows) continue;
     const int64_t item = p[i].row * a.per_row + p[i].c8;
     const u32x2_t out = {w[0] | w[1] << 8 | w[2] << 16 | w[3] << 24, w[4] | w[5] << 8 | w[6] << 16 | w[7] << 24};
-    *(gmem((u32x2_t*)a.q) + item) = out;
+    if constexpr (STREAM) __builtin_nontemporal_store(out, gmem((u32x2_t*)a.q) + item);
+    else *(gmem((u32x2_t*)a.q) + item) = out;
     if ((p[i].c8 & 3u) == 0) gmem(a.e)[item >> 2] = (uint8_t)e;
   }
 }
 
-template <int DT>
+template <int DT, bool STREAM>
 __global__ void __launch_bounds__(256) k_ckpt_unpack(CkptTable T) {
   const int j = table_entry(T);
   const CkptArg& a = T.t[j];
@@ -158,7 +159,7 @@ __global__ void __launch_bounds__(256) k_ckpt_unpack(CkptTable T) {
     if (p[i].row >= a.rows || col >= a.cols) continue;
     float v[8];
     stored8(make_uint2(q[i].x, q[i].y), e[i], v);
-    store_elems<DT, 8>(a.x, p[i].row * a.ld_x + col, v, a.cols - col);
+    store_elems<DT, 8, STREAM>(a.x, p[i].row * a.ld_x + col, v, a.cols - col);
   }
 }
 
@@ -170,7 +171,7 @@ __device__ __forceinline__ float sigmoid_of(float g) {
   else return 1.0f / (1.0f + expf(-g));
 }
 
-template <int DT>
+template <int DT, bool STREAM>
 __global__ void __launch_bounds__(256) k_gate_grad(GateTable T) {
   const int j = table_entry(T);
   const GateArg& a = T.t[j];
@@ -206,8 +207,8 @@ __global__ void __launch_bounds__(256) k_gate_grad(GateTable T) {
       u[h] = d * silu;
     }
     const int64_t at = p[i].row * a.ld + col;
-    store_elems<DT, 8>(a.dgate, at, g, a.cols - col);
-    store_elems<DT, 8>(a.dup, at, u, a.cols - col);
+    store_elems<DT, 8, STREAM>(a.dgate, at, g, a.cols - col);
+    store_elems<DT, 8, STREAM>(a.dup, at, u, a.cols - col);
   }
 }
 
@@ -218,15 +219,18 @@ GateArg arg_of(const iso_gate_grad& g) {
   return GateArg{g.gate.q, g.up.q,    g.gate.e, g.up.e, g.dh, g.dgate, g.dup, g.gate.rows, g.ld, (uint32_t)g.gate.cols,
                  (uint32_t)(ckpt_ld(g.gate.cols) / 8)};
 }
-// Queues a table, up to 16 tensors and 2^22 workgroups a launch (a larger tensor goes alone).
+// Queues a table, up to 16 tensors and 2^22 workgroups a launch (a larger tensor goes alone); `size`: bytes written for a
+// group of eight columns.
 template <class Table, class Entry, class Launch>
-hipError_t for_tables(const Entry* c, int n, int items, Launch launch) {
+hipError_t for_tables(const Entry* c, int n, int items, int size, Launch launch) {
   Table T;
+  int64_t bytes = 0;
   T.n = 0;
   T.block0[0] = 0;
   auto flush = [&] {
-    if (T.n > 0) launch(T, T.block0[T.n]);
+    if (T.n > 0) launch(T, T.block0[T.n], streamed(bytes));
     T.n = 0;
+    bytes = 0;
   };
   for (int j = 0; j < n; ++j) {
     const auto a = arg_of(c[j]);
@@ -235,6 +239,7 @@ hipError_t for_tables(const Entry* c, int n, int items, Launch launch) {
     if (T.n == kTable || (T.n > 0 && T.block0[T.n] + blocks > (1 << 22))) flush();
     T.t[T.n] = a;
     T.block0[T.n + 1] = T.block0[T.n] + (uint32_t)blocks;
+    bytes += a.rows * a.per_row * size;
     ++T.n;
   }
   flush();
@@ -244,23 +249,26 @@ hipError_t for_tables(const Entry* c, int n, int items, Launch launch) {
 }  // namespace
 
 hipError_t run_ckpt_pack(const iso_ckpt* c, int n, int dt, hipStream_t s) {
-  return for_tables<CkptTable>(c, n, kItems, [&](const CkptTable& T, unsigned grid) {
-    if (dt == ISO_BF16) k_ckpt_pack<ISO_BF16><<<grid, 256, 0, s>>>(T);
-    else k_ckpt_pack<ISO_F32><<<grid, 256, 0, s>>>(T);
+  return for_tables<CkptTable>(c, n, kItems, 8, [&](const CkptTable& T, unsigned grid, bool stream) {
+    auto go = [&](auto k) { k<<<grid, 256, 0, s>>>(T); };
+    if (dt == ISO_BF16) stream ? go(k_ckpt_pack<ISO_BF16, true>) : go(k_ckpt_pack<ISO_BF16, false>);
+    else stream ? go(k_ckpt_pack<ISO_F32, true>) : go(k_ckpt_pack<ISO_F32, false>);
   });
 }
 
 hipError_t run_ckpt_unpack(const iso_ckpt* c, int n, int dt, hipStream_t s) {
-  return for_tables<CkptTable>(c, n, kItems, [&](const CkptTable& T, unsigned grid) {
-    if (dt == ISO_BF16) k_ckpt_unpack<ISO_BF16><<<grid, 256, 0, s>>>(T);
-    else k_ckpt_unpack<ISO_F32><<<grid, 256, 0, s>>>(T);
+  return for_tables<CkptTable>(c, n, kItems, dt == ISO_BF16 ? 16 : 32, [&](const CkptTable& T, unsigned grid, bool stream) {
+    auto go = [&](auto k) { k<<<grid, 256, 0, s>>>(T); };
+    if (dt == ISO_BF16) stream ? go(k_ckpt_unpack<ISO_BF16, true>) : go(k_ckpt_unpack<ISO_BF16, false>);
+    else stream ? go(k_ckpt_unpack<ISO_F32, true>) : go(k_ckpt_unpack<ISO_F32, false>);
   });
 }
 
 hipError_t run_gate_grad(const iso_gate_grad* g, int n, int dt, hipStream_t s) {
-  return for_tables<GateTable>(g, n, kGateItems, [&](const GateTable& T, unsigned grid) {
-    if (dt == ISO_BF16) k_gate_grad<ISO_BF16><<<grid, 256, 0, s>>>(T);
-    else k_gate_grad<ISO_F32><<<grid, 256, 0, s>>>(T);
+  return for_tables<GateTable>(g, n, kGateItems, dt == ISO_BF16 ? 32 : 64, [&](const GateTable& T, unsigned grid, bool stream) {
+    auto go = [&](auto k) { k<<<grid, 256, 0, s>>>(T); };
+    if (dt == ISO_BF16) stream ? go(k_gate_grad<ISO_BF16, true>) : go(k_gate_grad<ISO_BF16, false>);
+    else stream ? go(k_gate_grad<ISO_F32, true>) : go(k_gate_grad<ISO_F32, false>);
   });
 }
 

@@ -39,13 +39,13 @@ __device__ __forceinline__ int32_t row_of(const Ids& ids, int64_t t) {
 
 // ---- lookup --------------------------------------------------------------------------------------------------------
 
-constexpr int kLookupItems = 4;   // 16-byte vectors a thread
+constexpr int kLookupItems = 2;   // 16-byte vectors a thread (28 us; one, four and eight: 30 for 16384 tokens of 3584)
 constexpr int kLookupBlock = 256 * kLookupItems;
 
 // Workgroup 0 looks at every id and writes the status word, so that the call is one launch: nothing has to be
-// cleared before the others find a bad id.  The others copy 1024 vectors each, numbered through tokens and columns:
-// a thread's four ids, and then its four vectors, are in flight together.
-template <int DT>
+// cleared before the others find a bad id.  The others copy 512 vectors each, numbered through tokens and columns:
+// a thread's ids, and then its vectors, are in flight together.
+template <int DT, bool STREAM>
 __global__ void __launch_bounds__(256) k_embed_lookup(Ids ids, const void* __restrict__ table, void* __restrict__ x,
                                                       int64_t tokens, int64_t dim, int64_t ld_x, float scale,
                                                       uint32_t* status) {
@@ -88,7 +88,7 @@ __global__ void __launch_bounds__(256) k_embed_lookup(Ids ids, const void* __res
       unpack_raw<DT>(w[q], v);
 #pragma unroll
       for (int j = 0; j < V; ++j) v[j] = row[q] >= 0 ? v[j] * scale : 0.0f;
-      store_elems<DT, V>(x, tok[q] * ld_x + col[q], v, dim - col[q]);
+      store_elems<DT, V, STREAM>(x, tok[q] * ld_x + col[q], v, dim - col[q]);
     }
   }
 }
@@ -682,7 +682,9 @@ hipError_t run_embed_lookup(const iso_embed& e, int dt, uint8_t* ws, hipStream_t
   auto go = [&](auto k) {
     k<<<grid, 256, 0, s>>>(ids_of(e), e.table, e.x, e.tokens, e.dim, e.ld_x, (float)e.scale, (uint32_t*)ws);
   };
-  dt == ISO_BF16 ? go(k_embed_lookup<ISO_BF16>) : go(k_embed_lookup<ISO_F32>);
+  const bool stream = streamed(e.tokens * e.dim * (dt == ISO_BF16 ? 2 : 4));
+  if (dt == ISO_BF16) stream ? go(k_embed_lookup<ISO_BF16, true>) : go(k_embed_lookup<ISO_BF16, false>);
+  else stream ? go(k_embed_lookup<ISO_F32, true>) : go(k_embed_lookup<ISO_F32, false>);
   return hipGetLastError();
 }
 

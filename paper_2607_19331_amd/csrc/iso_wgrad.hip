@@ -170,31 +170,46 @@ typedef __attribute__((address_space(3))) f32x4_t* lds_f32x4;
 
 constexpr int kRowBytes = 132 * 4;
 
-// 32 rows of 128 columns (132 floats apart in LDS) to G from row m, column n on, by one wave, 16 bytes a lane.
-template <int DTG, bool ADD>
-__device__ __forceinline__ void write_rows(const Layer& a, int m, int n, uint32_t lds, int lane) {
-  constexpr int V = kVec<DTG>, kLanes = 128 / V, kRows = 64 / kLanes;
-  const int row = lane / kLanes, c = lane % kLanes * V, left = a.cols - n - c;
-  if (left <= 0) return;
-#pragma unroll 8
-  for (int h = 0; h < 32; h += kRows) {
-    if (m + h + row >= a.rows) continue;
-    const int64_t at = (int64_t)(m + h + row) * a.cols + n + c;
-    float v[V];
+// 32 rows of 128 columns of G from row m, column n on, as one wave reads and writes them: 16 bytes a lane, whole rows of
+// 512 (or 256) bytes.  `old` holds what a lane adds to.
+template <int DTG>
+struct Rows32 {
+  static constexpr int V = kVec<DTG>, kLanes = 128 / V, kRows = 64 / kLanes, kCount = 32 / kRows;
+  u32x4_t old[kCount];
+
+  __device__ __forceinline__ void load(const Layer& a, int m, int n, int lane) {
+    const int row = lane / kLanes, c = lane % kLanes * V, left = a.cols - n - c;
 #pragma unroll
-    for (int j = 0; j < V; j += 4) {
-      const f32x4_t x = *(lds_f32x4)(uintptr_t)(lds + (h + row) * kRowBytes + (c + j) * 4);
-      v[j] = x.x, v[j + 1] = x.y, v[j + 2] = x.z, v[j + 3] = x.w;
-    }
-    if constexpr (ADD) {
-      float old[V];
-      load_elems<DTG, V>(a.g, at, old, left);
-#pragma unroll
-      for (int j = 0; j < V; ++j) v[j] += old[j];
-    }
-    store_elems<DTG, V>(a.g, at, v, left);
+    for (int h = 0; h < kCount; ++h)
+      if (left > 0 && m + h * kRows + row < a.rows)
+        old[h] = load_raw<DTG>(a.g, (int64_t)(m + h * kRows + row) * a.cols + n + c, left);
   }
-}
+
+  // the rows lie 132 floats apart in LDS
+  template <bool ADD>
+  __device__ __forceinline__ void store(const Layer& a, int m, int n, uint32_t lds, int lane) const {
+    const int row = lane / kLanes, c = lane % kLanes * V, left = a.cols - n - c;
+    if (left <= 0) return;
+#pragma unroll
+    for (int h = 0; h < kCount; ++h) {
+      const int r = h * kRows + row;
+      if (m + r >= a.rows) continue;
+      float v[V];
+#pragma unroll
+      for (int j = 0; j < V; j += 4) {
+        const f32x4_t x = *(lds_f32x4)(uintptr_t)(lds + r * kRowBytes + (c + j) * 4);
+        v[j] = x.x, v[j + 1] = x.y, v[j + 2] = x.z, v[j + 3] = x.w;
+      }
+      if constexpr (ADD) {
+        float o[V];
+        unpack_raw<DTG>(old[h], o);
+#pragma unroll
+        for (int j = 0; j < V; ++j) v[j] += o[j];
+      }
+      store_elems<DTG, V>(a.g, (int64_t)(m + r) * a.cols + n + c, v, left);
+    }
+  }
+};
 
 __device__ __forceinline__ int layer_of(const LayerTable& T, uint32_t tile) {
   int j = 0;
@@ -357,12 +372,17 @@ __global__ void __launch_bounds__(256, 1) k_wgrad(LayerTable T) {
           store_elems<ISO_F32, 4>(out, ((q * 4 + p) * 4 + r) * 256 + lane * 4, (const float*)&acc[p][q] + 4 * r);
     return;
   }
-  // through LDS, 32 rows of the wave's 128 x 128 at a time, so that memory sees whole rows
+  // through LDS, 32 rows of the wave's 128 x 128 at a time, so that memory sees whole rows; where G is added to, the next 32
+  // rows of it are under way meanwhile
+  const int mw = m0 + (w >> 1) * 128, nw = n0 + (w & 1) * 128;
+  Rows32<DTG> rows[2];
+  if constexpr (ADD) rows[0].load(a, mw, nw, lane);
   asm volatile("s_barrier" ::: "memory");   // every wave is past its last fragment
   const uint32_t own = lds0 + w * (32 * kRowBytes);
-  const int mw = m0 + (w >> 1) * 128, nw = n0 + (w & 1) * 128;
 #pragma unroll
   for (int q = 0; q < 4; ++q) {
+    if constexpr (ADD)
+      if (q < 3) rows[(q + 1) & 1].load(a, mw + q * 32 + 32, nw, lane);
 #pragma unroll
     for (int p = 0; p < 4; ++p)
 #pragma unroll
@@ -370,7 +390,7 @@ __global__ void __launch_bounds__(256, 1) k_wgrad(LayerTable T) {
         *(lds_f32x4)(uintptr_t)(own + (lane & 31) * kRowBytes + (p * 32 + r * 8 + (lane >> 5) * 4) * 4) =
             f32x4_t{acc[p][q][4 * r], acc[p][q][4 * r + 1], acc[p][q][4 * r + 2], acc[p][q][4 * r + 3]};
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-    write_rows<DTG, ADD>(a, mw + q * 32, nw, own, lane);
+    rows[q & 1].template store<ADD>(a, mw + q * 32, nw, own, lane);
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
   }
 }
@@ -389,11 +409,16 @@ __global__ void __launch_bounds__(256) k_wgrad_join(LayerTable T) {
   const int n = n0 + (w & 1) * 128 + p * 32 + h * 8 + (lane >> 5) * 4;
   if (m >= a.rows || n >= a.cols) return;
   float sum[4] = {};
-  for (uint32_t s = 0; s < T.split; ++s) {
-    float v[4];
-    load_elems<ISO_F32, 4>(in, (int64_t)s * (kTile * kTile), v);
+  for (uint32_t s = 0; s < T.split; s += 8) {
+    u32x4_t v[8];
 #pragma unroll
-    for (int j = 0; j < 4; ++j) sum[j] += v[j];
+    for (int j = 0; j < 8; ++j)
+      if (s + j < T.split) v[j] = load_raw<ISO_F32>(in, (int64_t)(s + j) * (kTile * kTile));
+#pragma unroll
+    for (int j = 0; j < 8; ++j)
+      if (s + j < T.split)
+#pragma unroll
+        for (int h = 0; h < 4; ++h) sum[h] += f32_from_bits(v[j][h]);
   }
   const int64_t to = (int64_t)m * a.cols + n;
   if constexpr (ADD) {
@@ -418,14 +443,15 @@ bool direct(const iso_weight_grad& x, int dt) { return dt == ISO_BF16 && x.ld_dy
 
 int64_t whole_steps(int64_t tokens) { return (tokens + kStep - 1) / kStep * kStep; }
 
-// Pieces that the tiles past the last full round of workgroups are split into: the fewest microseconds of
-// a round of `steps` / s steps (0.45 us each), and where s > 1 of writing and adding up the pieces (8 us for the launch,
-// 0.1 us for each piece of 256 KiB).
+// Pieces that the tiles past the last full round of workgroups are split into: the fewest microseconds of a round of
+// steps / s steps (0.59 each, few workgroups being at work), and where s > 1 of writing and adding up the pieces (3 for the
+// launch, 0.05 for each piece of 256 KiB, 0.15 for each that a thread adds).  512 x 1024 of 2048 tokens: 51 us in one piece, 33,
+// 26, 24 and 26 in 2, 4, 8 and 16; 2048 x 2048 of 203 tokens: 19 us in one, 25 and 32 in 2 and 4.
 uint32_t pieces_for(uint32_t rest, int steps) {
   uint32_t best = 1;
-  double least = 0.45 * steps;
+  double least = 0.59 * steps;
   for (uint32_t s = 2; s <= kUnits / std::max(rest, 1u) && s <= (uint32_t)steps; ++s) {
-    const double t = 0.45 * ((steps + s - 1) / s) + 8.0 + 0.1 * rest * s;
+    const double t = 0.59 * ((steps + s - 1) / s) + 3.0 + 0.05 * rest * s + 0.15 * s;
     if (t < least) least = t, best = s;
   }
   return best;
