@@ -97,7 +97,6 @@ __global__ void __launch_bounds__(256) k_embed_lookup(Ids ids, const void* __res
 
 // The tokens of an id are added in runs of kRun, whose sums are then added in order.
 constexpr int kRun = 32;
-constexpr int kFlight = 8;     // rows whose loads are in flight together
 
 // Lanes of the wave whose key equals this lane's (of those with `on`), by one ballot per key bit.
 __device__ __forceinline__ uint64_t peers(uint32_t key, int bits, bool on) {
@@ -150,7 +149,9 @@ struct Rows {
   float scale;
 };
 
-// acc += the rows of dX of up to 64 tokens (lane l holds the l-th) for this lane's columns, in order.
+// acc += the rows of dX of up to 64 tokens (lane l holds the l-th) for this lane's columns, in order; eight rows' loads are
+// in flight together (32 in k_embed_parts took no less time).
+constexpr int kFlight = 8;
 template <int DT>
 __device__ __forceinline__ void add_rows(const Rows& a, uint32_t mine, uint32_t count, int64_t col, float* acc) {
   const int64_t left = a.dim - col;
@@ -336,7 +337,7 @@ __global__ void __launch_bounds__(256) k_embed_fill(Fill f) { fill_zeros(f, bloc
 // ---- gradient: many tokens -----------------------------------------------------------------------------------------
 //
 // Count (with further workgroups that write the gradient's zeros), scatter into buckets, sort each bucket, partial sums of
-// frequent ids, rows.  32768 tokens into 152064 x 3584 in bf16: 274 us, of which the zeros take 150 (1.09 GB), the sort's
+// frequent ids, rows.  32768 tokens into 152064 x 3584 in bf16: 266 us, of which the zeros take 150 (1.09 GB), the sort's
 // latencies 20, the reads of dX and the rows that have tokens the rest; their bytes alone would take 209.  Spreading the zeros
 // over the first four launches, under whose latencies they would hide, gained nothing (270 to 280 us).
 
@@ -514,18 +515,19 @@ __global__ void __launch_bounds__(256) k_embed_parts(const uint32_t* __restrict_
   }
 }
 
-// The gradient's rows that have tokens.  Frequent ids first, a workgroup a column block: its waves add up a quarter of the
-// id's runs each, in order, and then the quarters.  The others take a wave a column block; a wave has the list's entry after
+// The gradient's rows that have tokens.  Frequent ids take a workgroup a column block: its waves add up a quarter of the id's
+// runs each, in order, and then the quarters.  The others take a wave a column block; a wave has the list's entry after
 // next and the next one's tokens under way while it adds the current rows, so that it waits for one memory access a row
 // block instead of three.
 template <int DT, int DTG, bool ADD>
 __global__ void __launch_bounds__(256) k_embed_rows(const uint32_t* __restrict__ perm, Lists l, Rows a, int64_t blocks,
                                                     const float* __restrict__ part) {
-  constexpr int V = kVec<DT>, kSums = 2;
+  constexpr int V = kVec<DT>, kSums = 4;
   __shared__ float quarter[4][V][64];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int64_t many = (int64_t)l.n[2] * blocks, items = (int64_t)l.n[0] * blocks;
-  for (int64_t b = blockIdx.x; b < many; b += gridDim.x) {
+  const uint32_t own = (uint32_t)min(many, (int64_t)(gridDim.x / 2));   // workgroups of the frequent ids
+  for (int64_t b = blockIdx.x; b < many && blockIdx.x < own; b += own) {
     const int64_t unit = b / blocks;
     const uint4 id = l.many[unit];
     const int64_t col = (b - unit * blocks) * (64 * V) + lane * V;
@@ -553,8 +555,9 @@ __global__ void __launch_bounds__(256) k_embed_rows(const uint32_t* __restrict__
     }
     __syncthreads();
   }
-  const int64_t stride = (int64_t)gridDim.x * 4;
-  int64_t item = (int64_t)blockIdx.x * 4 + wave;
+  if (blockIdx.x < own) return;
+  const int64_t stride = (int64_t)(gridDim.x - own) * 4;
+  int64_t item = (int64_t)(blockIdx.x - own) * 4 + wave;
   auto entry = [&](int64_t at) { return at < items ? l.ids[at / blocks] : make_uint4(0, 0, 0, 0); };
   auto tokens = [&](const uint4& id) { return (uint32_t)lane < id.z ? perm[id.y + lane] : 0u; };
   uint4 now = entry(item), next = entry(item + stride);
@@ -637,7 +640,7 @@ hipError_t grad_many(const iso_embed& e, const Rows& a, uint8_t* ws, hipStream_t
   const int64_t blocks = (e.dim + 64 * kVec<DT> - 1) / (64 * kVec<DT>);
   k_embed_parts<DT><<<(unsigned)std::min<int64_t>((P.most_runs * blocks + 3) / 4, 2048), 256, 0, s>>>(perm, l, a, blocks, part);
   const int64_t most = (std::min(e.tokens, e.vocab) * blocks + 3) / 4;
-  k_embed_rows<DT, DTG, ADD><<<(unsigned)std::min<int64_t>(most, 2048), 256, 0, s>>>(perm, l, a, blocks, part);
+  k_embed_rows<DT, DTG, ADD><<<(unsigned)std::min<int64_t>(most + 1, 2048), 256, 0, s>>>(perm, l, a, blocks, part);
   return hipGetLastError();
 }
 
