@@ -6,7 +6,7 @@
 //
 // A call is up to three launches per 16 layers.  k_wgrad_prep brings operands into the form that the product reads,
 // bf16 rows aligned to 16 bytes: X always (once per checkpoint, however many layers share it), dY where it is fp32 or
-// its stride is odd.  k_wgrad forms 256 x 256 tiles of all layers.  k_wgrad_join adds up tiles whose tokens were split.
+// its stride is odd.  k_wgrad forms the tiles of all layers' gradients.  k_wgrad_join adds up tiles whose tokens were split.
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
@@ -23,11 +23,21 @@ namespace iso {
 namespace {
 
 constexpr int kLayers = 16;          // layers a launch
-constexpr int kTile = 256;           // a workgroup's tile of G
 constexpr int kStep = 32;            // tokens of a step
 constexpr int kStages = 4;           // steps in LDS
-constexpr int kStageBytes = 2 * kStep * kTile * 2;
-constexpr int kUnits = 256;          // workgroups that run at once: one a CU
+
+// A workgroup's tile of G, 256 x 256 or 128 x 128.
+template <int TILE>
+struct Tile {
+  static constexpr int kQuarter = TILE / 2;                 // a wave has kQuarter x kQuarter
+  static constexpr int kFrags = kQuarter / 32;              // fragments of 32 columns of a panel a wave reads
+  static constexpr int kRowBytes = TILE * 2;                // a token's row of a panel
+  static constexpr int kPanel = kStep * kRowBytes;
+  static constexpr int kStage = 2 * kPanel;
+  static constexpr int kLoads = TILE / 64;                  // 16-byte loads a lane and panel
+  static constexpr int kOutBytes = (kQuarter + 4) * 4;      // a row of the result in LDS
+  static constexpr int kUnits = TILE == 256 ? 256 : 512;    // workgroups that run at once: one or two a CU
+};
 constexpr int64_t kMaxStride = 1 << 25;   // 32 rows of it stay within 32-bit offsets
 
 // ---- operand preparation -------------------------------------------------------------------------------------------
@@ -128,7 +138,7 @@ struct Layer {
   int64_t y_ld, x_ld;          // row strides, bytes
   int64_t y_bytes, x_bytes;    // bytes from the first element to past the last (dY: of all its parts)
   int32_t rows, cols;          // of G
-  int32_t across;              // tiles of a tile row
+  int32_t across, down;        // tiles of a tile row, and tile rows
   int32_t steps, parts;        // steps of a part of dY
   uint32_t tile0;
 };
@@ -139,7 +149,7 @@ struct LayerTable {
   uint32_t tiles;     // of all layers
   uint32_t whole;     // tiles one workgroup does alone; the others' tokens are split `split` ways
   uint32_t split;
-  float* part;        // their partial sums, kTile * kTile a piece, (tile, piece) in order
+  float* part;        // their partial sums, a tile's size a piece, (tile, piece) in order
 };
 
 typedef __attribute__((address_space(3))) uint8_t lds_u8;
@@ -168,13 +178,11 @@ __device__ __forceinline__ void load_lds(u32x4_t buffer, uint32_t lds, uint32_t 
 
 typedef __attribute__((address_space(3))) f32x4_t* lds_f32x4;
 
-constexpr int kRowBytes = 132 * 4;
-
-// 32 rows of 128 columns of G from row m, column n on, as one wave reads and writes them: 16 bytes a lane, whole rows of
-// 512 (or 256) bytes.  `old` holds what a lane adds to.
-template <int DTG>
+// 32 rows of a wave's part of G from row m, column n on, as it reads and writes them: 16 bytes a lane, whole rows.  `old`
+// holds what a lane adds to.
+template <int TILE, int DTG>
 struct Rows32 {
-  static constexpr int V = kVec<DTG>, kLanes = 128 / V, kRows = 64 / kLanes, kCount = 32 / kRows;
+  static constexpr int V = kVec<DTG>, kLanes = Tile<TILE>::kQuarter / V, kRows = 64 / kLanes, kCount = 32 / kRows;
   u32x4_t old[kCount];
 
   __device__ __forceinline__ void load(const Layer& a, int m, int n, int lane) {
@@ -185,7 +193,6 @@ struct Rows32 {
         old[h] = load_raw<DTG>(a.g, (int64_t)(m + h * kRows + row) * a.cols + n + c, left);
   }
 
-  // the rows lie 132 floats apart in LDS
   template <bool ADD>
   __device__ __forceinline__ void store(const Layer& a, int m, int n, uint32_t lds, int lane) const {
     const int row = lane / kLanes, c = lane % kLanes * V, left = a.cols - n - c;
@@ -197,7 +204,7 @@ struct Rows32 {
       float v[V];
 #pragma unroll
       for (int j = 0; j < V; j += 4) {
-        const f32x4_t x = *(lds_f32x4)(uintptr_t)(lds + r * kRowBytes + (c + j) * 4);
+        const f32x4_t x = *(lds_f32x4)(uintptr_t)(lds + r * Tile<TILE>::kOutBytes + (c + j) * 4);
         v[j] = x.x, v[j + 1] = x.y, v[j + 2] = x.z, v[j + 3] = x.w;
       }
       if constexpr (ADD) {
@@ -219,11 +226,12 @@ __device__ __forceinline__ int layer_of(const LayerTable& T, uint32_t tile) {
 
 // Origin of a layer's tile: bands of eight tile rows, walked down their columns, so that the 32 tiles an XCD works on
 // at once are 8 x 4 and share 12 panels in its L2.
+template <int TILE>
 __device__ __forceinline__ void tile_origin(const Layer& a, uint32_t tile, int& m0, int& n0) {
-  const int t = (int)(tile - a.tile0), down = (a.rows + kTile - 1) / kTile;
-  const int band = t / (8 * a.across), r0 = band * 8, h = min(8, down - r0), in = t - r0 * a.across;
-  m0 = (r0 + in % h) * kTile;
-  n0 = in / h * kTile;
+  const int t = (int)(tile - a.tile0);
+  const int band = t / (8 * a.across), r0 = band * 8, h = min(8, a.down - r0), in = t - r0 * a.across;
+  m0 = (r0 + in % h) * TILE;
+  n0 = in / h * TILE;
 }
 
 // Consecutive pieces of [0, n) for the workgroups of one XCD (workgroup b runs on XCD b % 8).
@@ -232,19 +240,22 @@ __device__ __forceinline__ uint32_t by_xcd(uint32_t b, uint32_t n) {
   return x * each + min(x, more) + (b >> 3);
 }
 
-// One 256 x 256 tile of G (or a share of its tokens) a workgroup of four waves, each with 128 x 128 of it in 256
-// accumulator registers a lane.
-//   Steps of 32 tokens go from memory straight into LDS, four stages deep (two 16 KiB panels each, token rows of 512
+// One tile of G (or a share of its tokens) a workgroup of four waves, each with a quarter of it in accumulators: 256 registers
+// a lane for 256 x 256, 64 for 128 x 128.
+//   Steps of 32 tokens go from memory straight into LDS, four stages deep (two panels each, a token's row of 512 or 256
 // bytes); both operands have their tokens along the slow dimension, so fragments come through the transposing LDS read,
 // 16 lanes a 4 token x 16 column block.  The four 64-byte pieces that the first (or second) half of a wave reads at once
 // come from four successive token rows; piece c of row t lies at c ^ (t & 3), which puts the four into different quarters
 // of the 64 banks (no conflicts counted), while 64 bytes of memory stay together.
-//   The loop is laid out by hand, one LDS read or load between two matrix instructions: fragments of the next half step
-// are read, and loads issued, under the 16 products of the current one.  At the middle of a step all its fragments are in
-// registers: one barrier there frees its stage and vouches for the next.
-//   Bound by the power that matrix products of full entropy take (the clock falls to about 1.9 GHz) and the loads' issue.
-template <int DTG, bool ADD>
+//   The loop is laid out by hand, one LDS read or load between two matrix instructions (1335 -> 1600 TFLOP/s on zeros, 1170 ->
+// 1290 on random values at 4096 x 4096 of 8192 tokens): fragments of the next half step are read, and loads issued, under
+// the products of the current one.  At the middle of a step all its fragments are in registers: one barrier there frees its
+// stage and vouches for the next.
+//   Bound by the power that matrix products of random values take (the clock falls to about 1.9 GHz) and the loads' issue.
+template <int TILE, int DTG, bool ADD>
 __global__ void __launch_bounds__(256, 1) k_wgrad(LayerTable T) {
+  using S = Tile<TILE>;
+  constexpr int F = S::kFrags, L = S::kLoads, kReads = 4 * F;
   extern __shared__ __attribute__((aligned(1024))) uint8_t smem[];
   const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
   uint32_t tile, piece = 0, pieces = 1;
@@ -258,19 +269,20 @@ __global__ void __launch_bounds__(256, 1) k_wgrad(LayerTable T) {
   }
   const Layer& a = T.l[layer_of(T, tile)];
   int m0, n0;
-  tile_origin(a, tile, m0, n0);
+  tile_origin<TILE>(a, tile, m0, n0);
   const int all = a.steps * a.parts;
   const int first = (int)((int64_t)all * piece / pieces), last = (int)((int64_t)all * (piece + 1) / pieces);
   const int steps = last - first;
 
-  // loads: 16-byte column c of token row 8 j + row
-  const int row = 2 * w + (lane >> 5), c = lane & 31;
+  // loads: a wave's 1024 bytes are kAtOnce token rows; load j takes 16-byte column c of row 4 kAtOnce j + row
+  constexpr int kAtOnce = 1024 / S::kRowBytes, kAcross = 64 / kAtOnce;
+  const int row = w * kAtOnce + lane / kAcross, c = lane % kAcross;
   const uint32_t col = (uint32_t)(((c >> 2) ^ (row & 3)) * 64 + (c & 3) * 16);
-  uint32_t vy[4], vx[4];
+  uint32_t vy[L], vx[L];
 #pragma unroll
-  for (int j = 0; j < 4; ++j) {
-    vy[j] = (uint32_t)(row + 8 * j) * (uint32_t)a.y_ld + col;
-    vx[j] = (uint32_t)(row + 8 * j) * (uint32_t)a.x_ld + col;
+  for (int j = 0; j < L; ++j) {
+    vy[j] = (uint32_t)(row + 4 * kAtOnce * j) * (uint32_t)a.y_ld + col;
+    vx[j] = (uint32_t)(row + 4 * kAtOnce * j) * (uint32_t)a.x_ld + col;
   }
   const uint8_t* const x_base = a.x + 2 * (int64_t)n0;
   const int64_t x_left0 = a.x_bytes - 2 * (int64_t)n0, y_step = kStep * a.y_ld, x_step = kStep * a.x_ld;
@@ -287,72 +299,71 @@ __global__ void __launch_bounds__(256, 1) k_wgrad(LayerTable T) {
     if (++x_at == a.steps) x_at = 0, xp = x_base, x_left = x_left0;
   };
   const uint32_t lds0 = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(lds_u8*)smem);
-  auto load = [&](int j, int stage) {
-    const uint32_t to = lds0 + stage * kStageBytes + w * 1024;
-    if (j < 4) load_lds(yb, to + j * 4096, vy[j]);
-    else load_lds(xb, to + kStageBytes / 2 + (j - 4) * 4096, vx[j - 4]);
-  };
+  auto load_y = [&](int j, int stage) { load_lds(yb, lds0 + stage * S::kStage + w * 1024 + j * 4096, vy[j]); };
+  auto load_x = [&](int j, int stage) { load_lds(xb, lds0 + stage * S::kStage + S::kPanel + w * 1024 + j * 4096, vx[j]); };
 
   // fragments f of 32 columns: lane's token rows (lane / 32) * 8 ..., columns lane % 32
   const int g = lane >> 4, i = lane & 15;
-  uint32_t ay[4], ax[4];
+  uint32_t ay[F], ax[F];
 #pragma unroll
-  for (int f = 0; f < 4; ++f) {
-    const uint32_t at = lds0 + ((g >> 1) * 8 + (i >> 2)) * 512 + (f ^ (i >> 2)) * 64 + (g & 1) * 32 + (i & 3) * 8;
-    ay[f] = at + (w >> 1) * 256;
-    ax[f] = at + (w & 1) * 256 + kStageBytes / 2;
+  for (int f = 0; f < F; ++f) {
+    const uint32_t at = lds0 + ((g >> 1) * 8 + (i >> 2)) * S::kRowBytes + (g & 1) * 32 + (i & 3) * 8;
+    ay[f] = at + (((w >> 1) * F + f) ^ (i >> 2)) * 64;
+    ax[f] = at + (((w & 1) * F + f) ^ (i >> 2)) * 64 + S::kPanel;
   }
   struct Frag {
     s16x4_t h[2];
   };
-  Frag fx[2][4], fy[2][4];
-  auto read = [&](int set, int q, uint32_t offset) {   // piece q of 16: x0 y0 y1 y2 y3 x1 x2 x3, two halves each
+  Frag fx[2][F], fy[2][F];
+  auto read = [&](int set, int q, uint32_t offset) {   // piece q: x0 y0 y1 ... x1 x2 ..., two halves each
     const int n = q >> 1, h = q & 1;
-    const uint32_t at = (n == 0 ? ax[0] : n < 5 ? ay[n - 1] : ax[n - 4]) + offset + h * 2048;
+    const uint32_t at = (n == 0 ? ax[0] : n <= F ? ay[n - 1] : ax[n - F]) + offset + h * (4 * S::kRowBytes);
     const s16x4_t v = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_frag)(uintptr_t)at);
     if (n == 0) fx[set][0].h[h] = v;
-    else if (n < 5) fy[set][n - 1].h[h] = v;
-    else fx[set][n - 4].h[h] = v;
+    else if (n <= F) fy[set][n - 1].h[h] = v;
+    else fx[set][n - F].h[h] = v;
   };
-  f32x16_t acc[4][4];
+  f32x16_t acc[F][F];
 #pragma unroll
-  for (int p = 0; p < 4; ++p)
+  for (int p = 0; p < F; ++p)
 #pragma unroll
-    for (int q = 0; q < 4; ++q) acc[p][q] = 0.0f;
+    for (int q = 0; q < F; ++q) acc[p][q] = 0.0f;
   auto multiply = [&](int set, int q) {
-    acc[q >> 2][q & 3] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, fx[set][q >> 2]),
-                                                                 __builtin_bit_cast(bf16x8_t, fy[set][q & 3]),
-                                                                 acc[q >> 2][q & 3], 0, 0, 0);
+    acc[q / F][q % F] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, fx[set][q / F]),
+                                                               __builtin_bit_cast(bf16x8_t, fy[set][q % F]),
+                                                               acc[q / F][q % F], 0, 0, 0);
   };
 
   // the last stage's X panel is loaded in the first step
   for (int s = 0; s < kStages; ++s) {
     next();
 #pragma unroll
-    for (int j = 0; j < 8; ++j)
-      if (s < kStages - 1 || j < 4) load(j, s);
-  }
-  asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" ::"n"((kStages - 2) * 8 + 4) : "memory");
+    for (int j = 0; j < L; ++j) load_y(j, s);
+    if (s < kStages - 1)
 #pragma unroll
-  for (int q = 0; q < 16; ++q) read(0, q, 0);
+      for (int j = 0; j < L; ++j) load_x(j, s);
+  }
+  asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" ::"n"((kStages - 2) * 2 * L + L) : "memory");
+#pragma unroll
+  for (int q = 0; q < kReads; ++q) read(0, q, 0);
   int stage = 0, before = kStages - 1;
   for (int t = 0; t < steps; ++t) {
     const int after = stage + 1 == kStages ? 0 : stage + 1;
 #pragma unroll
-    for (int q = 0; q < 16; ++q) {
-      read(1, q, stage * kStageBytes + 8192);
-      multiply(0, q);
-      if ((q & 3) == 1) load(4 + (q >> 2), before);
+    for (int q = 0; q < kReads; ++q) {
+      read(1, q, stage * S::kStage + 16 * S::kRowBytes);
+      if (q * F % 4 == 0) multiply(0, q * F / 4);
+      if ((q & 3) == 1) load_x(q >> 2, before);
       __builtin_amdgcn_sched_barrier(0);
     }
     next();
-    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"((kStages - 2) * 8) : "memory");
+    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"((kStages - 2) * 2 * L) : "memory");
     __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-    for (int q = 0; q < 16; ++q) {
-      read(0, q, after * kStageBytes);
-      multiply(1, q);
-      if ((q & 3) == 1) load(q >> 2, stage);
+    for (int q = 0; q < kReads; ++q) {
+      read(0, q, after * S::kStage);
+      if (q * F % 4 == 0) multiply(1, q * F / 4);
+      if ((q & 3) == 1) load_y(q >> 2, stage);
       __builtin_amdgcn_sched_barrier(0);
     }
     before = stage;
@@ -362,32 +373,32 @@ __global__ void __launch_bounds__(256, 1) k_wgrad(LayerTable T) {
 
   // a lane holds four consecutive columns of a row in every four registers
   if (pieces > 1) {
-    float* const out = T.part + ((int64_t)(tile - T.whole) * pieces + piece) * (kTile * kTile) + w * (128 * 128);
+    float* const out = T.part + ((int64_t)(tile - T.whole) * pieces + piece) * (TILE * TILE) + w * (S::kQuarter * S::kQuarter);
 #pragma unroll
-    for (int q = 0; q < 4; ++q)
+    for (int q = 0; q < F; ++q)
 #pragma unroll
-      for (int p = 0; p < 4; ++p)
+      for (int p = 0; p < F; ++p)
 #pragma unroll
         for (int r = 0; r < 4; ++r)
-          store_elems<ISO_F32, 4>(out, ((q * 4 + p) * 4 + r) * 256 + lane * 4, (const float*)&acc[p][q] + 4 * r);
+          store_elems<ISO_F32, 4>(out, ((q * F + p) * 4 + r) * 256 + lane * 4, (const float*)&acc[p][q] + 4 * r);
     return;
   }
-  // through LDS, 32 rows of the wave's 128 x 128 at a time, so that memory sees whole rows; where G is added to, the next 32
+  // through LDS, 32 rows of the wave's quarter at a time, so that memory sees whole rows; where G is added to, the next 32
   // rows of it are under way meanwhile
-  const int mw = m0 + (w >> 1) * 128, nw = n0 + (w & 1) * 128;
-  Rows32<DTG> rows[2];
+  const int mw = m0 + (w >> 1) * S::kQuarter, nw = n0 + (w & 1) * S::kQuarter;
+  Rows32<TILE, DTG> rows[2];
   if constexpr (ADD) rows[0].load(a, mw, nw, lane);
   asm volatile("s_barrier" ::: "memory");   // every wave is past its last fragment
-  const uint32_t own = lds0 + w * (32 * kRowBytes);
+  const uint32_t own = lds0 + w * (32 * S::kOutBytes);
 #pragma unroll
-  for (int q = 0; q < 4; ++q) {
+  for (int q = 0; q < F; ++q) {
     if constexpr (ADD)
-      if (q < 3) rows[(q + 1) & 1].load(a, mw + q * 32 + 32, nw, lane);
+      if (q + 1 < F) rows[(q + 1) & 1].load(a, mw + q * 32 + 32, nw, lane);
 #pragma unroll
-    for (int p = 0; p < 4; ++p)
+    for (int p = 0; p < F; ++p)
 #pragma unroll
       for (int r = 0; r < 4; ++r)
-        *(lds_f32x4)(uintptr_t)(own + (lane & 31) * kRowBytes + (p * 32 + r * 8 + (lane >> 5) * 4) * 4) =
+        *(lds_f32x4)(uintptr_t)(own + (lane & 31) * S::kOutBytes + (p * 32 + r * 8 + (lane >> 5) * 4) * 4) =
             f32x4_t{acc[p][q][4 * r], acc[p][q][4 * r + 1], acc[p][q][4 * r + 2], acc[p][q][4 * r + 3]};
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
     rows[q & 1].template store<ADD>(a, mw + q * 32, nw, own, lane);
@@ -395,25 +406,26 @@ __global__ void __launch_bounds__(256, 1) k_wgrad(LayerTable T) {
   }
 }
 
-// Adds up the pieces of the split tiles, in order: a thread four columns of a row, 64 workgroups a tile.
-template <int DTG, bool ADD>
+// Adds up the pieces of the split tiles, in order: a thread four columns of a row.
+template <int TILE, int DTG, bool ADD>
 __global__ void __launch_bounds__(256) k_wgrad_join(LayerTable T) {
-  const uint32_t r = blockIdx.x >> 6, tile = T.whole + r;
+  constexpr int F = Tile<TILE>::kFrags, kQuarter = Tile<TILE>::kQuarter, kBlocks = TILE * TILE / 1024;
+  const uint32_t r = blockIdx.x / kBlocks, tile = T.whole + r;
   const Layer& a = T.l[layer_of(T, tile)];
   int m0, n0;
-  tile_origin(a, tile, m0, n0);
-  const int at = (int)(blockIdx.x & 63u) * 1024 + threadIdx.x * 4;
-  const float* const in = T.part + (int64_t)r * T.split * (kTile * kTile) + at;
-  const int w = at >> 14, q = (at >> 12) & 3, p = (at >> 10) & 3, h = (at >> 8) & 3, lane = (at >> 2) & 63;
-  const int m = m0 + (w >> 1) * 128 + q * 32 + (lane & 31);
-  const int n = n0 + (w & 1) * 128 + p * 32 + h * 8 + (lane >> 5) * 4;
+  tile_origin<TILE>(a, tile, m0, n0);
+  const int at = (int)(blockIdx.x % kBlocks) * 1024 + threadIdx.x * 4;
+  const float* const in = T.part + (int64_t)r * T.split * (TILE * TILE) + at;
+  const int w = at / (kQuarter * kQuarter), q = at / (F * 1024) % F, p = at / 1024 % F, h = (at >> 8) & 3, lane = (at >> 2) & 63;
+  const int m = m0 + (w >> 1) * kQuarter + q * 32 + (lane & 31);
+  const int n = n0 + (w & 1) * kQuarter + p * 32 + h * 8 + (lane >> 5) * 4;
   if (m >= a.rows || n >= a.cols) return;
   float sum[4] = {};
   for (uint32_t s = 0; s < T.split; s += 8) {
     u32x4_t v[8];
 #pragma unroll
     for (int j = 0; j < 8; ++j)
-      if (s + j < T.split) v[j] = load_raw<ISO_F32>(in, (int64_t)(s + j) * (kTile * kTile));
+      if (s + j < T.split) v[j] = load_raw<ISO_F32>(in, (int64_t)(s + j) * (TILE * TILE));
 #pragma unroll
     for (int j = 0; j < 8; ++j)
       if (s + j < T.split)
@@ -436,6 +448,7 @@ __global__ void __launch_bounds__(256) k_wgrad_join(LayerTable T) {
 struct Plan {
   PrepTable prep{};
   LayerTable layers{};
+  int tile = 256;
   size_t total = 0;
 };
 
@@ -443,18 +456,49 @@ bool direct(const iso_weight_grad& x, int dt) { return dt == ISO_BF16 && x.ld_dy
 
 int64_t whole_steps(int64_t tokens) { return (tokens + kStep - 1) / kStep * kStep; }
 
-// Pieces that the tiles past the last full round of workgroups are split into: the fewest microseconds of a round of
-// steps / s steps (0.59 each, few workgroups being at work), and where s > 1 of writing and adding up the pieces (3 for the
-// launch, 0.05 for each piece of 256 KiB, 0.15 for each that a thread adds).  512 x 1024 of 2048 tokens: 51 us in one piece, 33,
-// 26, 24 and 26 in 2, 4, 8 and 16; 2048 x 2048 of 203 tokens: 19 us in one, 25 and 32 in 2 and 4.
-uint32_t pieces_for(uint32_t rest, int steps) {
-  uint32_t best = 1;
-  double least = 0.59 * steps;
-  for (uint32_t s = 2; s <= kUnits / std::max(rest, 1u) && s <= (uint32_t)steps; ++s) {
-    const double t = 0.59 * ((steps + s - 1) / s) + 3.0 + 0.05 * rest * s + 0.15 * s;
-    if (t < least) least = t, best = s;
+// How the tiles of a table, of `side` x `side`, are shared out: full rounds of workgroups take whole tiles, those past the
+// last full round are split into the pieces that take the fewest microseconds, by an estimate from measured parts: a step,
+// which takes longer the more workgroups are at work (memory, clock); a workgroup's start and end; for split tiles the second
+// launch, the pieces' writes and reads, and each piece that a thread adds.  The table takes the side whose estimate is less.
+// bf16 in microseconds, 256 x 256 tiles against 128 x 128: 2048 x 2048 of 203 tokens 18.6 and 15.4, of 1024 34 and 22, of 8192 95
+// and 108; four such matrices of 2048 tokens 72 and 88; 512 x 1024 of 512 tokens 19.3 and 15.8.  In one to sixteen pieces
+// (256 x 256) 512 x 1024 of 2048 tokens took 51, 33, 26, 24 and 26, 2048 x 2048 of 203 tokens 19, 25 and 32.
+struct Schedule {
+  uint32_t tiles = 0, whole = 0, split = 1;
+  double us = 0.0;
+};
+
+Schedule schedule(const std::vector<Layer>& layers, int side) {
+  const bool big = side == 256;
+  const double few = big ? 0.59 : 0.35, full = big ? 0.89 : 0.60, ends = big ? 8.0 : 5.0, piece = big ? 0.05 : 0.0125;
+  const uint32_t units = big ? Tile<256>::kUnits : Tile<128>::kUnits, alone = big ? 0 : 256;   // 256: one small tile a CU
+  auto step = [&](uint32_t n) { return few + (full - few) * (double)(n - std::min(n, alone)) / (units - alone); };
+  Schedule S;
+  std::vector<std::pair<uint32_t, int>> runs;   // tiles and their steps
+  for (const Layer& l : layers) {
+    const uint32_t n = (uint32_t)((l.rows + side - 1) / side) * (uint32_t)((l.cols + side - 1) / side);
+    runs.emplace_back(n, l.steps * l.parts);
+    S.tiles += n;
   }
-  return best;
+  S.whole = S.tiles / units * units;
+  uint32_t at = 0;
+  int steps = 0;   // of the longest tile past the full rounds
+  for (const auto& r : runs) {
+    const uint32_t in = std::min(r.first, S.whole > at ? S.whole - at : 0u);
+    S.us += (double)in / units * (full * r.second + ends);
+    if (in < r.first) steps = std::max(steps, r.second);
+    at += r.first;
+  }
+  const uint32_t rest = S.tiles - S.whole;
+  if (rest == 0) return S;
+  double least = step(rest) * steps + ends;
+  for (uint32_t s = 2; s <= units / rest && s <= (uint32_t)steps; ++s) {
+    const double us = step(rest * s) * ((steps + s - 1) / s) + ends + 3.0 + piece * rest * s + 0.15 * s;
+    if (us < least) least = us, S.split = s;
+  }
+  S.us += least;
+  if (S.split == 1) S.whole = S.tiles;
+  return S;
 }
 
 Plan plan_layers(const iso_weight_grad* g, int n, int dt, bool accumulate, uint8_t* ws) {
@@ -484,7 +528,6 @@ Plan plan_layers(const iso_weight_grad* g, int n, int dt, bool accumulate, uint8
     Layer l{};
     l.g = x.grad;
     l.rows = (int32_t)x.rows, l.cols = (int32_t)x.in.cols;
-    l.across = (l.cols + kTile - 1) / kTile;
     l.steps = (int32_t)(whole_steps(t) / kStep);
     l.parts = parts;
     const int64_t ld = ckpt_ld(x.in.cols);
@@ -516,38 +559,43 @@ Plan plan_layers(const iso_weight_grad* g, int n, int dt, bool accumulate, uint8
   // long sums first: the tiles past the last full round, which may be split, are then the shortest
   std::stable_sort(layers.begin(), layers.end(), [](const Layer& a, const Layer& b) { return a.steps > b.steps; });
   LayerTable& L = P.layers;
+  const Schedule big = schedule(layers, 256), small = schedule(layers, 128);
+  P.tile = small.us < big.us ? 128 : 256;
+  const Schedule& S = P.tile == 128 ? small : big;
+  L.whole = S.whole, L.split = S.split;
   for (Layer& l : layers) {
+    l.across = (l.cols + P.tile - 1) / P.tile, l.down = (l.rows + P.tile - 1) / P.tile;
     l.tile0 = L.tiles;
-    L.tiles += (uint32_t)((l.rows + kTile - 1) / kTile * l.across);
+    L.tiles += (uint32_t)l.across * (uint32_t)l.down;
     L.l[L.n++] = l;
   }
-  L.whole = L.tiles / kUnits * kUnits;
-  L.split = 1;
-  if (L.tiles > L.whole) {
-    int steps = 0;
-    for (const Layer& l : layers)
-      if (l.tile0 + (uint32_t)((l.rows + kTile - 1) / kTile * l.across) > L.whole) steps = std::max(steps, l.steps * l.parts);
-    L.split = pieces_for(L.tiles - L.whole, steps);
-    if (L.split == 1) L.whole = L.tiles;
-  }
-  L.part = (float*)region(sizeof(float) * kTile * kTile * (size_t)(L.tiles - L.whole) * L.split);
+  L.part = (float*)region(sizeof(float) * P.tile * P.tile * (size_t)(L.tiles - L.whole) * L.split);
   P.prep.status = (uint32_t*)ws;
   P.total = at;
   return P;
 }
 
-template <int DTG, bool ADD>
-void launch(const LayerTable& L, hipStream_t s) {
+template <int TILE, int DTG, bool ADD>
+void launch_tiles(const LayerTable& L, hipStream_t s) {
+  // the result passes through LDS too: no more of it than the stages take
+  static_assert(4 * 32 * Tile<TILE>::kOutBytes <= kStages * Tile<TILE>::kStage, "result rows fit into the stages");
   const uint32_t rest = L.tiles - L.whole;
-  k_wgrad<DTG, ADD><<<L.whole + rest * L.split, 256, kStages * kStageBytes, s>>>(L);
-  if (rest > 0) k_wgrad_join<DTG, ADD><<<rest * 64, 256, 0, s>>>(L);
+  k_wgrad<TILE, DTG, ADD><<<L.whole + rest * L.split, 256, kStages * Tile<TILE>::kStage, s>>>(L);
+  if (rest > 0) k_wgrad_join<TILE, DTG, ADD><<<rest * (TILE * TILE / 1024), 256, 0, s>>>(L);
+}
+
+template <int DTG, bool ADD>
+void launch(const Plan& P, hipStream_t s) {
+  P.tile == 128 ? launch_tiles<128, DTG, ADD>(P.layers, s) : launch_tiles<256, DTG, ADD>(P.layers, s);
 }
 
 }  // namespace
 
 size_t weight_grad_workspace_bytes(const iso_weight_grad* g, int n, int dt) {
   size_t most = kStatusBytes;
-  for (int j = 0; j < n; j += kLayers) most = std::max(most, plan_layers(g + j, std::min(kLayers, n - j), dt, false, nullptr).total);
+  for (int j = 0; j < n; j += kLayers)
+    for (bool accumulate : {false, true})   // a layer without tokens takes part in the one and not in the other
+      most = std::max(most, plan_layers(g + j, std::min(kLayers, n - j), dt, accumulate, nullptr).total);
   return most;
 }
 
@@ -558,8 +606,8 @@ hipError_t run_weight_grad(const iso_weight_grad* g, int n, int dt, int dt_grad,
     if (dt == ISO_BF16) k_wgrad_prep<ISO_BF16><<<grid, 256, 0, s>>>(P.prep);
     else k_wgrad_prep<ISO_F32><<<grid, 256, 0, s>>>(P.prep);
     if (P.layers.tiles > 0) {
-      if (dt_grad == ISO_BF16) accumulate ? launch<ISO_BF16, true>(P.layers, s) : launch<ISO_BF16, false>(P.layers, s);
-      else accumulate ? launch<ISO_F32, true>(P.layers, s) : launch<ISO_F32, false>(P.layers, s);
+      if (dt_grad == ISO_BF16) accumulate ? launch<ISO_BF16, true>(P, s) : launch<ISO_BF16, false>(P, s);
+      else accumulate ? launch<ISO_F32, true>(P, s) : launch<ISO_F32, false>(P, s);
     }
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
