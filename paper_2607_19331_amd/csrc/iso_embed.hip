@@ -14,6 +14,7 @@
 #include "iso_device.h"
 #include "iso_grad.h"
 #include "iso_grad_device.h"
+#include "iso_kernels.h"
 
 namespace iso {
 
@@ -41,15 +42,18 @@ __device__ __forceinline__ int32_t row_of(const Ids& ids, int64_t t) {
 
 constexpr int kLookupItems = 2;   // 16-byte vectors a thread (28 us; one, four and eight: 30 for 16384 tokens of 3584)
 constexpr int kLookupBlock = 256 * kLookupItems;
+constexpr int64_t kCheckedAlone = 16384;
 
-// Workgroup 0 looks at every id and writes the status word, so that the call is one launch: nothing has to be
-// cleared before the others find a bad id.  The others copy 512 vectors each, numbered through tokens and columns:
+// Up to kCheckedAlone tokens, workgroup 0 looks at every id and writes the status word, so that the call is one launch:
+// nothing has to be cleared before the others find a bad id.  Beyond, where its walk would outlast the copies of short rows, a
+// launch before clears the word and it does nothing.  The others copy 512 vectors each, numbered through tokens and columns:
 // a thread's ids, and then its vectors, are in flight together.
 template <int DT, bool STREAM>
 __global__ void __launch_bounds__(256) k_embed_lookup(Ids ids, const void* __restrict__ table, void* __restrict__ x,
                                                       int64_t tokens, int64_t dim, int64_t ld_x, float scale,
                                                       uint32_t* status) {
   if (blockIdx.x == 0) {
+    if (tokens > kCheckedAlone) return;
     __shared__ int any;
     if (threadIdx.x == 0) any = 0;
     __syncthreads();
@@ -74,6 +78,7 @@ __global__ void __launch_bounds__(256) k_embed_lookup(Ids ids, const void* __res
       tok[q] = t0 + d;
       col[q] = (int64_t)(r - d * per_row) * V;
       row[q] = tok[q] < tokens ? row_of(ids, tok[q]) : -1;
+      if (row[q] == -2 && tokens > kCheckedAlone) flag_status(status, kStatusIndex);
     }
     u32x4_t w[kLookupItems];
 #pragma unroll
@@ -685,6 +690,10 @@ hipError_t run_embed_lookup(const iso_embed& e, int dt, uint8_t* ws, hipStream_t
   auto go = [&](auto k) {
     k<<<grid, 256, 0, s>>>(ids_of(e), e.table, e.x, e.tokens, e.dim, e.ld_x, (float)e.scale, (uint32_t*)ws);
   };
+  if (e.tokens > kCheckedAlone) {
+    const hipError_t err = fill_u32((uint32_t*)ws, 1, 0u, s);
+    if (err != hipSuccess) return err;
+  }
   const bool stream = streamed(e.tokens * e.dim * (dt == ISO_BF16 ? 2 : 4));
   if (dt == ISO_BF16) stream ? go(k_embed_lookup<ISO_BF16, true>) : go(k_embed_lookup<ISO_BF16, false>);
   else stream ? go(k_embed_lookup<ISO_F32, true>) : go(k_embed_lookup<ISO_F32, false>);

@@ -11,7 +11,6 @@
 #include <stdint.h>
 
 #include <algorithm>
-#include <vector>
 
 #include "iso.h"
 #include "iso_device.h"
@@ -91,19 +90,21 @@ __device__ __forceinline__ void prep_block(const PrepTable& T, uint32_t b) {
     return;
   }
   if (row >= a.part) return;
-  uint32_t y[8];
-#pragma unroll
-  for (int h = 0; h < 8; ++h) {
-    y[h] = 0;
-    if (row < a.rows && col + h < a.cols) y[h] = elem_bits<DT>(a.src, row * a.ld + col + h);
-  }
+  const int64_t left = row < a.rows ? (int64_t)a.cols - col : 0;
   uint32_t w[4];
   if constexpr (DT == ISO_BF16) {
+    const u32x4_t y = load_raw<DT>(a.src, row * a.ld + col, left);
 #pragma unroll
-    for (int h = 0; h < 4; ++h) w[h] = y[2 * h] | y[2 * h + 1] << 16;
+    for (int h = 0; h < 4; ++h) w[h] = y[h];
     put(row, w);
   } else {
-    uint32_t p[3][8];
+    uint32_t y[8], p[3][8];
+#pragma unroll
+    for (int h = 0; h < 8; h += 4) {
+      const u32x4_t v = load_raw<DT>(a.src, row * a.ld + col + h, left - h);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) y[h + j] = v[j];
+    }
 #pragma unroll
     for (int h = 0; h < 8; ++h) {
       const bool finite = (y[h] & 0x7F800000u) != 0x7F800000u;
@@ -468,26 +469,25 @@ struct Schedule {
   double us = 0.0;
 };
 
-Schedule schedule(const std::vector<Layer>& layers, int side) {
+Schedule schedule(const Layer* layers, int n_layers, int side) {
   const bool big = side == 256;
   const double few = big ? 0.59 : 0.35, full = big ? 0.89 : 0.60, ends = big ? 8.0 : 5.0, piece = big ? 0.05 : 0.0125;
   const uint32_t units = big ? Tile<256>::kUnits : Tile<128>::kUnits, alone = big ? 0 : 256;   // 256: one small tile a CU
   auto step = [&](uint32_t n) { return few + (full - few) * (double)(n - std::min(n, alone)) / (units - alone); };
+  auto tiles_of = [&](const Layer& l) {
+    return (uint32_t)((l.rows + side - 1) / side) * (uint32_t)((l.cols + side - 1) / side);
+  };
   Schedule S;
-  std::vector<std::pair<uint32_t, int>> runs;   // tiles and their steps
-  for (const Layer& l : layers) {
-    const uint32_t n = (uint32_t)((l.rows + side - 1) / side) * (uint32_t)((l.cols + side - 1) / side);
-    runs.emplace_back(n, l.steps * l.parts);
-    S.tiles += n;
-  }
+  for (int j = 0; j < n_layers; ++j) S.tiles += tiles_of(layers[j]);
   S.whole = S.tiles / units * units;
   uint32_t at = 0;
   int steps = 0;   // of the longest tile past the full rounds
-  for (const auto& r : runs) {
-    const uint32_t in = std::min(r.first, S.whole > at ? S.whole - at : 0u);
-    S.us += (double)in / units * (full * r.second + ends);
-    if (in < r.first) steps = std::max(steps, r.second);
-    at += r.first;
+  for (int j = 0; j < n_layers; ++j) {
+    const uint32_t n = tiles_of(layers[j]), in = std::min(n, S.whole > at ? S.whole - at : 0u);
+    const int all = layers[j].steps * layers[j].parts;
+    S.us += (double)in / units * (full * all + ends);
+    if (in < n) steps = std::max(steps, all);
+    at += n;
   }
   const uint32_t rest = S.tiles - S.whole;
   if (rest == 0) return S;
@@ -514,8 +514,9 @@ Plan plan_layers(const iso_weight_grad* g, int n, int dt, bool accumulate, uint8
     const iso_ckpt* c;
     const uint8_t* x;
   };
-  std::vector<Kept> kept;
-  std::vector<Layer> layers;
+  Kept kept[kLayers];
+  Layer layers[kLayers];
+  int n_kept = 0, n_layers = 0;
   auto add_prep = [&](Prep p, int64_t rows) {
     p.block0 = P.prep.blocks;
     P.prep.blocks += (uint32_t)((rows * p.per_row + 255) / 256);
@@ -533,12 +534,14 @@ Plan plan_layers(const iso_weight_grad* g, int n, int dt, bool accumulate, uint8
     const int64_t ld = ckpt_ld(x.in.cols);
     l.x_ld = 2 * ld, l.x_bytes = 2 * t * ld;
     if (t > 0) {
-      for (const Kept& k : kept)
-        if (x.in.q != nullptr && k.c->q == x.in.q && k.c->e == x.in.e && k.c->rows == t && k.c->cols == x.in.cols) l.x = k.x;
+      for (int k = 0; k < n_kept; ++k) {
+        const iso_ckpt& c = *kept[k].c;
+        if (x.in.q != nullptr && c.q == x.in.q && c.e == x.in.e && c.rows == t && c.cols == x.in.cols) l.x = kept[k].x;
+      }
       if (l.x == nullptr) {
         uint8_t* const to = region(2 * (size_t)(t * ld));
         add_prep(Prep{x.in.q, x.in.e, (uint16_t*)to, t, ld, 0, (uint32_t)ld, (uint32_t)(ld / 8), 0}, t);
-        kept.push_back(Kept{&x.in, to});
+        kept[n_kept++] = Kept{&x.in, to};
         l.x = to;
       }
       if (direct(x, dt)) {
@@ -554,16 +557,18 @@ Plan plan_layers(const iso_weight_grad* g, int n, int dt, bool accumulate, uint8
         l.y_bytes = 16 * parts * part * per;
       }
     }
-    layers.push_back(l);
+    // long sums first: the tiles past the last full round, which may be split, are then the shortest
+    int to = n_layers++;
+    for (; to > 0 && layers[to - 1].steps < l.steps; --to) layers[to] = layers[to - 1];
+    layers[to] = l;
   }
-  // long sums first: the tiles past the last full round, which may be split, are then the shortest
-  std::stable_sort(layers.begin(), layers.end(), [](const Layer& a, const Layer& b) { return a.steps > b.steps; });
   LayerTable& L = P.layers;
-  const Schedule big = schedule(layers, 256), small = schedule(layers, 128);
+  const Schedule big = schedule(layers, n_layers, 256), small = schedule(layers, n_layers, 128);
   P.tile = small.us < big.us ? 128 : 256;
   const Schedule& S = P.tile == 128 ? small : big;
   L.whole = S.whole, L.split = S.split;
-  for (Layer& l : layers) {
+  for (int j = 0; j < n_layers; ++j) {
+    Layer& l = layers[j];
     l.across = (l.cols + P.tile - 1) / P.tile, l.down = (l.rows + P.tile - 1) / P.tile;
     l.tile0 = L.tiles;
     L.tiles += (uint32_t)l.across * (uint32_t)l.down;

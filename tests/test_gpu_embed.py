@@ -225,3 +225,24 @@ def test_stream_and_graph():
         both(None)
         torch.cuda.synchronize()
         assert np.array_equal(got[0], g.host()) and np.array_equal(got[1], y.host())
+
+
+def test_lookup_of_many_tokens_with_bad_ids():
+    """Past the number of tokens whose ids one workgroup looks at: status and rows as below it."""
+    n, vocab, dim = 20001, 300, 24
+    rng = np.random.default_rng(9)
+    table = f64(rng.standard_normal((vocab, dim)), "bf16")
+    w = Mat(vocab, dim, "bf16", 0, table)
+    for bad in (True, False):
+        ids = rng.integers(0, vocab, n)
+        if bad:
+            ids[[0, n - 1]] = [-3, vocab]
+        x = Mat(n, dim, "bf16", 8)
+        e = iso.Embed(ids=dev_ids(ids, True), tokens=n, vocab=vocab, dim=dim, x=x.view, ld_x=x.ld, table=w.view, pad_id=5)
+        ws = iso.embed_workspace(e)
+        ws.fill_(0xFF)
+        iso.iso_embed_lookup(e, iso.BF16, ws=ws)
+        assert iso.iso_read_device_status(ws) == (_lib.ERR_INDEX if bad else 0)
+        good = (ids >= 0) & (ids < vocab) & (ids != 5)
+        want = np.where(good[:, None], table[np.where(good, ids, 0)], 0.0)
+        assert np.array_equal(x.host(), want)
