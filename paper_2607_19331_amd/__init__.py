@@ -252,11 +252,17 @@ def _embed(e: Embed):
                          e.scale, _ptr(e.table), _ptr(e.x), e.dim if e.ld_x is None else e.ld_x, _ptr(e.grad))
 
 
+_ID_TYPES = {}
+
+
 def _id_type(ids):
-    size = {"torch.int32": _lib.I32, "torch.int64": _lib.I64}.get(str(getattr(ids, "dtype", None)))
-    if size is None:
+    if not _ID_TYPES:
+        import torch
+        _ID_TYPES.update({torch.int32: _lib.I32, torch.int64: _lib.I64})
+    kind = _ID_TYPES.get(getattr(ids, "dtype", None))
+    if kind is None:
         raise TypeError("ids are an int32 or int64 tensor (or give id_type)")
-    return size
+    return kind
 
 
 def _bytes(n, device):

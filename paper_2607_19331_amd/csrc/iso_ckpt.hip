@@ -7,7 +7,9 @@
 // Why int8 and not an 8-bit float with the same exponents: three bits of significand leave 2^-4 of each value, against
 // at most 2^-7 of the group's largest here; activations of one token in 32 neighbouring channels are of one order.
 //
-// All three are bound by the bytes: each reads its inputs and writes its outputs once.  A lane holds eight neighbouring
+// All three are bound by the bytes: each reads its inputs and writes its outputs once (4096 tokens of a 7B layer's activations,
+// 277e6 values in bf16: packed in 133 to 145 us, 5.8 to 6.3 TB/s, unpacked in 143 to 159; the gate's gradients of 8192 x 18944 in
+// 205 us, 6.1 TB/s).  A lane holds eight neighbouring
 // columns (16 bytes of bf16, 8 bytes of q), four lanes a group; q and e are written in their own order, contiguously.
 // Tables of tensors go to the kernel as an argument, up to 16 a launch, so a call copies nothing from the host.
 #include <hip/hip_runtime.h>
@@ -26,7 +28,7 @@ namespace {
 
 constexpr int kTable = 16;     // tensors a launch
 // Groups of eight columns a thread: 4096 tokens of a 7B layer's activations there and back take 327, 298 and 309 us with
-// one, two and four, the gate's gradients of 8192 x 18944 213, 222 and 229 us.
+// one, two and four (outputs kept in the caches), the gate's gradients of 8192 x 18944 213, 222 and 229 us.
 constexpr int kItems = 2;
 constexpr int kGateItems = 1;
 
