@@ -482,13 +482,14 @@ typedef enum iso_id_type { ISO_I32 = 0, ISO_I64 = 1 } iso_id_type;
 #define ISO_NO_PAD INT64_MIN
 
 #define ISO_EMBED_MAX_VOCAB (1 << 20)
+#define ISO_EMBED_MAX_DIM (1 << 18)
 
 /* An embedding and the tokens of one pass through it.  Which pointers are read depends on the call. */
 typedef struct iso_embed {
   const void* ids;       /* tokens ids, of id_type                                                   */
   int32_t id_type;       /* an iso_id_type                                                           */
   int64_t tokens;        /* 0 <= tokens < 2^31                                                       */
-  int64_t vocab, dim;    /* the table is vocab x dim; vocab <= ISO_EMBED_MAX_VOCAB                   */
+  int64_t vocab, dim;    /* the table is vocab x dim, up to ISO_EMBED_MAX_VOCAB x ISO_EMBED_MAX_DIM  */
   int64_t pad_id;        /* tokens with this id are padding (it need not lie in the table)           */
   double scale;          /* finite                                                                   */
   const void* table;     /* lookup: W, vocab x dim                                                   */

@@ -612,7 +612,7 @@ template <int DT, int DTG, bool ADD>
 hipError_t grad_few(const iso_embed& e, const Rows& a, uint8_t* ws, hipStream_t s) {
   // 512 buckets, or as many as the vocabulary takes to leave at most 512 ids in each
   const Buckets B = buckets_of(e.vocab, std::max(std::min(9, log2_up(e.vocab)), log2_up((e.vocab + kFewWidth - 1) / kFewWidth)));
-  const int64_t blocks = (e.dim + 64 * kVec<DT> - 1) / (64 * kVec<DT>);
+  const int64_t blocks = (e.dim + 64 * kVec<DT> - 1) / (64 * kVec<DT>);   // at most 1024: 2^21 workgroups, 2^30 threads
   const bool fill = !ADD && e.vocab * e.dim * (DTG == ISO_BF16 ? 2 : 4) >= kOwnFill;
   if (fill) {
     const Fill f = zeros_of(e, DTG);

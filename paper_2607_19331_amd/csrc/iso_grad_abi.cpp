@@ -37,7 +37,7 @@ iso_status check_embed_sizes(const iso_embed* e) {
   if (e == nullptr) return ISO_ERR_INVALID_ARG;
   if (e->id_type != ISO_I32 && e->id_type != ISO_I64) return ISO_ERR_INVALID_ARG;
   if (e->tokens < 0 || e->vocab < 1 || e->dim < 1) return ISO_ERR_INVALID_ARG;
-  if (e->tokens >= (1ll << 31) || e->vocab > ISO_EMBED_MAX_VOCAB || e->dim > kMaxDim) return ISO_ERR_UNSUPPORTED;
+  if (e->tokens >= (1ll << 31) || e->vocab > ISO_EMBED_MAX_VOCAB || e->dim > ISO_EMBED_MAX_DIM) return ISO_ERR_UNSUPPORTED;
   return ISO_OK;
 }
 

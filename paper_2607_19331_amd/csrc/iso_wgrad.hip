@@ -505,9 +505,9 @@ Plan plan_layers(const iso_weight_grad* g, int n, int dt, bool accumulate, uint8
   Plan P;
   size_t at = kStatusBytes;
   auto region = [&](size_t bytes) {
-    const size_t o = at;
+    const uintptr_t o = (uintptr_t)ws + at;   // ws is null where only the size is asked for
     at = align_up(at + bytes, 256);
-    return ws + o;
+    return (uint8_t*)o;
   };
   const int parts = dt == ISO_F32 ? 3 : 1;
   struct Kept {

@@ -46,7 +46,7 @@ def test_embed_refusals(call):
     assert call(embed(), ws_bytes=255) == _lib.ERR_WORKSPACE
     assert call(embed(tokens=1 << 31)) == _lib.ERR_UNSUPPORTED
     assert call(embed(vocab=_lib.EMBED_MAX_VOCAB + 1)) == _lib.ERR_UNSUPPORTED
-    assert call(embed(dim=(1 << 24) + 1)) == _lib.ERR_UNSUPPORTED
+    assert call(embed(dim=(1 << 18) + 1)) == _lib.ERR_UNSUPPORTED
     assert call(embed(tokens=1 << 30, ld_x=1 << 30)) == _lib.ERR_UNSUPPORTED
     # an id pointer of its own size is enough; the workspace is checked last
     assert call(embed(ids=FAKE + 4, id_type=_lib.I32), ws_bytes=16) == _lib.ERR_WORKSPACE
