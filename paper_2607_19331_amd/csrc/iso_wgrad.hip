@@ -6,7 +6,8 @@
 //
 // A call is up to three launches per 16 layers.  k_wgrad_prep brings operands into the form that the product reads,
 // bf16 rows aligned to 16 bytes: X always (once per checkpoint, however many layers share it), dY where it is fp32 or
-// its stride is odd.  k_wgrad forms the tiles of all layers' gradients.  k_wgrad_join adds up tiles whose tokens were split.
+// its rows are not aligned.  k_wgrad forms the tiles of all layers' gradients.  k_wgrad_join adds up tiles whose
+// tokens were split.
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
