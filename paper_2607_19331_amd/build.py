@@ -10,10 +10,12 @@ BUILD = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "libiso.so")
 
 SOURCES = ["iso_abi.cpp", "iso_select.hip", "iso_merge.hip", "iso_fused.hip", "iso_spectral.hip", "iso_tsv.hip",
-           "iso_noalloc.hip", "iso_ortho.hip", "iso_grad_abi.cpp", "iso_embed.hip", "iso_ckpt.hip", "iso_wgrad.hip"]
+           "iso_noalloc.hip", "iso_ortho.hip", "iso_grad_abi.cpp", "iso_grad_plan.cpp", "iso_embed.hip", "iso_ckpt.hip",
+           "iso_wgrad.hip"]
 
-# the C ABI layers: argument checks and host-side planning (what the sanitized build instruments)
-HOST_SOURCES = ["iso_abi.cpp", "iso_grad_abi.cpp"]
+# the C ABI layers and the gradient operators' plans: argument checks and host-side planning (what the sanitized build
+# instruments)
+HOST_SOURCES = ["iso_abi.cpp", "iso_grad_abi.cpp", "iso_grad_plan.cpp"]
 
 HIPFLAGS = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC",

@@ -26,7 +26,6 @@ namespace iso {
 
 namespace {
 
-constexpr int kTable = 16;     // tensors a launch
 // Groups of eight columns a thread: 4096 tokens of a 7B layer's activations there and back take 327, 298 and 309 us with
 // one, two and four (outputs kept in the caches), the gate's gradients of 8192 x 18944 213, 222 and 229 us.
 constexpr int kItems = 2;
@@ -221,37 +220,19 @@ GateArg arg_of(const iso_gate_grad& g) {
   return GateArg{g.gate.q, g.up.q,    g.gate.e, g.up.e, g.dh, g.dgate, g.dup, g.gate.rows, g.ld, (uint32_t)g.gate.cols,
                  (uint32_t)(ckpt_ld(g.gate.cols) / 8)};
 }
-// Queues a table, up to 16 tensors and 2^22 workgroups a launch (a larger tensor goes alone); `size`: bytes written for a
-// group of eight columns.
+
+// Queues a table.
 template <class Table, class Entry, class Launch>
-hipError_t for_tables(const Entry* c, int n, int items, int size, Launch launch) {
-  Table T;
-  int64_t bytes = 0;
-  T.n = 0;
-  T.block0[0] = 0;
-  auto flush = [&] {
-    if (T.n > 0) launch(T, T.block0[T.n], streamed(bytes));
-    T.n = 0;
-    bytes = 0;
-  };
-  for (int j = 0; j < n; ++j) {
-    const auto a = arg_of(c[j]);
-    if (a.rows == 0 || a.cols == 0) continue;
-    const int64_t blocks = (a.rows * a.per_row + 256 * items - 1) / (256 * items);
-    if (T.n == kTable || (T.n > 0 && T.block0[T.n] + blocks > (1 << 22))) flush();
-    T.t[T.n] = a;
-    T.block0[T.n + 1] = T.block0[T.n] + (uint32_t)blocks;
-    bytes += a.rows * a.per_row * size;
-    ++T.n;
-  }
-  flush();
+hipError_t run_tables(const Entry* c, int n, int items, int size, Launch launch) {
+  for_tables<Table>(c, n, items, size, [](const Entry& x) { return arg_of(x); },
+                    [&](const Table& T, unsigned grid, int64_t bytes) { launch(T, grid, streamed(bytes)); });
   return hipGetLastError();
 }
 
 }  // namespace
 
 hipError_t run_ckpt_pack(const iso_ckpt* c, int n, int dt, hipStream_t s) {
-  return for_tables<CkptTable>(c, n, kItems, 8, [&](const CkptTable& T, unsigned grid, bool stream) {
+  return run_tables<CkptTable>(c, n, kItems, 8, [&](const CkptTable& T, unsigned grid, bool stream) {
     auto go = [&](auto k) { k<<<grid, 256, 0, s>>>(T); };
     if (dt == ISO_BF16) stream ? go(k_ckpt_pack<ISO_BF16, true>) : go(k_ckpt_pack<ISO_BF16, false>);
     else stream ? go(k_ckpt_pack<ISO_F32, true>) : go(k_ckpt_pack<ISO_F32, false>);
@@ -259,7 +240,7 @@ hipError_t run_ckpt_pack(const iso_ckpt* c, int n, int dt, hipStream_t s) {
 }
 
 hipError_t run_ckpt_unpack(const iso_ckpt* c, int n, int dt, hipStream_t s) {
-  return for_tables<CkptTable>(c, n, kItems, dt == ISO_BF16 ? 16 : 32, [&](const CkptTable& T, unsigned grid, bool stream) {
+  return run_tables<CkptTable>(c, n, kItems, dt == ISO_BF16 ? 16 : 32, [&](const CkptTable& T, unsigned grid, bool stream) {
     auto go = [&](auto k) { k<<<grid, 256, 0, s>>>(T); };
     if (dt == ISO_BF16) stream ? go(k_ckpt_unpack<ISO_BF16, true>) : go(k_ckpt_unpack<ISO_BF16, false>);
     else stream ? go(k_ckpt_unpack<ISO_F32, true>) : go(k_ckpt_unpack<ISO_F32, false>);
@@ -267,7 +248,7 @@ hipError_t run_ckpt_unpack(const iso_ckpt* c, int n, int dt, hipStream_t s) {
 }
 
 hipError_t run_gate_grad(const iso_gate_grad* g, int n, int dt, hipStream_t s) {
-  return for_tables<GateTable>(g, n, kGateItems, dt == ISO_BF16 ? 32 : 64, [&](const GateTable& T, unsigned grid, bool stream) {
+  return run_tables<GateTable>(g, n, kGateItems, dt == ISO_BF16 ? 32 : 64, [&](const GateTable& T, unsigned grid, bool stream) {
     auto go = [&](auto k) { k<<<grid, 256, 0, s>>>(T); };
     if (dt == ISO_BF16) stream ? go(k_gate_grad<ISO_BF16, true>) : go(k_gate_grad<ISO_BF16, false>);
     else stream ? go(k_gate_grad<ISO_F32, true>) : go(k_gate_grad<ISO_F32, false>);

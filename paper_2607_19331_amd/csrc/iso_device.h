@@ -5,18 +5,9 @@
 #include <stdint.h>
 
 #include "iso.h"
+#include "iso_workspace.h"
 
 namespace iso {
-
-// ---- workspace layout ----------------------------------------------------------------------------
-// [0, 256)            status block (u32 flags)
-// [256, ...)          per-call tables and scratch, each region 256-byte aligned
-constexpr size_t kStatusBytes = 256;
-constexpr uint32_t kStatusNonFinite = 1u;
-constexpr uint32_t kStatusInternal = 2u;   // a kernel found counts that cannot occur; results invalid
-constexpr uint32_t kStatusIndex = 4u;      // a token id outside the vocabulary
-
-inline size_t align_up(size_t x, size_t a) { return (x + a - 1) / a * a; }
 
 // Global-memory view of a generic pointer (one that points into device memory).  A pointer read
 // from a job or problem table is generic, and accesses through it compile to flat instructions,

@@ -100,9 +100,6 @@ __global__ void __launch_bounds__(256) k_embed_lookup(Ids ids, const void* __res
 
 // ---- gradient: shared pieces ---------------------------------------------------------------------------------------
 
-// The tokens of an id are added in runs of kRun, whose sums are then added in order.
-constexpr int kRun = 32;
-
 // Lanes of the wave whose key equals this lane's (of those with `on`), by one ballot per key bit.
 __device__ __forceinline__ uint64_t peers(uint32_t key, int bits, bool on) {
   uint64_t m = __ballot(on);
@@ -215,9 +212,6 @@ __device__ __forceinline__ void fill_zeros(const Fill& f, uint32_t block, uint32
 
 // ---- gradient: few tokens, one launch ------------------------------------------------------------------------------
 
-// Up to 4096 tokens of a 151936 x 1536 table are added in 24 us this way and in 38 by the launches below (2048: 18 and 35);
-// 4096 tokens of one id, the worst case, in 98 and 44.
-constexpr int kFewTokens = 4096;
 constexpr int kFewWaves = 8;
 constexpr int kFewWidth = 512;   // local ids of a bucket, at most
 
@@ -346,17 +340,11 @@ __global__ void __launch_bounds__(256) k_embed_fill(Fill f) { fill_zeros(f, bloc
 // latencies 20, the reads of dX and the rows that have tokens the rest; their bytes alone would take 209.  Spreading the zeros
 // over the first four launches, under whose latencies they would hide, gained nothing (270 to 280 us).
 
-constexpr int kMaxTiles = 64;
-constexpr int kMinTile = 1024;
-constexpr int kMaxBuckets = 512;
 constexpr int kMaxWidth = ISO_EMBED_MAX_VOCAB / kMaxBuckets;
 
 // Distinct ids and the runs of frequent ones, appended bucket by bucket in any order (each is worked on by itself).  Ids of
 // 1/16 of the buckets share a counter, on a line of its own, and the part of the list that their tokens take in sorted order:
 // with one counter for all, 512 additions to one address took 7 of the sort's 12 us.
-constexpr int kGroups = 16;
-constexpr int kLine = 32;   // words between counters
-
 struct Lists {
   uint32_t* n;               // runs, frequent ids; from kLine on the groups' ids, kLine apart
   uint4* ids;                // id, first sorted position, tokens (at most kRun)
@@ -609,12 +597,6 @@ __global__ void __launch_bounds__(256) k_embed_rows(const uint32_t* __restrict__
 
 // ---- host ----------------------------------------------------------------------------------------------------------
 
-int log2_up(int64_t n) {
-  int b = 0;
-  while ((1ll << b) < n) ++b;
-  return b;
-}
-
 Buckets buckets_of(int64_t vocab, int log2) {
   Buckets B;
   B.log2 = log2;
@@ -685,32 +667,6 @@ hipError_t grad(const iso_embed& e, uint8_t* ws, hipStream_t s) {
 }
 
 }  // namespace
-
-EmbedPlan embed_plan(int64_t tokens, int64_t vocab, int64_t dim) {
-  EmbedPlan P;
-  P.total = kStatusBytes;
-  if (tokens <= kFewTokens) return P;
-  const size_t buckets = (size_t)1 << std::min(9, log2_up(vocab));
-  P.tile = std::max<int64_t>(kMinTile, (tokens + kMaxTiles - 1) / kMaxTiles);
-  P.tiles = (tokens + P.tile - 1) / P.tile;
-  P.most_runs = tokens / (kRun / 2) + 1;   // an id with m > kRun tokens has ceil(m / kRun) <= m / (kRun / 2)
-  auto region = [&](size_t bytes) {
-    const size_t o = P.total;
-    P.total = align_up(P.total + bytes, 256);
-    return o;
-  };
-  P.bad = region(sizeof(uint32_t) * P.tiles);
-  P.hist = region(sizeof(uint32_t) * P.tiles * buckets);
-  P.bucket0 = region(sizeof(uint32_t) * (buckets + 1));
-  P.pairs = region(sizeof(uint2) * tokens);
-  P.perm = region(sizeof(uint32_t) * tokens);
-  P.listed = region(sizeof(uint32_t) * kLine * (kGroups + 1));
-  P.ids = region(sizeof(uint4) * tokens);
-  P.runs = region(sizeof(uint2) * P.most_runs);
-  P.many = region(sizeof(uint4) * (tokens / kRun + 1));
-  P.part = region(sizeof(float) * P.most_runs * dim);
-  return P;
-}
 
 hipError_t run_embed_lookup(const iso_embed& e, int dt, uint8_t* ws, hipStream_t s) {
   const int v = dt == ISO_BF16 ? kVec<ISO_BF16> : kVec<ISO_F32>;

@@ -1,0 +1,129 @@
+// Host-side planning of the gradient operators: workspace regions, the tables that the launches take, and how work is shared
+// out.  Plain C++ (no HIP), so that it is compiled by itself in the sanitized build and in the CPU tests.
+#pragma once
+
+#include <stddef.h>
+#include <stdint.h>
+
+#include "iso.h"
+#include "iso_workspace.h"
+
+namespace iso {
+
+// ---- embedding gradient --------------------------------------------------------------------------------------------
+
+// The tokens of an id are added in runs of kRun, whose sums are then added in order.
+constexpr int kRun = 32;
+
+// Up to 4096 tokens of a 151936 x 1536 table are added in 24 us in one launch and in 38 by the sorted launches (2048: 18 and
+// 35); 4096 tokens of one id, the worst case, in 98 and 44.
+constexpr int kFewTokens = 4096;
+
+constexpr int kMaxTiles = 64;
+constexpr int kMinTile = 1024;
+constexpr int kMaxBuckets = 512;
+
+// Counters of the lists of distinct ids: groups of buckets, and words between their counters.
+constexpr int kGroups = 16;
+constexpr int kLine = 32;
+
+// Workspace regions of the embedding's gradient (many tokens; few take the status block alone).
+struct EmbedPlan {
+  int64_t tiles = 0, tile = 0;     // tokens are counted and scattered by tiles of `tile`
+  int64_t most_runs = 0;           // partial sums of ids with many tokens
+  size_t bad = 0, hist = 0, bucket0 = 0, pairs = 0, perm = 0, listed = 0, ids = 0, runs = 0, many = 0, part = 0, total = 0;
+};
+
+int log2_up(int64_t n);
+EmbedPlan embed_plan(int64_t tokens, int64_t vocab, int64_t dim);
+
+// ---- checkpoints ---------------------------------------------------------------------------------------------------
+
+inline int64_t ckpt_ld(int64_t cols) { return (cols + ISO_CKPT_GROUP - 1) / ISO_CKPT_GROUP * ISO_CKPT_GROUP; }
+
+constexpr int kTable = 16;     // tensors a launch
+
+// Cuts n entries, in the form that the kernel takes (`arg`), into tables of up to 16 tensors and 2^22 workgroups (a larger
+// tensor goes alone), and hands each to `launch`, with its workgroups and the bytes that they write.  `items`: groups of eight
+// columns a thread, 256 threads a workgroup; `size`: bytes written for such a group.
+template <class Table, class Entry, class Arg, class Launch>
+void for_tables(const Entry* c, int n, int items, int size, Arg arg, Launch launch) {
+  Table T;
+  int64_t bytes = 0;
+  T.n = 0;
+  T.block0[0] = 0;
+  auto flush = [&] {
+    if (T.n > 0) launch(T, T.block0[T.n], bytes);
+    T.n = 0;
+    bytes = 0;
+  };
+  for (int j = 0; j < n; ++j) {
+    const auto a = arg(c[j]);
+    if (a.rows == 0 || a.cols == 0) continue;
+    const int64_t blocks = (a.rows * a.per_row + 256 * items - 1) / (256 * items);
+    if (T.n == kTable || (T.n > 0 && T.block0[T.n] + blocks > (1 << 22))) flush();
+    T.t[T.n] = a;
+    T.block0[T.n + 1] = T.block0[T.n] + (uint32_t)blocks;
+    bytes += a.rows * a.per_row * size;
+    ++T.n;
+  }
+  flush();
+}
+
+// ---- weight gradients ----------------------------------------------------------------------------------------------
+
+constexpr int kLayers = 16;               // layers a launch
+constexpr int kStep = 32;                 // tokens of a step
+constexpr int64_t kMaxStride = 1 << 25;   // 32 rows of it stay within 32-bit offsets
+
+struct Prep {
+  const void* src;        // q, or dY
+  const uint8_t* e;       // exponents of q; null for dY
+  uint16_t* dst;
+  int64_t rows, ld;       // rows and row stride of the source
+  int64_t part;           // rows of a part of the destination (rows rounded up to whole steps); 0 for X
+  uint32_t cols, per_row; // columns of the source; groups of eight in a destination row
+  uint32_t block0;
+};
+
+struct PrepTable {
+  Prep p[2 * kLayers];
+  int n;
+  uint32_t blocks;
+  uint32_t* status;
+};
+
+struct Layer {
+  const uint8_t* y;            // bf16 dY and X, token rows
+  const uint8_t* x;
+  void* g;
+  int64_t y_ld, x_ld;          // row strides, bytes
+  int64_t y_bytes, x_bytes;    // bytes from the first element to past the last (dY: of all its parts)
+  int32_t rows, cols;          // of G
+  int32_t across, down;        // tiles of a tile row, and tile rows
+  int32_t steps, parts;        // steps of a part of dY
+  uint32_t tile0;
+};
+
+struct LayerTable {
+  Layer l[kLayers];
+  int n;
+  uint32_t tiles;     // of all layers
+  uint32_t whole;     // tiles one workgroup does alone; the others' tokens are split `split` ways
+  uint32_t split;
+  float* part;        // their partial sums, a tile's size a piece, (tile, piece) in order
+};
+
+// What up to 16 layers take: the tables of their launches, with workspace offsets in place of pointers until bound.
+struct WeightGradPlan {
+  PrepTable prep{};
+  LayerTable layers{};
+  int tile = 256;
+  size_t total = 0;
+};
+
+// `ws` may be null where only sizes matter.
+WeightGradPlan plan_weight_grad(const iso_weight_grad* g, int n, int dt, bool accumulate, uint8_t* ws);
+size_t weight_grad_workspace_bytes(const iso_weight_grad* g, int n, int dt);
+
+}  // namespace iso

@@ -22,8 +22,6 @@ namespace iso {
 
 namespace {
 
-constexpr int kLayers = 16;          // layers a launch
-constexpr int kStep = 32;            // tokens of a step
 constexpr int kStages = 4;           // steps in LDS
 
 // A workgroup's tile of G, 256 x 256 or 128 x 128.
@@ -36,28 +34,9 @@ struct Tile {
   static constexpr int kStage = 2 * kPanel;
   static constexpr int kLoads = TILE / 64;                  // 16-byte loads a lane and panel
   static constexpr int kOutBytes = (kQuarter + 4) * 4;      // a row of the result in LDS
-  static constexpr int kUnits = TILE == 256 ? 256 : 512;    // workgroups that run at once: one or two a CU
 };
-constexpr int64_t kMaxStride = 1 << 25;   // 32 rows of it stay within 32-bit offsets
 
 // ---- operand preparation -------------------------------------------------------------------------------------------
-
-struct Prep {
-  const void* src;        // q, or dY
-  const uint8_t* e;       // exponents of q; null for dY
-  uint16_t* dst;
-  int64_t rows, ld;       // rows and row stride of the source
-  int64_t part;           // rows of a part of the destination (rows rounded up to whole steps); 0 for X
-  uint32_t cols, per_row; // columns of the source; groups of eight in a destination row
-  uint32_t block0;
-};
-
-struct PrepTable {
-  Prep p[2 * kLayers];
-  int n;
-  uint32_t blocks;
-  uint32_t* status;
-};
 
 // Eight columns of one row a thread.  X: q 2^k, whose upper 16 bits are the whole value.  dY: its bf16 parts, least
 // first, rows up to a whole step zero (X has none there, and 0 times what lies there may be NaN).
@@ -132,27 +111,6 @@ __global__ void __launch_bounds__(256) k_wgrad_prep(PrepTable T) {
 }
 
 // ---- the product ---------------------------------------------------------------------------------------------------
-
-struct Layer {
-  const uint8_t* y;            // bf16 dY and X, token rows
-  const uint8_t* x;
-  void* g;
-  int64_t y_ld, x_ld;          // row strides, bytes
-  int64_t y_bytes, x_bytes;    // bytes from the first element to past the last (dY: of all its parts)
-  int32_t rows, cols;          // of G
-  int32_t across, down;        // tiles of a tile row, and tile rows
-  int32_t steps, parts;        // steps of a part of dY
-  uint32_t tile0;
-};
-
-struct LayerTable {
-  Layer l[kLayers];
-  int n;
-  uint32_t tiles;     // of all layers
-  uint32_t whole;     // tiles one workgroup does alone; the others' tokens are split `split` ways
-  uint32_t split;
-  float* part;        // their partial sums, a tile's size a piece, (tile, piece) in order
-};
 
 typedef __attribute__((address_space(3))) uint8_t lds_u8;
 typedef short s16x4_t __attribute__((ext_vector_type(4)));
@@ -446,141 +404,6 @@ __global__ void __launch_bounds__(256) k_wgrad_join(LayerTable T) {
 
 // ---- host ----------------------------------------------------------------------------------------------------------
 
-// What up to 16 layers take: the tables of their launches, with workspace offsets in place of pointers until bound.
-struct Plan {
-  PrepTable prep{};
-  LayerTable layers{};
-  int tile = 256;
-  size_t total = 0;
-};
-
-bool direct(const iso_weight_grad& x, int dt) { return dt == ISO_BF16 && x.ld_dy % 8 == 0 && x.ld_dy <= kMaxStride; }
-
-int64_t whole_steps(int64_t tokens) { return (tokens + kStep - 1) / kStep * kStep; }
-
-// How the tiles of a table, of `side` x `side`, are shared out: full rounds of workgroups take whole tiles, those past the
-// last full round are split into the pieces that take the fewest microseconds, by an estimate from measured parts: a step,
-// which takes longer the more workgroups are at work (memory, clock); a workgroup's start and end; for split tiles the second
-// launch, the pieces' writes and reads, and each piece that a thread adds.  The table takes the side whose estimate is less.
-// bf16 in microseconds, 256 x 256 tiles against 128 x 128: 2048 x 2048 of 203 tokens 18.6 and 15.4, of 1024 34 and 22, of 8192 95
-// and 108; four such matrices of 2048 tokens 72 and 88; 512 x 1024 of 512 tokens 19.3 and 15.8.  In one to sixteen pieces
-// (256 x 256) 512 x 1024 of 2048 tokens took 51, 33, 26, 24 and 26, 2048 x 2048 of 203 tokens 19, 25 and 32.
-struct Schedule {
-  uint32_t tiles = 0, whole = 0, split = 1;
-  double us = 0.0;
-};
-
-Schedule schedule(const Layer* layers, int n_layers, int side) {
-  const bool big = side == 256;
-  const double few = big ? 0.59 : 0.35, full = big ? 0.89 : 0.60, ends = big ? 8.0 : 5.0, piece = big ? 0.05 : 0.0125;
-  const uint32_t units = big ? Tile<256>::kUnits : Tile<128>::kUnits, alone = big ? 0 : 256;   // 256: one small tile a CU
-  auto step = [&](uint32_t n) { return few + (full - few) * (double)(n - std::min(n, alone)) / (units - alone); };
-  auto tiles_of = [&](const Layer& l) {
-    return (uint32_t)((l.rows + side - 1) / side) * (uint32_t)((l.cols + side - 1) / side);
-  };
-  Schedule S;
-  for (int j = 0; j < n_layers; ++j) S.tiles += tiles_of(layers[j]);
-  S.whole = S.tiles / units * units;
-  uint32_t at = 0;
-  int steps = 0;   // of the longest tile past the full rounds
-  for (int j = 0; j < n_layers; ++j) {
-    const uint32_t n = tiles_of(layers[j]), in = std::min(n, S.whole > at ? S.whole - at : 0u);
-    const int all = layers[j].steps * layers[j].parts;
-    S.us += (double)in / units * (full * all + ends);
-    if (in < n) steps = std::max(steps, all);
-    at += n;
-  }
-  const uint32_t rest = S.tiles - S.whole;
-  if (rest == 0) return S;
-  double least = step(rest) * steps + ends;
-  for (uint32_t s = 2; s <= units / rest && s <= (uint32_t)steps; ++s) {
-    const double us = step(rest * s) * ((steps + s - 1) / s) + ends + 3.0 + piece * rest * s + 0.15 * s;
-    if (us < least) least = us, S.split = s;
-  }
-  S.us += least;
-  if (S.split == 1) S.whole = S.tiles;
-  return S;
-}
-
-Plan plan_layers(const iso_weight_grad* g, int n, int dt, bool accumulate, uint8_t* ws) {
-  Plan P;
-  size_t at = kStatusBytes;
-  auto region = [&](size_t bytes) {
-    const uintptr_t o = (uintptr_t)ws + at;   // ws is null where only the size is asked for
-    at = align_up(at + bytes, 256);
-    return (uint8_t*)o;
-  };
-  const int parts = dt == ISO_F32 ? 3 : 1;
-  struct Kept {
-    const iso_ckpt* c;
-    const uint8_t* x;
-  };
-  Kept kept[kLayers];
-  Layer layers[kLayers];
-  int n_kept = 0, n_layers = 0;
-  auto add_prep = [&](Prep p, int64_t rows) {
-    p.block0 = P.prep.blocks;
-    P.prep.blocks += (uint32_t)((rows * p.per_row + 255) / 256);
-    P.prep.p[P.prep.n++] = p;
-  };
-  for (int j = 0; j < n; ++j) {
-    const iso_weight_grad& x = g[j];
-    const int64_t t = x.in.rows;
-    if (x.rows == 0 || x.in.cols == 0 || (t == 0 && accumulate)) continue;
-    Layer l{};
-    l.g = x.grad;
-    l.rows = (int32_t)x.rows, l.cols = (int32_t)x.in.cols;
-    l.steps = (int32_t)(whole_steps(t) / kStep);
-    l.parts = parts;
-    const int64_t ld = ckpt_ld(x.in.cols);
-    l.x_ld = 2 * ld, l.x_bytes = 2 * t * ld;
-    if (t > 0) {
-      for (int k = 0; k < n_kept; ++k) {
-        const iso_ckpt& c = *kept[k].c;
-        if (x.in.q != nullptr && c.q == x.in.q && c.e == x.in.e && c.rows == t && c.cols == x.in.cols) l.x = kept[k].x;
-      }
-      if (l.x == nullptr) {
-        uint8_t* const to = region(2 * (size_t)(t * ld));
-        add_prep(Prep{x.in.q, x.in.e, (uint16_t*)to, t, ld, 0, (uint32_t)ld, (uint32_t)(ld / 8), 0}, t);
-        kept[n_kept++] = Kept{&x.in, to};
-        l.x = to;
-      }
-      if (direct(x, dt)) {
-        l.y = (const uint8_t*)x.dy;
-        l.y_ld = 2 * x.ld_dy;
-        l.y_bytes = (int64_t)align_up(2 * (size_t)((t - 1) * x.ld_dy + x.rows), 16);
-      } else {
-        const int64_t per = (x.rows + 7) / 8, part = whole_steps(t);
-        uint8_t* const to = region(2 * (size_t)(parts * part * per * 8));
-        add_prep(Prep{x.dy, nullptr, (uint16_t*)to, t, x.ld_dy, part, (uint32_t)x.rows, (uint32_t)per, 0}, part);
-        l.y = to;
-        l.y_ld = 16 * per;
-        l.y_bytes = 16 * parts * part * per;
-      }
-    }
-    // long sums first: the tiles past the last full round, which may be split, are then the shortest
-    int to = n_layers++;
-    for (; to > 0 && layers[to - 1].steps < l.steps; --to) layers[to] = layers[to - 1];
-    layers[to] = l;
-  }
-  LayerTable& L = P.layers;
-  const Schedule big = schedule(layers, n_layers, 256), small = schedule(layers, n_layers, 128);
-  P.tile = small.us < big.us ? 128 : 256;
-  const Schedule& S = P.tile == 128 ? small : big;
-  L.whole = S.whole, L.split = S.split;
-  for (int j = 0; j < n_layers; ++j) {
-    Layer& l = layers[j];
-    l.across = (l.cols + P.tile - 1) / P.tile, l.down = (l.rows + P.tile - 1) / P.tile;
-    l.tile0 = L.tiles;
-    L.tiles += (uint32_t)l.across * (uint32_t)l.down;
-    L.l[L.n++] = l;
-  }
-  L.part = (float*)region(sizeof(float) * P.tile * P.tile * (size_t)(L.tiles - L.whole) * L.split);
-  P.prep.status = (uint32_t*)ws;
-  P.total = at;
-  return P;
-}
-
 template <int TILE, int DTG, bool ADD>
 void launch_tiles(const LayerTable& L, hipStream_t s) {
   // the result passes through LDS too: no more of it than the stages take
@@ -591,23 +414,15 @@ void launch_tiles(const LayerTable& L, hipStream_t s) {
 }
 
 template <int DTG, bool ADD>
-void launch(const Plan& P, hipStream_t s) {
+void launch(const WeightGradPlan& P, hipStream_t s) {
   P.tile == 128 ? launch_tiles<128, DTG, ADD>(P.layers, s) : launch_tiles<256, DTG, ADD>(P.layers, s);
 }
 
 }  // namespace
 
-size_t weight_grad_workspace_bytes(const iso_weight_grad* g, int n, int dt) {
-  size_t most = kStatusBytes;
-  for (int j = 0; j < n; j += kLayers)
-    for (bool accumulate : {false, true})   // a layer without tokens takes part in the one and not in the other
-      most = std::max(most, plan_layers(g + j, std::min(kLayers, n - j), dt, accumulate, nullptr).total);
-  return most;
-}
-
 hipError_t run_weight_grad(const iso_weight_grad* g, int n, int dt, int dt_grad, bool accumulate, uint8_t* ws, hipStream_t s) {
   for (int j = 0; j < n || j == 0; j += kLayers) {
-    const Plan P = plan_layers(g + j, std::min(kLayers, n - j), dt, accumulate, ws);
+    const WeightGradPlan P = plan_weight_grad(g + j, std::min(kLayers, n - j), dt, accumulate, ws);
     const unsigned grid = std::min(std::max(P.prep.blocks, 1u), 1u << 22);
     if (dt == ISO_BF16) k_wgrad_prep<ISO_BF16><<<grid, 256, 0, s>>>(P.prep);
     else k_wgrad_prep<ISO_F32><<<grid, 256, 0, s>>>(P.prep);
