@@ -591,7 +591,11 @@ typedef struct iso_weight_grad {
   int64_t rows;
 } iso_weight_grad;
 
-/* Bytes of workspace of a table (0 on bad arguments); 256-byte aligned. */
+/*
+ * Bytes of workspace of a table (0 on bad arguments); 256-byte aligned.  They do not fall as tokens grow: a
+ * workspace for the longest batch holds the shorter ones.  Of the pointers only in.q and in.e count, which say
+ * what layers share; null ones are taken as shared by none, the most that any call of these sizes needs.
+ */
 size_t iso_workspace_size_weight_grad(const iso_weight_grad* g, int n, int dt);
 
 iso_status iso_ckpt_weight_grad(const iso_weight_grad* g, int n, int dt, int dt_grad, int accumulate, void* ws,

@@ -55,21 +55,24 @@ struct Schedule {
   double us = 0.0;
 };
 
+uint32_t units_of(int side) { return side == 256 ? 256 : 512; }   // workgroups at once: one or two a CU
+
+uint32_t tiles_of(const Layer& l, int side) {
+  return (uint32_t)((l.rows + side - 1) / side) * (uint32_t)((l.cols + side - 1) / side);
+}
+
 Schedule schedule(const Layer* layers, int n_layers, int side) {
   const bool big = side == 256;
   const double few = big ? 0.59 : 0.35, full = big ? 0.89 : 0.60, ends = big ? 8.0 : 5.0, piece = big ? 0.05 : 0.0125;
-  const uint32_t units = big ? 256 : 512, alone = big ? 0 : 256;   // workgroups at once: one or two a CU
+  const uint32_t units = units_of(side), alone = big ? 0 : 256;
   auto step = [&](uint32_t n) { return few + (full - few) * (double)(n - std::min(n, alone)) / (units - alone); };
-  auto tiles_of = [&](const Layer& l) {
-    return (uint32_t)((l.rows + side - 1) / side) * (uint32_t)((l.cols + side - 1) / side);
-  };
   Schedule S;
-  for (int j = 0; j < n_layers; ++j) S.tiles += tiles_of(layers[j]);
+  for (int j = 0; j < n_layers; ++j) S.tiles += tiles_of(layers[j], side);
   S.whole = S.tiles / units * units;
   uint32_t at = 0;
   int steps = 0;   // of the longest tile past the full rounds
   for (int j = 0; j < n_layers; ++j) {
-    const uint32_t n = tiles_of(layers[j]), in = std::min(n, S.whole > at ? S.whole - at : 0u);
+    const uint32_t n = tiles_of(layers[j], side), in = std::min(n, S.whole > at ? S.whole - at : 0u);
     const int all = layers[j].steps * layers[j].parts;
     S.us += (double)in / units * (full * all + ends);
     if (in < n) steps = std::max(steps, all);
@@ -85,6 +88,23 @@ Schedule schedule(const Layer* layers, int n_layers, int side) {
   S.us += least;
   if (S.split == 1) S.whole = S.tiles;
   return S;
+}
+
+// Bytes that hold the pieces of split tiles by either side: as many as workgroups run at once (64 MiB), fewer only where the
+// tiles have no more steps in all.  The pieces that a schedule makes fall here and there as tokens grow; this does not, so that a
+// workspace for the longest batch holds the shorter ones.
+size_t most_pieces(const Layer* layers, int n_layers) {
+  size_t most = 0;
+  for (int side : {128, 256}) {
+    uint64_t tiles = 0;
+    int steps = 0;
+    for (int j = 0; j < n_layers; ++j) {
+      tiles += tiles_of(layers[j], side);
+      steps = std::max(steps, layers[j].steps * layers[j].parts);
+    }
+    if (steps > 1) most = std::max(most, sizeof(float) * side * side * (size_t)std::min<uint64_t>(units_of(side), tiles * steps));
+  }
+  return most;
 }
 
 }  // namespace
@@ -162,7 +182,7 @@ WeightGradPlan plan_weight_grad(const iso_weight_grad* g, int n, int dt, bool ac
     L.tiles += (uint32_t)l.across * (uint32_t)l.down;
     L.l[L.n++] = l;
   }
-  L.part = (float*)region(sizeof(float) * P.tile * P.tile * (size_t)(L.tiles - L.whole) * L.split);
+  L.part = (float*)region(most_pieces(layers, n_layers));
   P.prep.status = (uint32_t*)ws;
   P.total = at;
   return P;

@@ -59,3 +59,29 @@ def test_embedding_sizes():
         assert sizes == sorted(sizes) and sizes[0] == sizes[2] == 256
         assert sizes[3] >= 4097 * (8 + 4 + 16) + 4 * dim * (4097 // 16)
     assert need(1 << 31, 5, 5) == 0 and need(1, (1 << 20) + 1, 5) == 0
+
+
+@pytest.mark.parametrize("dt", [iso.F32, iso.BF16])
+@pytest.mark.parametrize("o,i", [(2048, 2048), (1024, 1024), (517, 1027), (1, 1), (4100, 300)])
+def test_longest_batch_holds_the_shorter_ones(dt, o, i):
+    """A workspace made for the longest batch is enough for every other: the need does not fall as tokens grow."""
+    tokens = sorted([*range(0, 9000, 31), 4992, 5024, 7104, 7392])
+    sizes = [size([job(t, o, i)], dt) for t in tokens]
+    assert sizes == sorted(sizes)
+
+
+@pytest.mark.parametrize("dt", [iso.F32, iso.BF16])
+def test_need_grows_with_the_table(dt):
+    """Nor as one layer of a table gets tokens (from none on) or a layer joins the launch, and unknown pointers count most."""
+    rng = random.Random(dt)
+    for _ in range(60):
+        shapes = [(rng.choice([0, 0, 5, 300, 3000, 8192]), rng.randint(1, 4000), rng.randint(1, 4000)) for _ in range(rng.randint(1, 16))]
+        need = size([job(*s) for s in shapes], dt)
+        k = rng.randrange(len(shapes))
+        t, o, i = shapes[k]
+        for more in (t + 1, t + 31, t + 32, 2 * t + 100):
+            assert size([job(*s) for s in shapes[:k] + [(more, o, i)] + shapes[k + 1:]], dt) >= need
+        if len(shapes) < 16:
+            assert size([job(*s) for s in shapes + [(rng.choice([0, 700]), 900, 800)]], dt) >= need
+        assert need >= max(size([job(*s)], dt) for s in shapes)
+        assert need >= size([job(*s, q=1 << 32) for s in shapes], dt)
