@@ -467,7 +467,7 @@ iso_status iso_blockdiag_project_factors(const iso_tensor* t, int n_t, int K, in
  *    stride ld >= features, in elements, so that they may be column ranges of a wider buffer.  Any
  *    stride is taken; rows that stay 16-byte aligned are read and written 16 bytes at a time.
  *  - Pointers are device memory, 16-byte aligned, except the ids (their own size).  Outputs must not
- *    overlap inputs unless said so.
+ *    overlap inputs or, in one table, each other unless said so.
  *  - All calls are asynchronous on `stream`, allocate nothing, copy nothing from the host and may be
  *    captured into a graph.  Argument errors are returned before anything is queued.  Tables are
  *    read before the call returns.
@@ -580,7 +580,10 @@ iso_status iso_ckpt_gate_grad(const iso_gate_grad* g, int n, int dt, void* strea
  * of W (in.x is not used); dy is tokens x rows of type dt with row stride ld_dy;
  * grad is rows x cols of type dt_grad.  accumulate = 1 adds to what grad holds.
  * No tokens: a zero gradient (accumulate: unchanged).  Layers of one call that
- * share a checkpoint (q-k-v, gate-up) share the work on it.  Products are exact:
+ * share a checkpoint (q-k-v, gate-up) share the work on it.  A table stands for
+ * its layers one after another: where two name the same grad (tied weights, a
+ * layer used twice), both are added with accumulate = 1, and without it the
+ * later one's result stays.  Products are exact:
  * x is exact in bf16, and an fp32 dy is taken in three bf16 parts.
  */
 typedef struct iso_weight_grad {

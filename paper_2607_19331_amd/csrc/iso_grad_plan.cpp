@@ -109,6 +109,19 @@ size_t most_pieces(const Layer* layers, int n_layers) {
 
 }  // namespace
 
+int weight_grad_group(const iso_weight_grad* g, int n, int dt_grad) {
+  const uint64_t size = dt_grad == ISO_BF16 ? 2 : 4;
+  uint64_t from[kLayers], to[kLayers];
+  n = std::min(n, kLayers);
+  for (int j = 0; j < n; ++j) {
+    from[j] = (uintptr_t)g[j].grad;
+    to[j] = from[j] + size * (uint64_t)(g[j].rows * g[j].in.cols);   // an empty matrix shares nothing
+    for (int k = 0; k < j; ++k)
+      if (std::max(from[j], from[k]) < std::min(to[j], to[k])) return j;
+  }
+  return n;
+}
+
 WeightGradPlan plan_weight_grad(const iso_weight_grad* g, int n, int dt, bool accumulate, uint8_t* ws) {
   WeightGradPlan P;
   size_t at = kStatusBytes;

@@ -122,6 +122,10 @@ struct WeightGradPlan {
   size_t total = 0;
 };
 
+// How many of the first n layers (at most kLayers) go into one launch: those before the first whose gradient shares memory with
+// an earlier one's.  Tiles of one launch run in any order, two that add to the same element would lose one of the sums.
+int weight_grad_group(const iso_weight_grad* g, int n, int dt_grad);
+
 // `ws` may be null where only sizes matter.
 WeightGradPlan plan_weight_grad(const iso_weight_grad* g, int n, int dt, bool accumulate, uint8_t* ws);
 size_t weight_grad_workspace_bytes(const iso_weight_grad* g, int n, int dt);

@@ -421,8 +421,12 @@ void launch(const WeightGradPlan& P, hipStream_t s) {
 }  // namespace
 
 hipError_t run_weight_grad(const iso_weight_grad* g, int n, int dt, int dt_grad, bool accumulate, uint8_t* ws, hipStream_t s) {
-  for (int j = 0; j < n || j == 0; j += kLayers) {
-    const WeightGradPlan P = plan_weight_grad(g + j, std::min(kLayers, n - j), dt, accumulate, ws);
+  // Launches take up to 16 layers; a repeated gradient cuts one of these short, so that the workspace, which was asked for
+  // without a look at the gradients, holds what they need.
+  int j = 0, many;
+  do {
+    many = weight_grad_group(g + j, std::min(kLayers - j % kLayers, n - j), dt_grad);
+    const WeightGradPlan P = plan_weight_grad(g + j, many, dt, accumulate, ws);
     const unsigned grid = std::min(std::max(P.prep.blocks, 1u), 1u << 22);
     if (dt == ISO_BF16) k_wgrad_prep<ISO_BF16><<<grid, 256, 0, s>>>(P.prep);
     else k_wgrad_prep<ISO_F32><<<grid, 256, 0, s>>>(P.prep);
@@ -432,7 +436,8 @@ hipError_t run_weight_grad(const iso_weight_grad* g, int n, int dt, int dt_grad,
     }
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
-  }
+    j += many;
+  } while (j < n);
   return hipSuccess;
 }
 

@@ -141,3 +141,28 @@ def test_embedding_regions(tmp_path):
                 assert o + size <= end
             assert total >= most
             most = total
+
+
+GROUPS = r"""int main(int n, char** v) {
+  std::vector<iso_weight_grad> g((n - 2) / 3);
+  for (size_t j = 0; j < g.size(); ++j)
+    g[j].grad = (void*)(uintptr_t)atoll(v[2 + 3 * j]), g[j].rows = atoll(v[3 + 3 * j]), g[j].in.cols = atoll(v[4 + 3 * j]);
+  printf("%d\n", weight_grad_group(g.data(), (int)g.size(), atoi(v[1])));
+}"""
+
+
+def test_layers_of_one_launch(tmp_path):
+    """A launch ends before a gradient that shares memory with one of its own, and after 16 layers."""
+    run = program(tmp_path, GROUPS)
+    apart = [(4096 * (j + 1), 16, 64) for j in range(20)]          # 4096 bytes each in fp32, 2048 in bf16
+
+    def group(layers, dt=0):
+        return int(run(dt, *[w for l in layers for w in l])[0][0])
+    assert group([]) == 0 and group(apart[:1]) == 1 and group(apart[:9]) == 9 and group(apart) == 16
+    for dt in (0, 1):
+        assert group(apart[:5] + apart[2:3] + apart[6:9], dt) == 5          # the same
+        assert group(apart[:2] + apart[:1] * 3, dt) == 2
+    part = [(4096, 16, 64), (4096 + 2048, 16, 64)]                 # the second half of the first in fp32, behind it in bf16
+    assert group(part, 0) == 1 and group(part[::-1], 0) == 1 and group(part, 1) == 2
+    assert group([(4096, 16, 64), (4096, 0, 64), (5000, 16, 0), (8192, 1, 1)]) == 4    # empty ones share nothing
+    assert group([(4096, 1 << 24, 1 << 10), (4096 + (1 << 35), 4, 4)]) == 1            # past 32 bits
