@@ -58,17 +58,18 @@ class Model:
         self.scale = math.sqrt(DIM)
         self.ws = {}
 
-    def workspace(self, name, make):
-        if name not in self.ws:
-            self.ws[name] = make()
-        return self.ws[name]
+    def workspace(self, name, make, tokens=0):
+        """Kept until a longer batch comes: what a call needs does not fall as tokens grow."""
+        if name not in self.ws or self.ws[name][0] < tokens:
+            self.ws[name] = tokens, make()
+        return self.ws[name][1]
 
     def gradients(self, ids, targets):
         """Loss of the tokens that are no padding; leaves the gradients in the weights' buffers."""
         n = ids.numel()
         table = iso.Embed(ids=ids, tokens=n, vocab=VOCAB, dim=DIM, x=torch.empty(n, DIM, dtype=self.dtype, device="cuda"),
                           table=self.embed.w, grad=self.embed.grad, scale=self.scale, pad_id=PAD)
-        ws = self.workspace("embed", lambda: iso.embed_workspace(table))
+        ws = self.workspace("embed", lambda: iso.embed_workspace(table), n)
         iso.iso_embed_lookup(table, self.code, ws=ws)
         x = table.x
         kept_x = Kept(x, self.code)
@@ -94,7 +95,7 @@ class Model:
         jobs = [iso.WeightGrad(kept.ckpt, dy=dy, grad=w.grad, rows=w.w.shape[0])
                 for kept, dy, w in ((kept_z, dlogits, self.head), (kept_h, dz, self.down), (kept_x, dg, self.gate),
                                     (kept_x, du, self.up))]
-        jobs_ws = self.workspace("jobs", lambda: iso.weight_grad_workspace(jobs, self.code))
+        jobs_ws = self.workspace("jobs", lambda: iso.weight_grad_workspace(jobs, self.code), n)
         iso.iso_ckpt_weight_grad(jobs, self.code, self.code, ws=jobs_ws)
         iso.iso_embed_grad(table, self.code, self.code, ws=ws)
         return loss
