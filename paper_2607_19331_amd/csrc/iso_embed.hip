@@ -42,18 +42,16 @@ __device__ __forceinline__ int32_t row_of(const Ids& ids, int64_t t) {
 
 constexpr int kLookupItems = 2;   // 16-byte vectors a thread (28 us; one, four and eight: 30 for 16384 tokens of 3584)
 constexpr int kLookupBlock = 256 * kLookupItems;
-constexpr int64_t kCheckedAlone = 16384;
 
-// Up to kCheckedAlone tokens, workgroup 0 looks at every id and writes the status word, so that the call is one launch:
-// nothing has to be cleared before the others find a bad id.  Beyond, where its walk would outlast the copies of short rows, a
-// launch before clears the word and it does nothing.  The others copy 512 vectors each, numbered through tokens and columns:
-// a thread's ids, and then its vectors, are in flight together.
+// With `alone` (lookup_checks_alone) workgroup 0 looks at every id and writes the status word, so that the call is one launch:
+// nothing has to be cleared before the others find a bad id.  Else a launch before clears the word and it does nothing.  The
+// others copy 512 vectors each, numbered through tokens and columns: a thread's ids, and then its vectors, are in flight together.
 template <int DT, bool STREAM>
 __global__ void __launch_bounds__(256) k_embed_lookup(Ids ids, const void* __restrict__ table, void* __restrict__ x,
                                                       int64_t tokens, int64_t dim, int64_t ld_x, float scale,
-                                                      uint32_t* status) {
+                                                      bool alone, uint32_t* status) {
   if (blockIdx.x == 0) {
-    if (tokens > kCheckedAlone) return;
+    if (!alone) return;
     __shared__ int any;
     if (threadIdx.x == 0) any = 0;
     __syncthreads();
@@ -78,7 +76,7 @@ __global__ void __launch_bounds__(256) k_embed_lookup(Ids ids, const void* __res
       tok[q] = t0 + d;
       col[q] = (int64_t)(r - d * per_row) * V;
       row[q] = tok[q] < tokens ? row_of(ids, tok[q]) : -1;
-      if (row[q] == -2 && tokens > kCheckedAlone) flag_status(status, kStatusIndex);
+      if (row[q] == -2 && !alone) flag_status(status, kStatusIndex);
     }
     u32x4_t w[kLookupItems];
 #pragma unroll
@@ -670,16 +668,17 @@ hipError_t grad(const iso_embed& e, uint8_t* ws, hipStream_t s) {
 
 hipError_t run_embed_lookup(const iso_embed& e, int dt, uint8_t* ws, hipStream_t s) {
   const int v = dt == ISO_BF16 ? kVec<ISO_BF16> : kVec<ISO_F32>;
-  const int64_t items = e.tokens * ((e.dim + v - 1) / v);
+  const int64_t items = e.tokens * ((e.dim + v - 1) / v), row_bytes = e.dim * (dt == ISO_BF16 ? 2 : 4);
+  const bool alone = lookup_checks_alone(e.tokens, row_bytes);
   const unsigned grid = 1 + grid_for((items + kLookupBlock - 1) / kLookupBlock);
   auto go = [&](auto k) {
-    k<<<grid, 256, 0, s>>>(ids_of(e), e.table, e.x, e.tokens, e.dim, e.ld_x, (float)e.scale, (uint32_t*)ws);
+    k<<<grid, 256, 0, s>>>(ids_of(e), e.table, e.x, e.tokens, e.dim, e.ld_x, (float)e.scale, alone, (uint32_t*)ws);
   };
-  if (e.tokens > kCheckedAlone) {
+  if (!alone) {
     const hipError_t err = fill_u32((uint32_t*)ws, 1, 0u, s);
     if (err != hipSuccess) return err;
   }
-  const bool stream = streamed(e.tokens * e.dim * (dt == ISO_BF16 ? 2 : 4));
+  const bool stream = streamed(e.tokens * row_bytes);
   if (dt == ISO_BF16) stream ? go(k_embed_lookup<ISO_BF16, true>) : go(k_embed_lookup<ISO_BF16, false>);
   else stream ? go(k_embed_lookup<ISO_F32, true>) : go(k_embed_lookup<ISO_F32, false>);
   return hipGetLastError();

@@ -10,6 +10,19 @@
 
 namespace iso {
 
+// ---- embedding lookup ----------------------------------------------------------------------------------------------
+
+// Whether one workgroup looks at all ids, under the copies of the others; where its walk (0.65 us for 1024 ids) outlasts them, a
+// launch before clears the status word and every workgroup looks at its own.  Microseconds on the GPU, alone against that
+// launch, bf16 rows of a table of about 152000 (fp32 rows of the same bytes take about the same; a table of 32000 too):
+//   columns      4096 tokens      6000      8192        16384       32768
+//        64      4.2  4.6           -     6.7  4.6   11.8  4.7   22.2  5.2
+//      1024      5.2  6.0    6.9  7.2    10.3  8.0   23.3 12.3   42.3 17.7
+//      2048      6.4  8.0    8.8 10.1    12.9 12.3   20.6 18.8   45.4 33.2
+//      2560      7.9  9.4   10.4 11.7    10.5 11.8   22.9 22.8   49.0 41.0
+//      3584      9.9 11.4   10.8 12.3    15.6 17.1   29.0 30.6   54.4 55.8
+inline bool lookup_checks_alone(int64_t tokens, int64_t row_bytes) { return tokens <= (row_bytes > 4096 ? 16384 : 6144); }
+
 // ---- embedding gradient --------------------------------------------------------------------------------------------
 
 // The tokens of an id are added in runs of kRun, whose sums are then added in order.

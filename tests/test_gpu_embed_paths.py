@@ -207,3 +207,25 @@ def test_streamed_lookup(dtype, n, vocab, dim, gap):
         off = (x.view.double() - ref).abs() - (2.0 ** -23 + unit(dtype)) * SLACK * ref.abs()
         assert float(off.max()) <= 0
         x.guards()
+
+
+@pytest.mark.parametrize("dtype,n,dim", [("bf16", 6144, 2048), ("bf16", 6145, 2048), ("bf16", 6145, 2049), ("f32", 16384, 1025),
+                                         ("f32", 16385, 1025), ("f32", 6145, 1024), ("bf16", 6145, 1), ("bf16", 16384, 9)])
+def test_who_looks_at_the_ids(dtype, n, dim):
+    """On both sides of each bound: rows, status with the one bad id at either end, status cleared by the next call."""
+    import torch
+    say(f"embed paths: bad id in a lookup {dtype} n={n} dim={dim}")
+    gen = torch.Generator(device="cuda").manual_seed(n + dim)
+    table = torch.randn(301, dim, generator=gen, device="cuda").to(ttype(dtype))
+    x = Buf(n, dim, dtype, 1)
+    ws = iso.embed_workspace(iso.Embed(ids=1, tokens=n, vocab=301, dim=dim, x=None, id_type=iso.I64))
+    ws.fill_(0xFF)
+    for at in (0, None, n - 1, n // 2, None):
+        ids = draw_ids(gen, n, 301, None, "even")
+        if at is not None:
+            ids[at] = 301
+        iso.iso_embed_lookup(iso.Embed(ids=ids, tokens=n, vocab=301, dim=dim, x=x.view, ld_x=x.ld, table=table), code(dtype), ws=ws)
+        assert iso.iso_read_device_status(ws) == (0 if at is None else _lib.ERR_INDEX)
+        want = table[ids.clamp(max=300)] * (ids < 301)[:, None]
+        assert torch.equal(x.view, want)
+        x.guards()

@@ -166,3 +166,11 @@ def test_layers_of_one_launch(tmp_path):
     assert group(part, 0) == 1 and group(part[::-1], 0) == 1 and group(part, 1) == 2
     assert group([(4096, 16, 64), (4096, 0, 64), (5000, 16, 0), (8192, 1, 1)]) == 4    # empty ones share nothing
     assert group([(4096, 1 << 24, 1 << 10), (4096 + (1 << 35), 4, 4)]) == 1            # past 32 bits
+
+
+def test_who_looks_at_the_ids(tmp_path):
+    """Up to 6144 tokens one workgroup, up to 16384 where rows are long enough for the copies to outlast it."""
+    run = program(tmp_path, 'int main(int, char** v) { printf("%d\\n", lookup_checks_alone(atoll(v[1]), atoll(v[2]))); }')
+    for row, most in ((2, 6144), (128, 6144), (4096, 6144), (4098, 16384), (7168, 16384), (1 << 20, 16384)):
+        for tokens, alone in ((0, 1), (1, 1), (6144, 1), (most, 1), (most + 1, 0), (1 << 31, 0)):
+            assert run(tokens, row) == [[str(alone)]], (tokens, row)
