@@ -28,8 +28,17 @@ inline bool lookup_checks_alone(int64_t tokens, int64_t row_bytes) { return toke
 // The tokens of an id are added in runs of kRun, whose sums are then added in order.
 constexpr int kRun = 32;
 
-// Up to 4096 tokens of a 151936 x 1536 table are added in 24 us in one launch and in 38 by the sorted launches (2048: 18 and
-// 35); 4096 tokens of one id, the worst case, in 98 and 44.
+// Tokens of the gradient's single launch: as many as its workgroups hold (eight ids a thread, two bytes of LDS a token).
+// Microseconds on the GPU, the single launch against the sorted ones, bf16 rows added to fp32:
+//   table, ids                          256 tokens       1024          2048          4096
+//   1031 x 256, by frequency             6.9  17.5     9.8  24.4    11.3  25.7    16.4  27.2
+//   151936 x 1536, by frequency          9.5  18.2    12.7  26.5    16.2  29.4    20.6  32.9
+//   151936 x 1536, evenly                9.9  17.4    13.7  21.6    18.0  27.2    24.5  30.5
+//   152064 x 3584, by frequency         16.2  17.9    23.3  29.2    30.6  33.9    41.1  40.3
+//   152064 x 3584, evenly               17.2  18.5    25.8  26.9    33.3  31.9    43.9  43.2
+//   151936 x 1536, all the same         10.3  20.2    26.3  24.3    47.6  30.5    98.5  41.2
+// It is ahead over its whole range but for the widest rows (level from 2048 on) and for batches of one id from 1024 on, whose
+// tokens one workgroup a column block adds: which ids there are is not known on the host.
 constexpr int kFewTokens = 4096;
 
 constexpr int kMaxTiles = 64;
