@@ -461,11 +461,14 @@ iso_status iso_blockdiag_project_factors(const iso_tensor* t, int n_t, int K, in
  *
  * G_W of iso_frame (rows x cols row-major, the step's storage type) is what a backward pass leaves for
  * a weight matrix.  The calls below make it for an embedding and for linear layers, the latter from
- * activations kept in 8 bits between the forward and the backward pass.
+ * activations kept in 8 bits between the forward and the backward pass.  The step reads G in the type of
+ * its weights: an fp32 G (one that bf16 micro-batches were added to, say) goes with fp32 weights, and the
+ * caller rounds it for a step on bf16 ones; a bf16 G can be added to as well, rounded at every call.
  *
  *  - Weights and weight gradients are contiguous; activation matrices (tokens x features) have a row
- *    stride ld >= features, in elements, so that they may be column ranges of a wider buffer.  Any
- *    stride is taken; rows that stay 16-byte aligned are read and written 16 bytes at a time.
+ *    stride ld >= features, in elements, so that they may be column ranges of a wider buffer
+ *    that start at a multiple of 16 bytes.  Any stride is taken; a weight
+ *    gradient copies a bf16 dy first whose stride is no multiple of 8 (or exceeds 2^25).
  *  - Pointers are device memory, 16-byte aligned, except the ids (their own size).  Outputs must not
  *    overlap inputs or, in one table, each other unless said so.
  *  - All calls are asynchronous on `stream`, allocate nothing, copy nothing from the host and may be
@@ -498,7 +501,8 @@ typedef struct iso_embed {
   void* grad;            /* gradient: G, vocab x dim                                                 */
 } iso_embed;
 
-/* Bytes of workspace for either call on these sizes (0 on bad arguments); 256-byte aligned. */
+/* Bytes of workspace for either call on these sizes (0 on bad arguments); 256-byte aligned.  They do not
+ * fall as tokens grow: a workspace for the longest batch holds the shorter ones. */
 size_t iso_workspace_size_embed(const iso_embed* e);
 
 /*
@@ -528,9 +532,11 @@ iso_status iso_embed_grad(const iso_embed* e, int dt, int dt_grad, int accumulat
  * of a group of 32 columns in a row share a power of two:
  *   2^k the least with max |x| <= 127 * 2^k and k >= -126,
  *   q = x / 2^k rounded to the nearest integer, ties to even  (|q| <= 127),
- * so a value is off by at most 2^(k-1) <= max|x| / 127 of its group (for k = 122,
+ * so a value is off by at most 2^(k-1), which is less than max|x| / 127 of its
+ * group except where k is held at -126: a group whose largest is 127 * 2^-127 or
+ * less is off by up to 2^-127, whatever that is of its largest.  (For k = 122,
  * reached above 127 * 2^121 only, |q| is held at 63, off by at most 2^122: 64 *
- * 2^122 would come back infinite).  q holds rows x ld
+ * 2^122 would come back infinite.)  q holds rows x ld
  * int8 values (zeros in the padding), e holds rows x ld/32 bytes k + 127 (1 for
  * a group of zeros).  A group that holds a NaN or an infinity is kept as
  * e = 255, q = 0 and comes back as NaN in all its columns.  The stored values q 2^k are
@@ -578,7 +584,9 @@ iso_status iso_ckpt_gate_grad(const iso_gate_grad* g, int n, int dt, void* strea
  *   G = round([G +] sum over the tokens t of dy_t x_t^T),
  * the sum in binary32.  in.rows is the number of tokens and in.cols the columns
  * of W (in.x is not used); dy is tokens x rows of type dt with row stride ld_dy;
- * grad is rows x cols of type dt_grad.  accumulate = 1 adds to what grad holds.
+ * grad is rows x cols of type dt_grad.  A bf16 dy is read in whole pieces of 16
+ * bytes: up to 14 bytes behind its last element, within the piece that holds it,
+ * are read and not used.  accumulate = 1 adds to what grad holds.
  * No tokens: a zero gradient (accumulate: unchanged).  Layers of one call that
  * share a checkpoint (q-k-v, gate-up) share the work on it.  A table stands for
  * its layers one after another: where two name the same grad (tied weights, a

@@ -4,7 +4,7 @@
 // lose nothing but the sum's own rounding; a binary32 dY is the sum of three bf16 parts of 8 bits each (cut, not
 // rounded: every remainder is exact), which makes it three products with the same X, added least part first.
 //
-// A call is up to three launches per 16 layers.  k_wgrad_prep brings operands into the form that the product reads,
+// A call is up to three launches per 16 layers (fewer where a gradient repeats).  k_wgrad_prep brings operands into the form that the product reads,
 // bf16 rows aligned to 16 bytes: X always (once per checkpoint, however many layers share it), dY where it is fp32 or
 // its rows are not aligned.  k_wgrad forms the tiles of all layers' gradients.  k_wgrad_join adds up tiles whose
 // tokens were split.
