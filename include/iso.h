@@ -67,7 +67,9 @@
  * optimizer steps take come from iso_embed_lookup / iso_embed_grad (an
  * embedding and its gradient) and from 8-bit activation checkpoints:
  * iso_ckpt_pack, iso_ckpt_unpack, iso_ckpt_gate_grad, iso_ckpt_weight_grad;
- * their conventions stand with them.
+ * between them attention (iso_attend, iso_attend_grad), and at the logits the
+ * distillation from a teacher's top entries (iso_distill_loss,
+ * iso_distill_grad); their conventions stand with them.
  */
 #ifndef ISO_H
 #define ISO_H
@@ -90,7 +92,7 @@ typedef enum iso_status {
   ISO_ERR_HIP = 5,
   ISO_ERR_UNSUPPORTED = 6,
   ISO_ERR_INTERNAL = 7,    /* a kernel met counts that cannot occur; outputs invalid */
-  ISO_ERR_INDEX = 8        /* a token id outside the vocabulary                        */
+  ISO_ERR_INDEX = 8        /* a token id outside the vocabulary, or row offsets of no range */
 } iso_status;
 
 /* The enumerations name the values of plain int parameters and fields: the library checks
@@ -611,6 +613,112 @@ size_t iso_workspace_size_weight_grad(const iso_weight_grad* g, int n, int dt);
 
 iso_status iso_ckpt_weight_grad(const iso_weight_grad* g, int n, int dt, int dt_grad, int accumulate, void* ws,
                                 size_t ws_bytes, void* stream);
+
+/*
+ * Attention over packed sequences.  Sequence s has the rows start_q[s] ... start_q[s+1] - 1 of q (n of them) and
+ * start_k[s] ... start_k[s+1] - 1 of k and v (m of them).  Its query i stands at position p = i + m - n (the last
+ * query at the last key) and sees the keys j of the sequence with
+ *   j <= p  where causal,   j > p - window  and  j < p + window  where window > 0.
+ * Query heads share key and value heads in consecutive groups of heads / heads_kv: head h reads kv head
+ * h / (heads / heads_kv).  A row of q or out holds heads * dim values (head by head), one of k or v heads_kv * dim.
+ *
+ *  - q, k, v, out and the gradients are of one type, their row strides multiples of 16 bytes (ISO_ERR_ALIGNMENT
+ *    otherwise), of up to ISO_ATTN_MAX_LD elements; dim is a multiple of 8 up to ISO_ATTN_MAX_DIM.
+ *  - Offsets are device memory, sequences + 1 values each, ascending, 0 <= start <= tokens.  A sequence whose
+ *    offsets are no range of the rows is left out, and reported by iso_read_device_status (ISO_ERR_INDEX).
+ *  - Rows of q, k and v that belong to no sequence are not read, and those of the outputs not written.
+ *  - A result depends on the keys (or queries) that are seen and on no others: what non-finite values others
+ *    hold does not reach it.  Calls that meet non-finite values in a result work that part out once more, row
+ *    by row and slowly.
+ */
+#define ISO_ATTN_MAX_DIM 128
+#define ISO_ATTN_MAX_LD (1 << 21)
+#define ISO_ATTN_MAX_SEQUENCES (1 << 20)
+
+/* Which pointers (and strides) are read depends on the call. */
+typedef struct iso_attn {
+  const void* q;             /* tokens_q x heads * dim, row stride ld_q                              */
+  const void* k;             /* tokens_k x heads_kv * dim, row stride ld_k                           */
+  const void* v;             /* tokens_k x heads_kv * dim, row stride ld_v                           */
+  int64_t ld_q, ld_k, ld_v;
+  const int32_t* start_q;
+  const int32_t* start_k;
+  int64_t sequences, tokens_q, tokens_k;
+  int32_t heads, heads_kv, dim;
+  int32_t causal;            /* 0 or 1                                                               */
+  int64_t window;            /* 0: none                                                              */
+  double scale;              /* finite, > 0                                                          */
+  void* out;                 /* O: tokens_q x heads * dim, row stride ld_out                         */
+  int64_t ld_out;
+  float* lse;                /* tokens_q x heads, contiguous                                         */
+  const void* dout;          /* gradient of out, row stride ld_dout                                  */
+  int64_t ld_dout;
+  void* dq;                  /* gradients of q, k, v                                                 */
+  void* dk;
+  void* dv;
+  int64_t ld_dq, ld_dk, ld_dv;
+} iso_attn;
+
+/* Bytes of workspace for iso_attend (grad = 0) or iso_attend_grad (grad = 1) on these sizes (0 on bad arguments);
+ * 256-byte aligned.  They do not fall as tokens or sequences grow. */
+size_t iso_workspace_size_attend(const iso_attn* a, int dt, int grad);
+
+/*
+ * iso_attend -- O_i = sum over the keys j seen of P_ij v_j, P_ij = exp(scale q_i.k_j - L_i), L_i the logarithm of
+ * the sum of exp(scale q_i.k_j).  A query that sees no key has O = 0 and L = -infinity.  out and lse are written.
+ * With bf16, P is rounded to bf16 in the product with V (its sum is not).
+ */
+iso_status iso_attend(const iso_attn* a, int dt, void* ws, size_t ws_bytes, void* stream);
+
+/*
+ * iso_attend_grad -- from out, lse (those of iso_attend) and dout: with P as above, D_i = dout_i.O_i and
+ * S_ij = P_ij (dout_i.v_j - D_i),
+ *   dv_j = sum_i P_ij dout_i,   dk_j = scale sum_i S_ij q_i,   dq_i = scale sum_j S_ij k_j,
+ * the first two over the heads of a group too.  All three are written.  With bf16, P and S are rounded to bf16 in
+ * the products.
+ */
+iso_status iso_attend_grad(const iso_attn* a, int dt, void* ws, size_t ws_bytes, void* stream);
+
+/*
+ * Distillation from a teacher's top entries.  A token has logits z over the vocabulary and a list of `top` entries,
+ * an id and the teacher's logit y each.  With t = softmax(y / T) over the list and L = logsumexp(z / T),
+ *   loss = w T^2 sum over the entries of t (log t - z_id / T + L),
+ *   grad_v = w T (exp(z_v / T - L) - sum of t over the entries with id v).
+ * One entry at T = 1 is the cross entropy with its id.
+ *
+ *  - Entries with id pad_id or a logit of -infinity are none; a token without entries, and one of weight 0, has a
+ *    zero loss and a zero gradient, whatever its logits hold (L is written all the same).  Ids may repeat in a list.
+ *  - An id that is neither pad_id nor in [0, vocab) is reported by iso_read_device_status (ISO_ERR_INDEX); its entry
+ *    is none.
+ *  - logits and grad are of type dt with any row strides.  grad may be logits itself (same stride).
+ */
+#define ISO_DISTILL_MAX_TOP 256
+
+typedef struct iso_distill {
+  const void* logits;        /* z: tokens x vocab, row stride ld                                     */
+  int64_t tokens, vocab, ld; /* tokens < 2^31, 1 <= vocab <= ISO_EMBED_MAX_VOCAB                     */
+  const void* ids;           /* tokens x top, contiguous, of id_type                                 */
+  int32_t id_type;
+  int32_t top;               /* 1 <= top <= ISO_DISTILL_MAX_TOP                                      */
+  const float* teacher;      /* y: tokens x top, contiguous                                          */
+  int64_t pad_id;
+  const float* weight;       /* w: one a token; NULL: 1                                              */
+  double temperature;        /* T, finite, > 0                                                       */
+  float* loss;               /* one a token                                                          */
+  float* lse;                /* L, one a token                                                       */
+  void* grad;                /* tokens x vocab, row stride ld_grad                                   */
+  int64_t ld_grad;
+} iso_distill;
+
+/* Bytes of workspace for either call (0 on bad arguments); 256-byte aligned.  They do not fall as tokens grow. */
+size_t iso_workspace_size_distill(const iso_distill* d);
+
+/* iso_distill_loss -- writes loss and lse, and the gradient too unless grad is NULL: rows that fit on chip are read
+ * once for all three. */
+iso_status iso_distill_loss(const iso_distill* d, int dt, void* ws, size_t ws_bytes, void* stream);
+
+/* iso_distill_grad -- writes the gradient from the lse that iso_distill_loss left (loss is not used). */
+iso_status iso_distill_grad(const iso_distill* d, int dt, void* ws, size_t ws_bytes, void* stream);
 
 /* round(n * num / den), halves rounded up, in exact integer arithmetic; -1 on bad arguments. */
 int64_t iso_k_from_density(int64_t n, int64_t num, int64_t den);

@@ -225,7 +225,7 @@ def iso_optimizer_step_muon(frames, dtype, lr, momentum=0.95, weight_decay=0.0, 
     _check(rc, "iso_optimizer_step_muon")
 
 
-# ---- gradients for the optimizer steps: embeddings, 8-bit activation checkpoints ----------------------------------
+# ---- gradients for the optimizer steps: embeddings, 8-bit activation checkpoints, attention, distillation ----------
 
 
 @dataclass
@@ -378,6 +378,120 @@ def iso_ckpt_weight_grad(jobs: Sequence[WeightGrad], dtype, grad_dtype, accumula
     rc = _lib.load().iso_ckpt_weight_grad(_weight_grads(jobs), len(jobs), dtype, grad_dtype, 1 if accumulate else 0, wp,
                                           wb, _stream(stream))
     _check(rc, "iso_ckpt_weight_grad")
+
+
+@dataclass
+class Attn:
+    """Attention over packed sequences: q (tokens_q x heads * dim), k and v (tokens_k x heads_kv * dim), int32 offsets of the
+    sequences' rows (sequences + 1 each, on the device), out like q and lse (tokens_q x heads, float32).  For the gradient also
+    dout, dq like q and dk, dv like k.  Row strides are those of contiguous rows if None.  window None or 0: none."""
+    q: object
+    k: object
+    v: object
+    start_q: object
+    start_k: object
+    sequences: int
+    tokens_q: int
+    tokens_k: int
+    heads: int
+    heads_kv: int
+    dim: int
+    scale: float
+    out: object
+    lse: object
+    causal: bool = False
+    window: Optional[int] = None
+    dout: Optional[object] = None
+    dq: Optional[object] = None
+    dk: Optional[object] = None
+    dv: Optional[object] = None
+    ld_q: Optional[int] = None
+    ld_k: Optional[int] = None
+    ld_v: Optional[int] = None
+    ld_out: Optional[int] = None
+    ld_dout: Optional[int] = None
+    ld_dq: Optional[int] = None
+    ld_dk: Optional[int] = None
+    ld_dv: Optional[int] = None
+
+
+def _attn(a: Attn):
+    wide, narrow = a.heads * a.dim, a.heads_kv * a.dim
+
+    def ld(x, default):
+        return default if x is None else x
+
+    return _lib.IsoAttn(_ptr(a.q), _ptr(a.k), _ptr(a.v), ld(a.ld_q, wide), ld(a.ld_k, narrow), ld(a.ld_v, narrow),
+                        _ptr(a.start_q), _ptr(a.start_k), a.sequences, a.tokens_q, a.tokens_k, a.heads, a.heads_kv, a.dim,
+                        1 if a.causal else 0, a.window or 0, a.scale, _ptr(a.out), ld(a.ld_out, wide), _ptr(a.lse),
+                        _ptr(a.dout), ld(a.ld_dout, wide), _ptr(a.dq), _ptr(a.dk), _ptr(a.dv), ld(a.ld_dq, wide),
+                        ld(a.ld_dk, narrow), ld(a.ld_dv, narrow))
+
+
+def attend_workspace(a: Attn, dtype, grad=False, device="cuda"):
+    """Workspace for iso_attend, or with grad for iso_attend_grad, on these sizes."""
+    n = _lib.load().iso_workspace_size_attend(ctypes.byref(_attn(a)), dtype, 1 if grad else 0)
+    if n == 0:
+        raise ValueError("bad attention sizes")
+    return _bytes(n, device)
+
+
+def iso_attend(a: Attn, dtype, ws=None, stream=None):
+    wp, wb = _ws(ws)
+    _check(_lib.load().iso_attend(ctypes.byref(_attn(a)), dtype, wp, wb, _stream(stream)), "iso_attend")
+
+
+def iso_attend_grad(a: Attn, dtype, ws=None, stream=None):
+    wp, wb = _ws(ws)
+    _check(_lib.load().iso_attend_grad(ctypes.byref(_attn(a)), dtype, wp, wb, _stream(stream)), "iso_attend_grad")
+
+
+@dataclass
+class Distill:
+    """Distillation from a teacher's top entries: logits (tokens x vocab, row stride ld, vocab if None), ids (int32 or int64)
+    and the teacher's logits (float32) of `top` entries a token, weight (float32, one a token; None: 1), loss and lse
+    (float32, one a token), grad (like logits, row stride ld_grad; may be the logits).  Entries with id pad_id are none."""
+    logits: object
+    tokens: int
+    vocab: int
+    ids: object
+    teacher: object
+    top: int
+    lse: object
+    loss: Optional[object] = None
+    grad: Optional[object] = None
+    weight: Optional[object] = None
+    temperature: float = 1.0
+    pad_id: Optional[int] = None
+    ld: Optional[int] = None
+    ld_grad: Optional[int] = None
+    id_type: Optional[int] = None      # I32 or I64; None: from ids.dtype
+
+
+def _distill(d: Distill):
+    wide = d.id_type if d.id_type is not None else _id_type(d.ids)
+    return _lib.IsoDistill(_ptr(d.logits), d.tokens, d.vocab, d.vocab if d.ld is None else d.ld, _ptr(d.ids), wide, d.top,
+                           _ptr(d.teacher), _lib.NO_PAD if d.pad_id is None else d.pad_id, _ptr(d.weight), d.temperature,
+                           _ptr(d.loss), _ptr(d.lse), _ptr(d.grad), d.vocab if d.ld_grad is None else d.ld_grad)
+
+
+def distill_workspace(d: Distill, device="cuda"):
+    """Workspace for iso_distill_loss and iso_distill_grad on these sizes."""
+    n = _lib.load().iso_workspace_size_distill(ctypes.byref(_distill(d)))
+    if n == 0:
+        raise ValueError("bad distillation sizes")
+    return _bytes(n, device)
+
+
+def iso_distill_loss(d: Distill, dtype, ws=None, stream=None):
+    """Loss and lse, and the gradient too where d.grad is given."""
+    wp, wb = _ws(ws)
+    _check(_lib.load().iso_distill_loss(ctypes.byref(_distill(d)), dtype, wp, wb, _stream(stream)), "iso_distill_loss")
+
+
+def iso_distill_grad(d: Distill, dtype, ws=None, stream=None):
+    wp, wb = _ws(ws)
+    _check(_lib.load().iso_distill_grad(ctypes.byref(_distill(d)), dtype, wp, wb, _stream(stream)), "iso_distill_grad")
 
 
 def iso_spectral_diagnostics(entries, dtype, out, ws=None, stream=None):

@@ -14,6 +14,8 @@ I32, I64 = 0, 1
 NO_PAD = -(1 << 63)
 CKPT_GROUP = 32
 EMBED_MAX_VOCAB = 1 << 20
+ATTN_MAX_DIM, ATTN_MAX_LD, ATTN_MAX_SEQUENCES = 128, 1 << 21, 1 << 20
+DISTILL_MAX_TOP = 256
 MERGE_TA, MERGE_TIES, MERGE_RAM = 0, 1, 2
 UPDATE_APPLY, UPDATE_FUSED, UPDATE_SPECTRAL, UPDATE_ORTHO = 0, 1, 2, 3
 (OP_TOPK, OP_SIGN, OP_MERGE, OP_UPDATE_APPLY, OP_UPDATE_FUSED, OP_UPDATE_FUSED_SELECT, OP_UPDATE_SPECTRAL,
@@ -25,7 +27,9 @@ SYMBOLS = ["iso_workspace_size", "iso_topk_mask", "iso_sign_elect", "iso_merge",
            "iso_workspace_size_optimizer", "iso_optimizer_step", "iso_optimizer_step_muon", "iso_spectral_diagnostics",
            "iso_spectrum_interpolate", "iso_transport_ratios", "iso_spectral_error", "iso_update_noalloc",
            "iso_workspace_size_embed", "iso_embed_lookup", "iso_embed_grad", "iso_ckpt_ld", "iso_ckpt_pack",
-           "iso_ckpt_unpack", "iso_ckpt_gate_grad", "iso_workspace_size_weight_grad", "iso_ckpt_weight_grad"]
+           "iso_ckpt_unpack", "iso_ckpt_gate_grad", "iso_workspace_size_weight_grad", "iso_ckpt_weight_grad",
+           "iso_workspace_size_attend", "iso_attend", "iso_attend_grad", "iso_workspace_size_distill", "iso_distill_loss",
+           "iso_distill_grad"]
 
 
 class IsoTensor(ctypes.Structure):
@@ -87,6 +91,26 @@ class IsoWeightGrad(ctypes.Structure):
                 ("rows", ctypes.c_int64)]
 
 
+class IsoAttn(ctypes.Structure):
+    _fields_ = [("q", ctypes.c_void_p), ("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("ld_q", ctypes.c_int64),
+                ("ld_k", ctypes.c_int64), ("ld_v", ctypes.c_int64), ("start_q", ctypes.c_void_p),
+                ("start_k", ctypes.c_void_p), ("sequences", ctypes.c_int64), ("tokens_q", ctypes.c_int64),
+                ("tokens_k", ctypes.c_int64), ("heads", ctypes.c_int32), ("heads_kv", ctypes.c_int32),
+                ("dim", ctypes.c_int32), ("causal", ctypes.c_int32), ("window", ctypes.c_int64),
+                ("scale", ctypes.c_double), ("out", ctypes.c_void_p), ("ld_out", ctypes.c_int64),
+                ("lse", ctypes.c_void_p), ("dout", ctypes.c_void_p), ("ld_dout", ctypes.c_int64),
+                ("dq", ctypes.c_void_p), ("dk", ctypes.c_void_p), ("dv", ctypes.c_void_p), ("ld_dq", ctypes.c_int64),
+                ("ld_dk", ctypes.c_int64), ("ld_dv", ctypes.c_int64)]
+
+
+class IsoDistill(ctypes.Structure):
+    _fields_ = [("logits", ctypes.c_void_p), ("tokens", ctypes.c_int64), ("vocab", ctypes.c_int64),
+                ("ld", ctypes.c_int64), ("ids", ctypes.c_void_p), ("id_type", ctypes.c_int32), ("top", ctypes.c_int32),
+                ("teacher", ctypes.c_void_p), ("pad_id", ctypes.c_int64), ("weight", ctypes.c_void_p),
+                ("temperature", ctypes.c_double), ("loss", ctypes.c_void_p), ("lse", ctypes.c_void_p),
+                ("grad", ctypes.c_void_p), ("ld_grad", ctypes.c_int64)]
+
+
 _lib = None
 
 
@@ -139,6 +163,13 @@ def load():
     L.iso_workspace_size_weight_grad.argtypes = [W, I, I]
     L.iso_workspace_size_weight_grad.restype = Z
     L.iso_ckpt_weight_grad.argtypes = [W, I, I, I, I, P, Z, P]
+    A, Q = ctypes.POINTER(IsoAttn), ctypes.POINTER(IsoDistill)
+    L.iso_workspace_size_attend.argtypes = [A, I, I]
+    L.iso_workspace_size_attend.restype = Z
+    L.iso_workspace_size_distill.argtypes = [Q]
+    L.iso_workspace_size_distill.restype = Z
+    for fn, t in (("iso_attend", A), ("iso_attend_grad", A), ("iso_distill_loss", Q), ("iso_distill_grad", Q)):
+        getattr(L, fn).argtypes = [t, I, P, Z, P]
     L.iso_status_string.argtypes = [I]
     L.iso_status_string.restype = ctypes.c_char_p
     for fn in ("iso_topk_mask", "iso_sign_elect", "iso_merge", "iso_update", "iso_update_noalloc",
@@ -148,7 +179,8 @@ def load():
                "iso_spectrum_interpolate", "iso_transport_ratios", "iso_spectral_error",
                "iso_read_device_status", "iso_read_fallback_count", "iso_profile_begin", "iso_profile_end",
                "iso_profile_flops", "iso_embed_lookup", "iso_embed_grad", "iso_ckpt_pack", "iso_ckpt_unpack",
-               "iso_ckpt_gate_grad", "iso_ckpt_weight_grad"):
+               "iso_ckpt_gate_grad", "iso_ckpt_weight_grad", "iso_attend", "iso_attend_grad", "iso_distill_loss",
+               "iso_distill_grad"):
         getattr(L, fn).restype = I
     _lib = L
     return L

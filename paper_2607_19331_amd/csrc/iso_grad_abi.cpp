@@ -97,6 +97,77 @@ iso_status check_weight_grads(const iso_weight_grad* g, int n, int dt, bool poin
   return ISO_OK;
 }
 
+// Rows of `cols` values with a stride that kernels read by 16 bytes.
+iso_status check_rows(const void* p, int64_t ld, int64_t cols, int dt, bool pointers) {
+  if (ld < cols) return ISO_ERR_INVALID_ARG;
+  if (ld > ISO_ATTN_MAX_LD) return ISO_ERR_UNSUPPORTED;
+  if (ld % (dt == ISO_BF16 ? 8 : 4) != 0) return ISO_ERR_ALIGNMENT;
+  return pointers ? check_ptr(p) : ISO_OK;
+}
+
+iso_status check_words(const void* p) {
+  if (p == nullptr) return ISO_ERR_INVALID_ARG;
+  return ((uintptr_t)p & 3u) == 0 ? ISO_OK : ISO_ERR_ALIGNMENT;
+}
+
+// Sizes only with pointers == false (workspace queries, which read no strides either).
+iso_status check_attn(const iso_attn* a, int dt, int grad, bool pointers) {
+  if (a == nullptr || !is_dtype(dt) || !is_flag(grad)) return ISO_ERR_INVALID_ARG;
+  if (a->sequences < 0 || a->tokens_q < 0 || a->tokens_k < 0 || a->heads < 1 || a->heads_kv < 1 || a->dim < 1)
+    return ISO_ERR_INVALID_ARG;
+  if (a->heads % a->heads_kv != 0 || !is_flag(a->causal) || a->window < 0) return ISO_ERR_INVALID_ARG;
+  if (!std::isfinite((float)a->scale) || !((float)a->scale > 0.0f)) return ISO_ERR_INVALID_ARG;
+  if (a->dim % 8 != 0 || a->dim > ISO_ATTN_MAX_DIM || a->sequences > ISO_ATTN_MAX_SEQUENCES) return ISO_ERR_UNSUPPORTED;
+  if (a->heads > ISO_ATTN_MAX_LD / a->dim || !attend_fits(*a)) return ISO_ERR_UNSUPPORTED;
+  if (!pointers || a->sequences == 0) return ISO_OK;
+  const int64_t wide = (int64_t)a->heads * a->dim, narrow = (int64_t)a->heads_kv * a->dim;
+  iso_status st;
+  if ((st = check_words(a->start_q)) != ISO_OK || (st = check_words(a->start_k)) != ISO_OK) return st;
+  if (a->tokens_q > 0) {
+    if ((st = check_rows(a->q, a->ld_q, wide, dt, true)) != ISO_OK) return st;
+    if ((st = check_rows(a->out, a->ld_out, wide, dt, true)) != ISO_OK) return st;
+    if ((st = check_ptr(a->lse)) != ISO_OK) return st;
+    if (grad != 0) {
+      if ((st = check_rows(a->dout, a->ld_dout, wide, dt, true)) != ISO_OK) return st;
+      if ((st = check_rows(a->dq, a->ld_dq, wide, dt, true)) != ISO_OK) return st;
+    }
+  }
+  if (a->tokens_k > 0) {
+    if ((st = check_rows(a->k, a->ld_k, narrow, dt, true)) != ISO_OK) return st;
+    if ((st = check_rows(a->v, a->ld_v, narrow, dt, true)) != ISO_OK) return st;
+    if (grad != 0) {
+      if ((st = check_rows(a->dk, a->ld_dk, narrow, dt, true)) != ISO_OK) return st;
+      if ((st = check_rows(a->dv, a->ld_dv, narrow, dt, true)) != ISO_OK) return st;
+    }
+  }
+  return ISO_OK;
+}
+
+iso_status check_distill_sizes(const iso_distill* d) {
+  if (d == nullptr || d->tokens < 0 || d->vocab < 1 || d->top < 1) return ISO_ERR_INVALID_ARG;
+  if (d->id_type != ISO_I32 && d->id_type != ISO_I64) return ISO_ERR_INVALID_ARG;
+  if (d->tokens >= (1ll << 31) || d->vocab > ISO_EMBED_MAX_VOCAB || d->top > ISO_DISTILL_MAX_TOP) return ISO_ERR_UNSUPPORTED;
+  return ISO_OK;
+}
+
+iso_status check_distill(const iso_distill* d, int dt, bool loss, bool grad) {
+  iso_status st = check_distill_sizes(d);
+  if (st != ISO_OK) return st;
+  const float t = (float)d->temperature, inv = (float)(1.0 / d->temperature);
+  if (!is_dtype(dt) || !std::isfinite(t) || !(t > 0.0f) || !std::isfinite(inv) || !(inv > 0.0f)) return ISO_ERR_INVALID_ARG;
+  if (d->tokens == 0) return ISO_OK;
+  if (d->ids == nullptr || d->ld < d->vocab) return ISO_ERR_INVALID_ARG;
+  if (((uintptr_t)d->ids & (d->id_type == ISO_I64 ? 7u : 3u)) != 0) return ISO_ERR_ALIGNMENT;
+  if (too_large(d->tokens, d->ld)) return ISO_ERR_UNSUPPORTED;
+  if ((st = check_ptr(d->logits)) != ISO_OK || (st = check_ptr(d->teacher)) != ISO_OK || (st = check_ptr(d->lse)) != ISO_OK) return st;
+  if (d->weight != nullptr && (st = check_ptr(d->weight)) != ISO_OK) return st;
+  if (loss && (st = check_ptr(d->loss)) != ISO_OK) return st;
+  if (!grad) return ISO_OK;
+  if (d->ld_grad < d->vocab || (d->grad == d->logits && d->ld_grad != d->ld)) return ISO_ERR_INVALID_ARG;
+  if (too_large(d->tokens, d->ld_grad)) return ISO_ERR_UNSUPPORTED;
+  return check_ptr(d->grad);
+}
+
 iso_status from_hip(hipError_t e) { return e == hipSuccess ? ISO_OK : ISO_ERR_HIP; }
 
 }  // namespace
@@ -168,6 +239,43 @@ iso_status iso_ckpt_weight_grad(const iso_weight_grad* g, int n, int dt, int dt_
   if (!is_dtype(dt_grad) || !is_flag(accumulate)) return ISO_ERR_INVALID_ARG;
   if ((st = check_ws(ws, ws_bytes, weight_grad_workspace_bytes(g, n, dt))) != ISO_OK) return st;
   return from_hip(run_weight_grad(g, n, dt, dt_grad, accumulate != 0, (uint8_t*)ws, (hipStream_t)stream));
+}
+
+size_t iso_workspace_size_attend(const iso_attn* a, int dt, int grad) {
+  if (check_attn(a, dt, grad, false) != ISO_OK) return 0;
+  return attend_workspace_bytes(*a, dt, grad != 0);
+}
+
+iso_status iso_attend(const iso_attn* a, int dt, void* ws, size_t ws_bytes, void* stream) {
+  iso_status st = check_attn(a, dt, 0, true);
+  if (st != ISO_OK) return st;
+  if ((st = check_ws(ws, ws_bytes, attend_workspace_bytes(*a, dt, false))) != ISO_OK) return st;
+  return from_hip(run_attend(*a, dt, (uint8_t*)ws, (hipStream_t)stream));
+}
+
+iso_status iso_attend_grad(const iso_attn* a, int dt, void* ws, size_t ws_bytes, void* stream) {
+  iso_status st = check_attn(a, dt, 1, true);
+  if (st != ISO_OK) return st;
+  if ((st = check_ws(ws, ws_bytes, attend_workspace_bytes(*a, dt, true))) != ISO_OK) return st;
+  return from_hip(run_attend_grad(*a, dt, (uint8_t*)ws, (hipStream_t)stream));
+}
+
+size_t iso_workspace_size_distill(const iso_distill* d) {
+  return check_distill_sizes(d) == ISO_OK ? distill_workspace_bytes() : 0;
+}
+
+iso_status iso_distill_loss(const iso_distill* d, int dt, void* ws, size_t ws_bytes, void* stream) {
+  iso_status st = check_distill(d, dt, true, d != nullptr && d->grad != nullptr);
+  if (st != ISO_OK) return st;
+  if ((st = check_ws(ws, ws_bytes, distill_workspace_bytes())) != ISO_OK) return st;
+  return from_hip(run_distill_loss(*d, dt, (uint8_t*)ws, (hipStream_t)stream));
+}
+
+iso_status iso_distill_grad(const iso_distill* d, int dt, void* ws, size_t ws_bytes, void* stream) {
+  iso_status st = check_distill(d, dt, false, true);
+  if (st != ISO_OK) return st;
+  if ((st = check_ws(ws, ws_bytes, distill_workspace_bytes())) != ISO_OK) return st;
+  return from_hip(run_distill_grad(*d, dt, (uint8_t*)ws, (hipStream_t)stream));
 }
 
 }  // extern "C"

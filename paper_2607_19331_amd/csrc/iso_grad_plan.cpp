@@ -209,4 +209,16 @@ size_t weight_grad_workspace_bytes(const iso_weight_grad* g, int n, int dt) {
   return most;
 }
 
+// ---- attention -----------------------------------------------------------------------------------------------------
+
+bool attend_fits(const iso_attn& a) {
+  // a row (query head) a wave of 64 lanes in launches of fewer than 2^32 threads
+  const int64_t most = 1ll << 25;
+  return a.tokens_q <= most && a.tokens_k <= most && a.heads <= most && a.tokens_q * a.heads <= most && a.tokens_k * a.heads_kv <= most;
+}
+
+size_t attend_workspace_bytes(const iso_attn& a, int, bool grad) {
+  return kStatusBytes + (grad ? align_up(sizeof(float) * (size_t)(a.tokens_q * a.heads), 256) : 0);
+}
+
 }  // namespace iso

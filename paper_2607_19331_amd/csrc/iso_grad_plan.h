@@ -152,4 +152,15 @@ int weight_grad_group(const iso_weight_grad* g, int n, int dt_grad);
 WeightGradPlan plan_weight_grad(const iso_weight_grad* g, int n, int dt, bool accumulate, uint8_t* ws);
 size_t weight_grad_workspace_bytes(const iso_weight_grad* g, int n, int dt);
 
+// ---- attention -----------------------------------------------------------------------------------------------------
+
+// Whether the rows of a call and its launches stay within 32 bits.
+bool attend_fits(const iso_attn& a);
+size_t attend_workspace_bytes(const iso_attn& a, int dt, bool grad);
+
+// ---- distillation --------------------------------------------------------------------------------------------------
+
+constexpr int64_t kMostPieces = 4096;   // of all rows of a call whose rows are shared out
+inline size_t distill_workspace_bytes() { return kStatusBytes + kMostPieces * 2 * sizeof(float); }
+
 }  // namespace iso

@@ -79,3 +79,49 @@ def test_weight_gradient_by_differences():
             step[o, i] = 1e-4
             hi, lo = (float(((x @ (w + s * step).T) * dy).sum()) for s in (1, -1))
             assert abs((hi - lo) / 2e-4 - g[o, i]) < 1e-8
+
+
+@pytest.mark.parametrize("n,m,causal,window", [(4, 4, True, 0), (3, 6, True, 0), (5, 3, True, 0), (4, 5, False, 2), (6, 6, True, 3),
+                                               (3, 0, False, 0)])
+def test_attention_gradients_against_differences(n, m, causal, window):
+    rng = np.random.default_rng(n * 10 + m)
+    q, k, v, g = (rng.standard_normal((r, 5)) for r in (n, m, m, n))
+    scale, h = 0.7, 1e-6
+    out, lse = gr.attend(q, k, v, scale, causal, window)
+    grads = gr.attend_grad(q, k, v, out, lse, g, scale, causal, window)
+    for x, dx in zip((q, k, v), grads):
+        for at in np.ndindex(x.shape):
+            keep, f = x[at], []
+            for e in (h, -h):
+                x[at] = keep + e
+                f.append((gr.attend(q, k, v, scale, causal, window)[0] * g).sum())
+            x[at] = keep
+            assert abs((f[0] - f[1]) / (2 * h) - dx[at]) < 1e-7
+    blind = [i for i in range(n) if gr.keys_seen(i, n, m, causal, window)[0] == gr.keys_seen(i, n, m, causal, window)[1]]
+    assert (out[blind] == 0).all() and (lse[blind] == -np.inf).all() and (grads[0][blind] == 0).all()
+
+
+@pytest.mark.parametrize("temp", [1.0, 2.5])
+def test_distillation_gradient_against_differences(temp):
+    rng = np.random.default_rng(5)
+    z, y = rng.standard_normal((4, 9)), rng.standard_normal((4, 3))
+    ids = np.array([[1, 4, 8], [3, 3, 0], [7, -1, 2], [-1, -1, -1]])
+    w, h = np.array([1.0, 0.5, 2.0, 1.0]), 1e-6
+    loss, _, grad = gr.distill(z, ids, y, temp, w, -1)
+    assert loss[3] == 0 and (grad[3] == 0).all()
+    for at in np.ndindex(z.shape):
+        keep, f = z[at], []
+        for e in (h, -h):
+            z[at] = keep + e
+            f.append(gr.distill(z, ids, y, temp, w, -1)[0].sum())
+        z[at] = keep
+        assert abs((f[0] - f[1]) / (2 * h) - grad[at]) < 1e-7
+
+
+def test_distillation_of_one_entry_is_cross_entropy():
+    rng = np.random.default_rng(6)
+    z = rng.standard_normal((5, 11))
+    ids = rng.integers(0, 11, (5, 1))
+    loss, lse, grad = gr.distill(z, ids, np.zeros((5, 1)), 1.0)
+    assert np.allclose(loss, lse - z[np.arange(5), ids[:, 0]])
+    assert np.allclose(grad.sum(1), 0)
