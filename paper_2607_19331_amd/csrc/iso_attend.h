@@ -13,6 +13,10 @@ namespace iso {
 
 constexpr float kLog2e = 1.44269504088896341f, kLn2 = 0.693147180559945309f;
 
+// A row's running maximum is only followed where it has grown by more than this (in powers of two): sums stay below
+// 2^8 times their terms, and most tiles scale nothing.
+constexpr float kSlack = 8.0f;
+
 struct AttnArgs {
   const void *q, *k, *v;
   int64_t ld_q, ld_k, ld_v;           // row strides, elements
@@ -30,6 +34,8 @@ struct AttnArgs {
   void *dq, *dk, *dv;
   int64_t ld_dq, ld_dk, ld_dv;
   float* delta;                       // D of every row, tokens_q x heads
+  int32_t pieces;                     // most pieces that a tile's keys are shared out to
+  float* part;                        // their sums: pieces x tokens_q x heads x kPartLd
   uint32_t* status;
 };
 
@@ -149,7 +155,7 @@ struct Two {
 
 // O and L of row r of kv head `head`.
 template <int DT>
-__device__ __noinline__ void attend_row(const AttnArgs& A, const Seq& s, int head, int64_t r, int lane) {
+__device__ __forceinline__ void attend_row(const AttnArgs& A, const Seq& s, int head, int64_t r, int lane) {
   const int64_t i = r / A.group;
   const int h = head * A.group + (int)(r - i * A.group);
   int32_t lo, hi;

@@ -1,0 +1,269 @@
+// Tiles of the attention kernels: panels of token rows in LDS, fragments of them for matrix instructions.
+//
+// All products have 32 x 32 results.  A result has one column a lane (lane % 32) and in register r row 8 (r / 4) + 4 half + r % 4,
+// half = lane / 32.  Scores are formed with the summed-over index of the next product as rows: that product then takes them from
+// the registers where they are.  Which 8 (bf16) values of the summed index a lane holds for one instruction is free as long as
+// both operands agree, so the other operand is read from LDS in the order that the result has.
+#pragma once
+
+#include "iso_attend.h"
+#include "iso_mfma.h"
+
+namespace iso {
+
+constexpr int kAttnWaves = 4;
+
+// Panels of kRows token rows of D dimensions (head dimensions up to D, the rest zero), 16 KiB; a row's 16-byte pieces are
+// permuted (piece p at p ^ mix(row)), so that 16 successive rows have the same piece in different banks, and so have four
+// successive rows 64 bytes next to each other (bf16) or two rows four apart 128 bytes (fp32).
+template <int DT, int D>
+struct Panel {
+  static constexpr int kSize = DT == ISO_BF16 ? 2 : 4;
+  static constexpr int kRowBytes = D * kSize;
+  static constexpr int kPieces = kRowBytes / 16;
+  static constexpr int kRows = D == 128 ? (DT == ISO_BF16 ? 64 : 32) : (DT == ISO_BF16 ? 64 : 32);
+  static constexpr int kBytes = kRows * kRowBytes;
+  static constexpr int kLoads = kBytes / (1024 * kAttnWaves);   // 16-byte loads a lane
+  static constexpr int kTiles = kRows / 32;                     // 32-row tiles
+  static constexpr int kGroups = kRowBytes / 32;                // 32-byte groups of a row: 16 bytes for either half of a wave
+  static constexpr int kDims = D / 32;                          // 32-dimension tiles
+
+  __device__ static __forceinline__ int mix(int row) {
+    if constexpr (DT == ISO_F32) return (row & 3) | ((row >> 3) & 1) << 2 | ((row >> 2) & 1) << 3;
+    else if constexpr (D == 128) return (row & 3) << 2 | ((row >> 2) & 3);
+    else return ((row >> 1) & 1) << 2 | ((row >> 2) & 3);
+  }
+
+  // Of load j of a wave: the panel's row and the byte of the row that a lane takes from memory.
+  __device__ static __forceinline__ void source(int j, int wave, int lane, int& row, int& byte) {
+    const int at = (j * kAttnWaves + wave) * 64 + lane;
+    row = at / kPieces;
+    byte = ((at % kPieces) ^ mix(row)) * 16;
+  }
+};
+
+constexpr uint32_t kOutside = 0xC0000000u;   // an offset behind the end of every buffer
+
+// One operand's rows in memory, loaded panel by panel: `row` 0 of a kv head of a sequence and how many there are.
+template <int DT, int D>
+struct Rows {
+  using P = Panel<DT, D>;
+  const uint8_t* base;
+  int64_t step, bytes;   // bytes of a panel's rows, and from row 0 on to the end of the last row
+  uint32_t offset[P::kLoads];
+
+  __device__ __forceinline__ Rows(const void* p, int64_t first, int64_t ld, int64_t col, int64_t rows, int dim, int wave, int lane) {
+    base = (const uint8_t*)p + (first * ld + col) * P::kSize;
+    step = P::kRows * ld * P::kSize;
+    bytes = rows > 0 ? ((rows - 1) * ld + dim) * P::kSize : 0;
+#pragma unroll
+    for (int j = 0; j < P::kLoads; ++j) {
+      int row, byte;
+      P::source(j, wave, lane, row, byte);
+      offset[j] = byte < dim * P::kSize ? (uint32_t)(row * (int)ld * P::kSize + byte) : kOutside;
+    }
+  }
+  // Panel t into LDS; one past the last, zeros.
+  __device__ __forceinline__ void load(int64_t t, uint32_t lds, int wave) const {
+    u32x4_t b = buffer_of(base + t * step, min(bytes - t * step, (int64_t)0x80000000ll));
+#pragma unroll
+    for (int j = 0; j < 4; ++j) b[j] = __builtin_amdgcn_readfirstlane(b[j]);
+    lds = __builtin_amdgcn_readfirstlane(lds);
+#pragma unroll
+    for (int j = 0; j < P::kLoads; ++j) load_lds(b, lds + (j * kAttnWaves + wave) * 1024, offset[j]);
+  }
+};
+
+typedef __attribute__((address_space(3))) const u32x4_t* lds_piece;
+typedef __attribute__((address_space(3))) const float* lds_float;
+
+// Where a lane reads a panel's fragments: rows, 16 bytes a group, for the product that sums over dimensions; and columns, for
+// the one that sums over rows.
+template <int DT, int D>
+struct Reader {
+  using P = Panel<DT, D>;
+  uint32_t row0;        // its row and half, for tile 0
+  int key;              // mix of that row
+  uint32_t col0[P::kDims];
+
+  __device__ __forceinline__ explicit Reader(int lane) {
+    const int r = lane & 31, half = lane >> 5, i = lane & 15, g = lane >> 4;
+    row0 = r * P::kRowBytes;
+    key = P::mix(r) ^ half;
+#pragma unroll
+    for (int d = 0; d < P::kDims; ++d) {
+      if constexpr (DT == ISO_BF16) {
+        // 16 lanes read a block of four rows by 16 columns and get a column each
+        const int row = 4 * (g >> 1) + (i >> 2), byte = d * 64 + (g & 1) * 32 + (i & 3) * 8;
+        col0[d] = row * P::kRowBytes + ((byte / 16) ^ P::mix(row)) * 16 + byte % 16;
+      } else {
+        const int row = 4 * half;
+        col0[d] = row * P::kRowBytes + (((d * 32 + r) / 4) ^ P::mix(row)) * 16 + (r % 4) * 4;
+      }
+    }
+  }
+  // 16 bytes of group g of the lane's row of tile t.
+  __device__ __forceinline__ u32x4_t row(uint32_t panel, int t, int g) const {
+    const int p = (2 * g) ^ key;   // half is part of key
+    return *(lds_piece)(uintptr_t)(panel + t * 32 * P::kRowBytes + row0 + p * 16);
+  }
+  // bf16: dimensions 32 d + lane % 32 of rows 16 s + 4 half + {0..3, 8..11} of tile t.
+  __device__ __forceinline__ bf16x8_t col(uint32_t panel, int t, int s, int d) const {
+    struct {
+      s16x4_t h[2];
+    } f;
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      // rows 16 s + 8 h on: mix changes by bit 3 of the row (bits 2 and 3 of a row are its lower bits)
+      const uint32_t at = panel + (t * 32 + 16 * s + 8 * h) * P::kRowBytes + (col0[d] ^ (h ? P::mix(8) * 16 : 0));
+      f.h[h] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_frag)(uintptr_t)at);
+    }
+    return __builtin_bit_cast(bf16x8_t, f);
+  }
+  // fp32: dimension 32 d + lane % 32 of row 8 g + 4 half + e of tile t.
+  __device__ __forceinline__ float one(uint32_t panel, int t, int g, int e, int d) const {
+    const uint32_t x = (uint32_t)(P::mix((8 * g) & 15) ^ P::mix(e)) * 16;
+    return *(lds_float)(uintptr_t)(panel + (t * 32 + 8 * g + e) * P::kRowBytes + (col0[d] ^ x));
+  }
+};
+
+// acc += A B over one group of 16 (bf16) or 8 (fp32) dimensions; of these, half of a wave holds 8 or 4 in order.
+template <int DT>
+__device__ __forceinline__ void multiply(u32x4_t a, u32x4_t b, f32x16_t& acc) {
+  if constexpr (DT == ISO_BF16) {
+    acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, a), __builtin_bit_cast(bf16x8_t, b), acc, 0, 0, 0);
+  } else {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) acc = __builtin_amdgcn_mfma_f32_32x32x2f32(f32_from_bits(a[e]), f32_from_bits(b[e]), acc, 0, 0, 0);
+  }
+}
+
+// A lane's row (a query's, say) as second operand: all groups, in registers.
+template <int DT, int D>
+struct OwnRow {
+  u32x4_t g[Panel<DT, D>::kGroups];
+  // From element `at` on, dim of them; zeros where !on.
+  __device__ __forceinline__ void load(const void* p, int64_t at, int dim, int half, bool on) {
+    constexpr int V = 16 / Panel<DT, D>::kSize;
+#pragma unroll
+    for (int i = 0; i < Panel<DT, D>::kGroups; ++i) {
+      const int c = (2 * i + half) * V;
+      g[i] = u32x4_t{0, 0, 0, 0};
+      if (on && c < dim) g[i] = load_raw<DT>(p, at + c);
+    }
+  }
+};
+
+// Results as second operand of a product that sums over their rows, in the type of the call.
+template <int DT>
+struct Packed;
+template <>
+struct Packed<ISO_BF16> {
+  u32x4_t s[2];
+  __device__ __forceinline__ void set(int i, float lo, float hi) { s[i / 4][i % 4] = pack_bf16(lo, hi); }   // registers 2i, 2i + 1
+};
+template <>
+struct Packed<ISO_F32> {
+  float v[16];
+  __device__ __forceinline__ void set(int i, float lo, float hi) { v[2 * i] = lo, v[2 * i + 1] = hi; }
+};
+
+// acc[d] += (columns 32 d ... of tile t of a panel)^T x, summed over the tile's 32 rows.
+template <int DT, int D>
+__device__ __forceinline__ void multiply_columns(const Reader<DT, D>& r, uint32_t panel, int t, const Packed<DT>& x,
+                                                 f32x16_t (&acc)[D / 32]) {
+  if constexpr (DT == ISO_BF16) {
+#pragma unroll
+    for (int s = 0; s < 2; ++s)
+#pragma unroll
+      for (int d = 0; d < D / 32; ++d)
+        acc[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(r.col(panel, t, s, d), __builtin_bit_cast(bf16x8_t, x.s[s]), acc[d], 0, 0, 0);
+  } else {
+#pragma unroll
+    for (int i = 0; i < 16; ++i)
+#pragma unroll
+      for (int d = 0; d < D / 32; ++d)
+        acc[d] = __builtin_amdgcn_mfma_f32_32x32x2f32(r.one(panel, t, i / 4, i % 4, d), x.v[i], acc[d], 0, 0, 0);
+  }
+}
+
+// All loads into LDS have landed and all LDS reads are done, of every wave.
+__device__ __forceinline__ void landed() { asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
+
+// The value of the lane with the same column in the other half.
+__device__ __forceinline__ float other_half(float v) { return __shfl_xor(v, 32); }
+
+// ---- which tile a workgroup has ------------------------------------------------------------------------------------
+
+// Work is a list of tiles of rows for every kv head.  Workgroup b runs on XCD b % 8: heads are dealt to as many classes of XCDs
+// as divide them evenly, so that a head's keys and values are read through few L2 caches, and a class takes the tiles of a head
+// from the last (which sees most under a causal mask) to the first, its XCDs in turn.
+struct Deal {
+  int32_t classes, per;   // classes of XCDs, XCDs of a class
+  uint32_t tiles;         // tiles of a head (or an upper bound), times the pieces of each
+};
+
+inline Deal deal_of(int heads, uint32_t tiles) {
+  int c = 8;
+  while (heads % c != 0) c /= 2;
+  return Deal{c, 8 / c, tiles};
+}
+inline uint32_t deal_grid(const Deal& d, int heads) {
+  const uint64_t n = (uint64_t)(heads / d.classes) * d.tiles;
+  return (uint32_t)((n + d.per - 1) / d.per * 8);
+}
+__device__ __forceinline__ bool dealt(const Deal& d, int heads, uint32_t b, int& head, uint32_t& tile) {
+  const uint32_t x = b & 7u, c = x % d.classes, j = (b >> 3) * d.per + x / d.classes, h = j / d.tiles;
+  if (h >= (uint32_t)(heads / d.classes)) return false;
+  head = (int)(c + d.classes * h);
+  tile = d.tiles - 1 - (j - h * d.tiles);
+  return true;
+}
+
+// The sequence that has tile `tile` of the list of all sequences' tiles of kTile rows each (rows: queries times the group, or
+// keys), and which of its tiles that is.  Every lane of a wave takes part, each with a sequence.
+template <bool KEYS, int TILE>
+__device__ __forceinline__ bool find_tile(const AttnArgs& A, uint32_t tile, Seq& s, uint32_t& at) {
+  const int lane = threadIdx.x & 63;
+  uint32_t before = 0;
+  for (int32_t s0 = 0; s0 < A.sequences; s0 += 64) {
+    Seq mine{0, 0, 0, 0};
+    if (s0 + lane < A.sequences) mine = seq_of(A, s0 + lane);
+    const uint32_t rows = KEYS ? (uint32_t)mine.nk : (uint32_t)mine.nq * (uint32_t)A.group;
+    uint32_t sum = (rows + TILE - 1) / TILE;
+    const uint32_t own = sum;
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) {
+      const uint32_t up = __shfl_up(sum, d);
+      if (lane >= d) sum += up;
+    }
+    const uint64_t behind = __ballot(before + sum > tile);
+    if (behind != 0) {
+      const int src = __builtin_ctzll(behind);
+      s.q0 = __shfl(mine.q0, src), s.k0 = __shfl(mine.k0, src);
+      s.nq = __shfl(mine.nq, src), s.nk = __shfl(mine.nk, src);
+      at = tile - before - __shfl(sum - own, src);
+      // the same in every lane; say so
+      s.q0 = (int64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int32_t)s.q0);
+      s.k0 = (int64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int32_t)s.k0);
+      s.nq = __builtin_amdgcn_readfirstlane(s.nq), s.nk = __builtin_amdgcn_readfirstlane(s.nk);
+      at = __builtin_amdgcn_readfirstlane(at);
+      return at < ((KEYS ? (uint32_t)s.nk : (uint32_t)s.nq * (uint32_t)A.group) + TILE - 1) / TILE;
+    }
+    before += __shfl(sum, 63);
+  }
+  return false;
+}
+
+// Whether the values of a wave hold a NaN or an infinity: 0 times such a value is NaN, and a sum with one stays one.
+template <int N>
+__device__ __forceinline__ float trouble(const f32x16_t (&v)[N], float f) {
+  float t = 0.0f;
+#pragma unroll
+  for (int d = 0; d < N; ++d)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) t = fmaf(v[d][r] * f, 0.0f, t);
+  return t;
+}
+
+}  // namespace iso

@@ -217,8 +217,17 @@ bool attend_fits(const iso_attn& a) {
   return a.tokens_q <= most && a.tokens_k <= most && a.heads <= most && a.tokens_q * a.heads <= most && a.tokens_k * a.heads_kv <= most;
 }
 
+// Pieces where they fit into the partial sums' share of the workspace, which few rows do: a call of many rows fills the card.
+int attend_pieces(const iso_attn& a) {
+  const int64_t rows = std::max<int64_t>(1, a.tokens_q * a.heads), by_keys = (a.tokens_k + kPieceKeys - 1) / kPieceKeys;
+  return (int)std::max<int64_t>(1, std::min({(int64_t)kMostKeyPieces, by_keys, kPartRows / rows}));
+}
+
 size_t attend_workspace_bytes(const iso_attn& a, int, bool grad) {
-  return kStatusBytes + (grad ? align_up(sizeof(float) * (size_t)(a.tokens_q * a.heads), 256) : 0);
+  const int64_t rows = a.tokens_q * a.heads;
+  if (grad) return kStatusBytes + align_up(sizeof(float) * (size_t)rows, 256);
+  const int64_t by_keys = std::max<int64_t>(1, std::min<int64_t>(kMostKeyPieces, (a.tokens_k + kPieceKeys - 1) / kPieceKeys));
+  return kStatusBytes + align_up(sizeof(float) * kPartLd * (size_t)std::min(kPartRows, rows * by_keys), 256);
 }
 
 }  // namespace iso

@@ -156,6 +156,16 @@ size_t weight_grad_workspace_bytes(const iso_weight_grad* g, int n, int dt);
 
 // Whether the rows of a call and its launches stay within 32 bits.
 bool attend_fits(const iso_attn& a);
+
+constexpr int kAttnTileRows = 128;     // rows (queries times the group) of a tile
+constexpr int kPieceKeys = 256;        // fewest keys of a piece of a tile
+constexpr int kMostKeyPieces = 64;     // of a tile
+constexpr int64_t kPartRows = 1 << 16; // rows of all pieces of a call
+constexpr int kPartLd = 132;           // floats of a row's piece: its sums, maximum and sum of weights
+
+// Tiles of `rows` rows in `sequences` sequences at most.
+inline int64_t attend_tiles(int64_t rows, int64_t sequences) { return rows / kAttnTileRows + sequences; }
+int attend_pieces(const iso_attn& a);
 size_t attend_workspace_bytes(const iso_attn& a, int dt, bool grad);
 
 // ---- distillation --------------------------------------------------------------------------------------------------

@@ -17,6 +17,7 @@
 #include "iso_device.h"
 #include "iso_grad.h"
 #include "iso_grad_device.h"
+#include "iso_mfma.h"
 
 namespace iso {
 
@@ -111,32 +112,6 @@ __global__ void __launch_bounds__(256) k_wgrad_prep(PrepTable T) {
 }
 
 // ---- the product ---------------------------------------------------------------------------------------------------
-
-typedef __attribute__((address_space(3))) uint8_t lds_u8;
-typedef short s16x4_t __attribute__((ext_vector_type(4)));
-typedef __attribute__((address_space(3))) s16x4_t* lds_frag;
-typedef __bf16 bf16x8_t __attribute__((ext_vector_type(8)));
-typedef float f32x16_t __attribute__((ext_vector_type(16)));
-
-// Descriptor of a buffer of `left` bytes: reads past its end give zeros.
-__device__ __forceinline__ u32x4_t buffer_of(const uint8_t* p, int64_t left) {
-  const uint64_t a = (uint64_t)p;
-  const uint32_t n = left <= 0 ? 0u : left > 0xFFFFFFF0ll ? 0xFFFFFFF0u : (uint32_t)left;
-  return u32x4_t{(uint32_t)a, (uint32_t)(a >> 32) & 0xFFFFu, n, 0x00027000u};
-}
-
-// 16 bytes a lane from the buffer into LDS, the wave's 1024 bytes one after another from byte `lds` on.  An instruction
-// of its own because the compiler waits for every such load before the next LDS read, whatever that reads; k_wgrad
-// counts them itself.  It has no destination register; m0 needs one instruction between its write and its use.
-#pragma clang diagnostic push
-#pragma clang diagnostic ignored "-Winline-asm"   // m0 among the clobbers
-__device__ __forceinline__ void load_lds(u32x4_t buffer, uint32_t lds, uint32_t offset) {
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(lds), "v"(offset), "s"(buffer)
-               : "m0");
-}
-#pragma clang diagnostic pop
-
-typedef __attribute__((address_space(3))) f32x4_t* lds_f32x4;
 
 // 32 rows of a wave's part of G from row m, column n on, as it reads and writes them: 16 bytes a lane, whole rows.  `old`
 // holds what a lane adds to.
