@@ -634,6 +634,8 @@ iso_status iso_ckpt_weight_grad(const iso_weight_grad* g, int n, int dt, int dt_
 #define ISO_ATTN_MAX_DIM 128
 #define ISO_ATTN_MAX_LD (1 << 21)
 #define ISO_ATTN_MAX_SEQUENCES (1 << 20)
+#define ISO_ATTN_MAX_GROUP 1024
+#define ISO_ATTN_MAX_ROWS (1 << 25)      /* tokens_q * heads, and tokens_k * heads_kv */
 
 /* Which pointers (and strides) are read depends on the call. */
 typedef struct iso_attn {

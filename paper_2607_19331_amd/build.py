@@ -11,7 +11,7 @@ LIB = os.path.join(HERE, "libiso.so")
 
 SOURCES = ["iso_abi.cpp", "iso_select.hip", "iso_merge.hip", "iso_fused.hip", "iso_spectral.hip", "iso_tsv.hip",
            "iso_noalloc.hip", "iso_ortho.hip", "iso_grad_abi.cpp", "iso_grad_plan.cpp", "iso_embed.hip", "iso_ckpt.hip",
-           "iso_wgrad.hip", "iso_attend.hip", "iso_distill.hip"]
+           "iso_wgrad.hip", "iso_attend.hip", "iso_attend_grad.hip", "iso_distill.hip"]
 
 # the C ABI layers and the gradient operators' plans: argument checks and host-side planning (what the sanitized build
 # instruments)

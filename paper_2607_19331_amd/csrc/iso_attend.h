@@ -8,6 +8,7 @@
 #include "iso.h"
 #include "iso_device.h"
 #include "iso_grad_device.h"
+#include "iso_grad_plan.h"
 
 namespace iso {
 
@@ -33,11 +34,24 @@ struct AttnArgs {
   int64_t ld_dout;
   void *dq, *dk, *dv;
   int64_t ld_dq, ld_dk, ld_dv;
-  float* delta;                       // D of every row, tokens_q x heads
-  int32_t pieces;                     // most pieces that a tile's keys are shared out to
+  float* stat;                        // for every row of a group's list, kv head by kv head: L log2(e), then D
+  Pieces pieces;                      // that a tile's keys are shared out to
   float* part;                        // their sums: pieces x tokens_q x heads x kPartLd
   uint32_t* status;
 };
+
+inline AttnArgs args_of(const iso_attn& a, uint8_t* ws) {
+  AttnArgs A{};
+  A.q = a.q, A.k = a.k, A.v = a.v, A.ld_q = a.ld_q, A.ld_k = a.ld_k, A.ld_v = a.ld_v;
+  A.start_q = a.start_q, A.start_k = a.start_k, A.tokens_q = a.tokens_q, A.tokens_k = a.tokens_k;
+  A.sequences = (int32_t)a.sequences, A.heads = a.heads, A.heads_kv = a.heads_kv, A.group = a.heads / a.heads_kv, A.dim = a.dim;
+  A.causal = a.causal, A.window = a.window;
+  A.scale = (float)a.scale, A.scale2 = (float)(a.scale * 1.4426950408889634);
+  A.out = a.out, A.ld_out = a.ld_out, A.lse = a.lse, A.dout = a.dout, A.ld_dout = a.ld_dout;
+  A.dq = a.dq, A.dk = a.dk, A.dv = a.dv, A.ld_dq = a.ld_dq, A.ld_dk = a.ld_dk, A.ld_dv = a.ld_dv;
+  A.status = (uint32_t*)ws;
+  return A;
+}
 
 // One sequence: first rows and lengths.  The queries of a kv head's group are taken as one list of `rows` = nq group rows,
 // row r being query r / group of head r % group of the group: rows next to each other see (almost) the same keys.
@@ -189,15 +203,23 @@ __device__ __forceinline__ void pair(const AttnArgs& A, int64_t q, int64_t g, in
   ds = p * (dot_row<DT>(A.dout, g, A.v, v, A.dim) - delta);
 }
 
+// Where the list of a kv head's rows starts in stat, and D of row r of it.
+__device__ __forceinline__ int64_t list_of(const AttnArgs& A, const Seq& s, int head) {
+  return ((int64_t)head * A.tokens_q + s.q0) * A.group;
+}
+__device__ __forceinline__ float delta_of(const AttnArgs& A, const Seq& s, int head, int64_t r) {
+  return gmem(A.stat)[A.tokens_q * A.heads + list_of(A, s, head) + r];
+}
+
 // dq of row r.
 template <int DT>
-__device__ __noinline__ void dq_row(const AttnArgs& A, const Seq& s, int head, int64_t r, int lane) {
+__device__ __forceinline__ void dq_row(const AttnArgs& A, const Seq& s, int head, int64_t r, int lane) {
   const int64_t i = r / A.group, col = (int64_t)head * A.dim;
   const int h = head * A.group + (int)(r - i * A.group);
   int32_t lo, hi;
   keys_of(A, s, i, lo, hi);
   const int64_t q = (s.q0 + i) * A.ld_q + (int64_t)h * A.dim, g = (s.q0 + i) * A.ld_dout + (int64_t)h * A.dim;
-  const float lse = gmem(A.lse)[(s.q0 + i) * A.heads + h], delta = gmem(A.delta)[(s.q0 + i) * A.heads + h];
+  const float lse = gmem(A.lse)[(s.q0 + i) * A.heads + h], delta = delta_of(A, s, head, r);
   Two<DT> sum;
   for (int32_t j0 = lo; j0 < hi; j0 += 64) {
     const int64_t j = s.k0 + min(j0 + lane, hi - 1);
@@ -211,7 +233,7 @@ __device__ __noinline__ void dq_row(const AttnArgs& A, const Seq& s, int head, i
 
 // dk and dv of key j.
 template <int DT>
-__device__ __noinline__ void dkv_row(const AttnArgs& A, const Seq& s, int head, int32_t j, int lane) {
+__device__ __forceinline__ void dkv_row(const AttnArgs& A, const Seq& s, int head, int32_t j, int lane) {
   int32_t lo, hi;
   queries_of(A, s, j, lo, hi);
   const int64_t col = (int64_t)head * A.dim, k = (s.k0 + j) * A.ld_k + col, v = (s.k0 + j) * A.ld_v + col;
@@ -222,7 +244,7 @@ __device__ __noinline__ void dkv_row(const AttnArgs& A, const Seq& s, int head, 
     const int h = head * A.group + (int)(r % A.group);
     const int64_t q = i * A.ld_q + (int64_t)h * A.dim, g = i * A.ld_dout + (int64_t)h * A.dim;
     float p, ds;
-    pair<DT>(A, q, g, k, v, gmem(A.lse)[i * A.heads + h], gmem(A.delta)[i * A.heads + h], p, ds);
+    pair<DT>(A, q, g, k, v, gmem(A.lse)[i * A.heads + h], delta_of(A, s, head, r), p, ds);
     const int n = (int)min((int64_t)64, last - r0);
     for (int c = 0; c < n; ++c) {
       dk.add(__shfl(ds, c), A.q, __shfl(q, c), lane, A.dim);

@@ -1,0 +1,504 @@
+// Attention over packed sequences, backward: with P = exp(scale Q K^T - L) worked out again, D = sum of dO O over a row and
+// S = P (dO V^T - D),  dV = P^T dO,  dK = scale S^T Q,  dQ = scale S K.
+//
+// Two kernels form P and S each for itself: k_attend_dkv has keys and walks over the rows that see them, k_attend_dq has rows
+// and walks over the keys that they see.  That is seven products of rows x keys x dim where one kernel would need five, but each
+// result has one owner who adds in a fixed order: no atomics, the same bits every time.
+#include <algorithm>
+
+#include "iso_attend_tiles.h"
+#include "iso_grad.h"
+
+namespace iso {
+
+namespace {
+
+// L log2(e) and D of every row, 16 lanes a row.
+template <int DT>
+__global__ void __launch_bounds__(256) k_attend_stat(AttnArgs A) {
+  if (blockIdx.x == 0) check_starts(A);
+  const int64_t at = (int64_t)blockIdx.x * 16 + (threadIdx.x >> 4), t = at / A.heads;
+  if (t >= A.tokens_q) return;
+  const Seq s = seq_at(A, A.start_q, t);
+  if (t < s.q0 || t >= s.q0 + s.nq) return;
+  const int h = (int)(at - t * A.heads), head = h / A.group, c = (threadIdx.x & 15) * 8;
+  float sum = 0.0f;
+  if (c < A.dim) {
+    float o[8], g[8];
+    load_elems<DT, 8>(A.out, t * A.ld_out + (int64_t)h * A.dim + c, o);
+    load_elems<DT, 8>(A.dout, t * A.ld_dout + (int64_t)h * A.dim + c, g);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) sum = fmaf(o[j], g[j], sum);
+  }
+#pragma unroll
+  for (int d = 8; d > 0; d >>= 1) sum += __shfl_xor(sum, d);
+  if (c == 0) {
+    const int64_t to = list_of(A, s, head) + (t - s.q0) * A.group + h % A.group;
+    gmem(A.stat)[to] = gmem(A.lse)[at] * kLog2e;
+    gmem(A.stat)[A.tokens_q * A.heads + to] = sum;
+  }
+}
+
+// ---- dQ ------------------------------------------------------------------------------------------------------------
+
+template <int DT, int D>
+constexpr int kDqWaves = DT == ISO_F32 && D == 128 ? 1 : 2;
+
+template <int DT, int D>
+__global__ void __launch_bounds__(256, (kDqWaves<DT, D>)) k_attend_dq(AttnArgs A, Deal deal) {
+  using P = Panel<DT, D>;
+  constexpr int kRows = 32 * kAttnWaves, KT = P::kTiles;
+  extern __shared__ __attribute__((aligned(1024))) uint8_t smem[];
+  int head;
+  uint32_t tile, at;
+  Seq s;
+  if (!dealt<false>(deal, A.heads_kv, blockIdx.x, head, tile)) return;
+  const int piece = (int)(tile % (uint32_t)A.pieces.most);
+  if (!find_tile<false, kRows>(A, tile / (uint32_t)A.pieces.most, s, at)) return;
+
+  const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, half = lane >> 5;
+  const int32_t rows = s.nq * A.group, row0 = (int32_t)at * kRows, end = min(row0 + kRows, rows);
+  const Span all = span_of(A, s, row0, end - 1);
+  const int pieces = pieces_of(all, A.pieces);
+  if (piece >= pieces) return;
+  const int tiles = (all.hi - all.lo + P::kRows - 1) / P::kRows;
+  const int first = __builtin_amdgcn_readfirstlane((int)((int64_t)tiles * piece / pieces));
+  const int last = __builtin_amdgcn_readfirstlane((int)((int64_t)tiles * (piece + 1) / pieces));
+
+  const int32_t r = row0 + 32 * w + (lane & 31), i = r / A.group;
+  const int h = head * A.group + r - i * A.group;
+  const bool on = r < end, busy = row0 + 32 * w < end;
+  int32_t lo = 0, hi = 0;
+  if (on) keys_of(A, s, i, lo, hi);
+  Span mine{0, 0, 0, 0};
+  if (busy) mine = span_of(A, s, row0 + 32 * w, min(row0 + 32 * w + 32, end) - 1);
+  if (row0 + 32 * w + 32 > end) mine.lo_all = INT32_MAX;
+
+  const int64_t col = (int64_t)head * A.dim, to = s.q0 + i;
+  const Rows<DT, D> kr(A.k, s.k0 + all.lo, A.ld_k, col, s.nk - all.lo, A.dim, w, lane);
+  const Rows<DT, D> vr(A.v, s.k0 + all.lo, A.ld_v, col, s.nk - all.lo, A.dim, w, lane);
+  const uint32_t lds = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(lds_u8*)smem);
+  constexpr uint32_t kV = 2 * P::kBytes;   // two panels of keys, then two of values
+  const Reader<DT, D> rd(lds, lane);
+  if (first < last) {
+    kr.load(first, lds, w);
+    vr.load(first, lds + kV, w);
+  }
+  OwnRow<DT, D> q, g;
+  q.load(A.q, to * A.ld_q + (int64_t)h * A.dim, A.dim, half, on);
+  g.load(A.dout, to * A.ld_dout + (int64_t)h * A.dim, A.dim, half, on);
+  const float lse = on ? gmem(A.stat)[list_of(A, s, head) + r] : 0.0f, delta = on ? delta_of(A, s, head, r) : 0.0f;
+
+  f32x16_t dq[D / 32];
+#pragma unroll
+  for (int d = 0; d < D / 32; ++d) dq[d] = 0.0f;
+  auto step = [&](int t, int b) {   // b: the tile's panels
+    landed();
+    kr.load(t + 1, lds + (b ^ 1) * P::kBytes, w);
+    vr.load(t + 1, lds + kV + (b ^ 1) * P::kBytes, w);
+    const int32_t k0 = all.lo + t * P::kRows;
+    if (!busy || k0 >= mine.hi || k0 + P::kRows <= mine.lo) return;
+    const bool whole = k0 >= mine.lo_all && k0 + P::kRows <= mine.hi_all;
+#pragma unroll
+    for (int j = 0; j < KT; ++j) {
+      f32x16_t x = 0.0f, y = -delta;
+#pragma unroll
+      for (int e = 0; e < P::kGroups; ++e) multiply<DT>(rd.row(b * P::kBytes, j, e), q.g[e], x);
+#pragma unroll
+      for (int e = 0; e < P::kGroups; ++e) multiply<DT>(rd.row(kV + b * P::kBytes, j, e), g.g[e], y);
+      Packed<DT> ds;
+#pragma unroll
+      for (int e = 0; e < 16; ++e) x[e] = __builtin_amdgcn_exp2f(fmaf(x[e], A.scale2, -lse)) * y[e];
+      if (!whole) {
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+          const int32_t key = k0 + 32 * j + 8 * (e / 4) + 4 * half + e % 4;
+          x[e] = (uint32_t)(key - lo) < (uint32_t)(hi - lo) ? x[e] : 0.0f;
+        }
+      }
+#pragma unroll
+      for (int e = 0; e < 16; e += 2) ds.set(e / 2, x[e], x[e + 1]);
+      multiply_columns<DT, D>(rd, b * P::kBytes, j, ds, dq);
+    }
+  };
+  for (int t = first; t < last; t += 2) {
+    step(t, 0);
+    if (t + 1 < last) step(t + 1, 1);
+  }
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");   // no load may reach LDS after the workgroup's end
+
+  if (pieces > 1) {
+    if (!on) return;
+    float* const part = A.part + (((int64_t)piece * A.tokens_q + to) * A.heads + h) * kPartLd;
+#pragma unroll
+    for (int d = 0; d < D / 32; ++d)
+#pragma unroll
+      for (int e = 0; e < 16; e += 4) {
+        const int c = 32 * d + 2 * e + 4 * half;
+        if (c < A.dim) store_elems<ISO_F32, 4>(part, c, (const float*)&dq[d] + e);
+      }
+    return;
+  }
+  // what is not finite may have met such a value at a key that the row does not see
+  const bool bad = on && trouble(dq, A.scale) != 0.0f;
+  if (on && !bad) {
+#pragma unroll
+    for (int d = 0; d < D / 32; ++d)
+#pragma unroll
+      for (int e = 0; e < 16; e += 4) {
+        const int c = 32 * d + 2 * e + 4 * half;
+        const float v[4] = {dq[d][e] * A.scale, dq[d][e + 1] * A.scale, dq[d][e + 2] * A.scale, dq[d][e + 3] * A.scale};
+        if (c < A.dim) store_elems<DT, 4>(A.dq, to * A.ld_dq + (int64_t)h * A.dim + c, v);
+      }
+  }
+  for (uint64_t rest = __ballot(bad); rest != 0;) {
+    const int n = __builtin_ctzll(rest) & 31;
+    rest &= ~(0x100000001ull << n);
+    dq_row<DT>(A, s, head, row0 + 32 * w + n, lane);
+  }
+}
+
+// Adds up the pieces of a row, one wave a row.
+template <int DT>
+__global__ void __launch_bounds__(256) k_attend_dq_join(AttnArgs A) {
+  const int64_t at = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6), t = at / A.heads;
+  if (t >= A.tokens_q) return;
+  const Seq s = seq_at(A, A.start_q, t);
+  if (t < s.q0 || t >= s.q0 + s.nq) return;
+  constexpr int kRows = 32 * kAttnWaves;
+  const int h = (int)(at - t * A.heads), head = h / A.group, lane = threadIdx.x & 63;
+  const int32_t r = (int32_t)(t - s.q0) * A.group + h % A.group, row0 = r / kRows * kRows;
+  const Span all = span_of(A, s, row0, min(row0 + kRows, s.nq * A.group) - 1);
+  const int pieces = pieces_of(all, A.pieces);
+  if (pieces == 1) return;
+  const auto part = gmem((const float*)A.part) + at * kPartLd;
+  const int64_t next = A.tokens_q * A.heads * kPartLd;
+  float v[2] = {0.0f, 0.0f};
+#pragma unroll 4
+  for (int p = 0; p < pieces; ++p)
+#pragma unroll
+    for (int c = 0; c < 2; ++c)
+      if (lane + 64 * c < A.dim) v[c] += part[p * next + lane + 64 * c];
+  v[0] *= A.scale, v[1] *= A.scale;
+  if (__any(fmaf(v[0], 0.0f, v[1] * 0.0f) != 0.0f)) return dq_row<DT>(A, s, head, r, lane);
+#pragma unroll
+  for (int c = 0; c < 2; ++c)
+    if (lane + 64 * c < A.dim) store_one<DT>(A.dq, t * A.ld_dq + (int64_t)h * A.dim + lane + 64 * c, v[c]);
+}
+
+// ---- dK and dV -----------------------------------------------------------------------------------------------------
+
+// Panels of a group's list of rows.  Offsets within a panel come from the row that it starts at: row / group and what is left.
+template <class P>
+struct ListRows {
+  const uint8_t* base;
+  int64_t ld, bytes;    // bytes from a token to the next; of all tokens
+  int32_t dim;
+
+  __device__ __forceinline__ ListRows(const void* p, int64_t first, int64_t ld_, int64_t col, const AttnArgs& A, int32_t tokens) {
+    base = (const uint8_t*)p + (first * ld_ + col) * P::kSize;
+    ld = ld_ * P::kSize;
+    bytes = tokens > 0 ? (tokens - 1) * ld + (int64_t)A.group * A.dim * P::kSize : 0;
+    dim = A.dim * P::kSize;
+  }
+  __device__ __forceinline__ u32x4_t buffer(int32_t token) const {
+    u32x4_t b = buffer_of(base + token * ld, min(bytes - token * ld, (int64_t)0x80000000ll));
+#pragma unroll
+    for (int j = 0; j < 4; ++j) b[j] = __builtin_amdgcn_readfirstlane(b[j]);
+    return b;
+  }
+  __device__ __forceinline__ uint32_t offset(uint32_t token, uint32_t in_group, int byte) const {
+    return byte < dim ? token * (uint32_t)ld + in_group * (uint32_t)dim + (uint32_t)byte : kOutside;
+  }
+};
+
+// Workgroup layout of k_attend_dkv.  Two waves a SIMD need 256 registers a lane to do: 128 hold the sums, so that bf16 values
+// stay in LDS and only keys are kept in registers.  fp32 has one wave a SIMD and both in registers.
+template <int DT, int D>
+struct Dkv {
+  using P = Panel<DT, D, 32>;
+  static constexpr bool kValuesInLds = DT == ISO_BF16;
+  static constexpr int kWaves = DT == ISO_F32 ? 1 : 2;
+  static constexpr uint32_t kG = 2 * P::kBytes, kValues = 4 * P::kBytes, kStat = kValues + (kValuesInLds ? 4 * P::kBytes : 0);   // 32 values a wave
+  static constexpr uint32_t kLds = kStat + 512;
+};
+
+template <int DT, int D>
+__global__ void __launch_bounds__(256, (Dkv<DT, D>::kWaves)) k_attend_dkv(AttnArgs A, Deal deal) {
+  using S = Dkv<DT, D>;
+  using P = typename S::P;
+  constexpr int kKeys = 32 * kAttnWaves;
+  extern __shared__ __attribute__((aligned(32768))) uint8_t smem[];   // panels in turn are one bit of an address apart
+  int head;
+  uint32_t tile, at;
+  Seq s;
+  if (!dealt<true>(deal, A.heads_kv, blockIdx.x, head, tile)) return;
+  const int piece = (int)(tile % (uint32_t)A.pieces.most);
+  if (!find_tile<true, kKeys>(A, tile / (uint32_t)A.pieces.most, s, at)) return;
+
+  const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, half = lane >> 5;
+  const int32_t key0 = (int32_t)at * kKeys, end = min(key0 + kKeys, s.nk);
+  const Span all = list_span(A, s, key0, end - 1);
+  const int pieces = pieces_of(all, A.pieces);
+  if (piece >= pieces) return;
+  const int tiles = (all.hi - all.lo + P::kRows - 1) / P::kRows;
+  const int first = __builtin_amdgcn_readfirstlane((int)((int64_t)tiles * piece / pieces));
+  const int last = __builtin_amdgcn_readfirstlane((int)((int64_t)tiles * (piece + 1) / pieces));
+
+  // a lane has one key of its wave's 32, the halves of a wave different rows
+  const int32_t key = key0 + 32 * w + (lane & 31);
+  const bool on = key < end, busy = key0 + 32 * w < end;
+  int32_t lo = 0, hi = 0;
+  if (on) {
+    queries_of(A, s, key, lo, hi);
+    lo *= A.group, hi *= A.group;
+  }
+  Span mine{0, 0, 0, 0};
+  if (busy) mine = list_span(A, s, key0 + 32 * w, min(key0 + 32 * w + 32, end) - 1);
+  if (key0 + 32 * w + 32 > end) mine.lo_all = INT32_MAX;
+
+  const int64_t col = (int64_t)head * A.dim, wide = (int64_t)head * A.group * A.dim, to = s.k0 + key;
+  const ListRows<P> qr(A.q, s.q0, A.ld_q, wide, A, s.nq), gr(A.dout, s.q0, A.ld_dout, wide, A, s.nq);
+  const uint32_t lds = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(lds_u8*)smem);
+  const float* const stat = A.stat + list_of(A, s, head) + all.lo;
+  // of a panel's rows, L in eight lanes' pieces and D in the next eight
+  const uint32_t stat_at = lane < 8 ? lane * 16 : lane < 16 ? (uint32_t)(A.tokens_q * A.heads * 4) + (lane - 8) * 16 : kOutside;
+  const uint32_t inverse = A.group > 1 ? 0xFFFFFFFFu / (uint32_t)A.group + 1 : 0;   // x / group = x inverse / 2^32 for small x
+  auto load = [&](int t, int b) {   // into panels b
+    if (t >= last) return;
+    const int32_t r0 = all.lo + t * P::kRows, token0 = r0 / A.group, rest = r0 - token0 * A.group;
+    const u32x4_t qb = qr.buffer(token0), gb = gr.buffer(token0);
+    const uint32_t to = lds + b * P::kBytes;
+#pragma unroll
+    for (int j = 0; j < P::kLoads; ++j) {
+      int row, byte;
+      P::source(j, w, lane, row, byte);
+      const uint32_t x = rest + row, token = A.group > 1 ? __umulhi(x, inverse) : x, in_group = x - token * A.group;
+      load_lds(qb, to + (j * kAttnWaves + w) * 1024, qr.offset(token, in_group, byte));
+      load_lds(gb, to + S::kG + (j * kAttnWaves + w) * 1024, gr.offset(token, in_group, byte));
+    }
+    if (w == 0 && lane < 16) {   // 256 bytes
+      u32x4_t sb = buffer_of((const uint8_t*)(stat + t * P::kRows), 0x80000000ll);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) sb[j] = __builtin_amdgcn_readfirstlane(sb[j]);
+      load_lds(sb, lds + S::kStat + b * 256, stat_at);
+    }
+  };
+  Reader<DT, D> rd(lds, lane);
+  OwnRow<DT, D> k, v;
+  if constexpr (S::kValuesInLds) {
+    const Rows<DT, D, P> vr(A.v, s.k0 + key0, A.ld_v, col, end - key0, A.dim, w, lane);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) vr.load(j, lds + S::kValues + j * P::kBytes, w);
+  } else {
+    v.load(A.v, to * A.ld_v + col, A.dim, half, on);
+  }
+  load(first, 0);
+  k.load(A.k, to * A.ld_k + col, A.dim, half, on);
+  const Reader<DT, D> own(lds + S::kValues + w * P::kBytes, lane);
+
+  f32x16_t dk[D / 32], dv[D / 32];
+#pragma unroll
+  for (int d = 0; d < D / 32; ++d) dk[d] = 0.0f, dv[d] = 0.0f;
+
+  auto sees = [&](int32_t r0, int e) { return (uint32_t)(r0 + 8 * (e / 4) + 4 * half + e % 4 - lo) < (uint32_t)(hi - lo); };
+  uint32_t of = lds + S::kStat + 16 * half;
+  constexpr uint32_t qp = 0, gp = S::kG;
+  for (int t = first; t < last; ++t) {
+    landed();
+    load(t + 1, (t - first + 1) & 1);
+    const int32_t r0 = all.lo + t * P::kRows;
+    if (!busy || r0 >= mine.hi || r0 + P::kRows <= mine.lo) {
+      rd.swap(P::kBytes);
+      of ^= 256;
+      continue;
+    }
+    const bool whole = r0 >= mine.lo_all && r0 + P::kRows <= mine.hi_all;
+    f32x16_t x = 0.0f, y = 0.0f;
+    Packed<DT> p, ds;
+    rd.again();
+    if constexpr (DT == ISO_BF16) {
+      // Fragments are read some products ahead, in the order laid out here: S and dP by rows, dV and dK by columns.  Left to
+      // itself the compiler reads a whole product's ahead, for which there are no registers.
+      constexpr int G = P::kGroups, N = 2 * P::kDims, kAhead = 3, kAll = 2 * G + 2 * N;
+      u32x4_t ring[kAhead], vf[2];
+      auto read = [&](int n) {
+        if (n < G) ring[n % kAhead] = rd.row(qp, 0, n);
+        else if (n < 2 * G) ring[n % kAhead] = rd.row(gp, 0, n - G);
+        else if (n < 2 * G + N) ring[n % kAhead] = __builtin_bit_cast(u32x4_t, rd.col(gp, 0, (n - 2 * G) / (N / 2), (n - 2 * G) % (N / 2)));
+        else if (n < kAll) ring[n % kAhead] = __builtin_bit_cast(u32x4_t, rd.col(qp, 0, (n - 2 * G - N) / (N / 2), (n - 2 * G - N) % (N / 2)));
+      };
+#pragma unroll
+      for (int n = 0; n < kAhead; ++n) read(n);
+#pragma unroll
+      for (int n = 0; n < G; ++n) {
+        multiply<DT>(ring[n % kAhead], k.g[n], x);
+        read(n + kAhead);
+        if (n >= G - 2) vf[n & 1] = own.row(0, 0, n - (G - 2));
+        __builtin_amdgcn_sched_barrier(0);
+      }
+      f32x4_t lse = *(lds_f32x4)(uintptr_t)of;
+#pragma unroll
+      for (int n = 0; n < G; ++n) {
+        multiply<DT>(ring[(G + n) % kAhead], vf[n & 1], y);
+        read(G + n + kAhead);
+        if (n + 2 < G) vf[n & 1] = own.row(0, 0, n + 2);
+#pragma unroll
+        for (int e = 16 / G * n; e < 16 / G * (n + 1); ++e) {
+          x[e] = __builtin_amdgcn_exp2f(fmaf(x[e], A.scale2, -lse[e % 4]));
+          if (e % 4 == 3 && e < 15) lse = *(lds_f32x4)(uintptr_t)(of + 8 * (e + 1));
+        }
+        __builtin_amdgcn_sched_barrier(0);
+      }
+#pragma unroll
+      for (int e = 0; e < 16; e += 4) {
+        const f32x4_t delta = *(lds_f32x4)(uintptr_t)(of + 128 + 8 * e);
+#pragma unroll
+        for (int c = 0; c < 4; ++c) y[e + c] = x[e + c] * (y[e + c] - delta[c]);
+      }
+      if (!whole) {   // of both: 0 times what is not seen may be NaN
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+          const bool on = sees(r0, e);
+          x[e] = on ? x[e] : 0.0f, y[e] = on ? y[e] : 0.0f;
+        }
+      }
+#pragma unroll
+      for (int e = 0; e < 16; e += 4) {
+        p.set(e / 2, x[e], x[e + 1]), p.set(e / 2 + 1, x[e + 2], x[e + 3]);
+        ds.set(e / 2, y[e], y[e + 1]), ds.set(e / 2 + 1, y[e + 2], y[e + 3]);
+      }
+      __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int n = 0; n < N; ++n) {
+        multiply<DT>(ring[(2 * G + n) % kAhead], p.s[n / (N / 2)], dv[n % (N / 2)]);
+        read(2 * G + n + kAhead);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+#pragma unroll
+      for (int n = 0; n < N; ++n) {
+        multiply<DT>(ring[(2 * G + N + n) % kAhead], ds.s[n / (N / 2)], dk[n % (N / 2)]);
+        read(2 * G + N + n + kAhead);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+    } else {
+#pragma unroll
+      for (int e = 0; e < P::kGroups; ++e) multiply<DT>(rd.row(qp, 0, e), k.g[e], x);
+#pragma unroll
+      for (int e = 0; e < P::kGroups; ++e) multiply<DT>(rd.row(gp, 0, e), v.g[e], y);
+#pragma unroll
+      for (int e = 0; e < 16; e += 4) {
+        const f32x4_t lse = *(lds_f32x4)(uintptr_t)(of + 8 * e), delta = *(lds_f32x4)(uintptr_t)(of + 128 + 8 * e);
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+          x[e + c] = __builtin_amdgcn_exp2f(fmaf(x[e + c], A.scale2, -lse[c]));
+          y[e + c] = x[e + c] * (y[e + c] - delta[c]);
+          if (!whole && !sees(r0, e + c)) x[e + c] = 0.0f, y[e + c] = 0.0f;
+        }
+      }
+#pragma unroll
+      for (int e = 0; e < 16; e += 2) p.set(e / 2, x[e], x[e + 1]), ds.set(e / 2, y[e], y[e + 1]);
+      multiply_columns<DT, D>(rd, gp, 0, p, dv);
+      multiply_columns<DT, D>(rd, qp, 0, ds, dk);
+    }
+    rd.swap(P::kBytes);
+    of ^= 256;
+  }
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");   // no load may reach LDS after the workgroup's end
+
+  if (pieces > 1) {
+    if (!on) return;
+    float* const part = A.part + (((int64_t)piece * A.tokens_k + to) * A.heads_kv + head) * (2 * kPartLd);
+#pragma unroll
+    for (int d = 0; d < D / 32; ++d)
+#pragma unroll
+      for (int e = 0; e < 16; e += 4) {
+        const int c = 32 * d + 2 * e + 4 * half;
+        if (c >= A.dim) continue;
+        store_elems<ISO_F32, 4>(part, c, (const float*)&dk[d] + e);
+        store_elems<ISO_F32, 4>(part, kPartLd + c, (const float*)&dv[d] + e);
+      }
+    return;
+  }
+  const bool bad = on && fmaf(trouble(dk, A.scale), 1.0f, trouble(dv, 1.0f)) != 0.0f;
+  if (on && !bad) {
+#pragma unroll
+    for (int d = 0; d < D / 32; ++d)
+#pragma unroll
+      for (int e = 0; e < 16; e += 4) {
+        const int c = 32 * d + 2 * e + 4 * half;
+        if (c >= A.dim) continue;
+        const float x[4] = {dk[d][e] * A.scale, dk[d][e + 1] * A.scale, dk[d][e + 2] * A.scale, dk[d][e + 3] * A.scale};
+        store_elems<DT, 4>(A.dk, to * A.ld_dk + col + c, x);
+        store_elems<DT, 4>(A.dv, to * A.ld_dv + col + c, (const float*)&dv[d] + e);
+      }
+  }
+  for (uint64_t rest = __ballot(bad); rest != 0;) {
+    const int n = __builtin_ctzll(rest) & 31;
+    rest &= ~(0x100000001ull << n);
+    dkv_row<DT>(A, s, head, key0 + 32 * w + n, lane);
+  }
+}
+
+// Adds up the pieces of a key, one wave a key and kv head.
+template <int DT>
+__global__ void __launch_bounds__(256) k_attend_dkv_join(AttnArgs A) {
+  const int64_t at = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6), t = at / A.heads_kv;
+  if (t >= A.tokens_k) return;
+  const Seq s = seq_at(A, A.start_k, t);
+  if (t < s.k0 || t >= s.k0 + s.nk) return;
+  constexpr int kKeys = 32 * kAttnWaves;
+  const int head = (int)(at - t * A.heads_kv), lane = threadIdx.x & 63;
+  const int32_t key = (int32_t)(t - s.k0), key0 = key / kKeys * kKeys;
+  const Span all = list_span(A, s, key0, min(key0 + kKeys, s.nk) - 1);
+  const int pieces = pieces_of(all, A.pieces);
+  if (pieces == 1) return;
+  const auto part = gmem((const float*)A.part) + at * (2 * kPartLd);
+  const int64_t next = A.tokens_k * A.heads_kv * (2 * kPartLd), col = (int64_t)head * A.dim;
+  float v[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll 4
+  for (int p = 0; p < pieces; ++p)
+#pragma unroll
+    for (int c = 0; c < 4; ++c)
+      if (lane + 64 * (c & 1) < A.dim) v[c] += part[p * next + (c >> 1) * kPartLd + lane + 64 * (c & 1)];
+  v[0] *= A.scale, v[1] *= A.scale;
+  if (__any(v[0] * 0.0f + v[1] * 0.0f + v[2] * 0.0f + v[3] * 0.0f != 0.0f)) return dkv_row<DT>(A, s, head, key, lane);
+#pragma unroll
+  for (int c = 0; c < 2; ++c) {
+    if (lane + 64 * c >= A.dim) continue;
+    store_one<DT>(A.dk, t * A.ld_dk + col + lane + 64 * c, v[c]);
+    store_one<DT>(A.dv, t * A.ld_dv + col + lane + 64 * c, v[2 + c]);
+  }
+}
+
+template <int DT, int D>
+hipError_t backward(AttnArgs A, const AttendPlan& plan, uint8_t* ws, hipStream_t s) {
+  const unsigned rows = (unsigned)((A.tokens_q * A.heads + 3) / 4), keys = (unsigned)((A.tokens_k * A.heads_kv + 3) / 4);
+  A.stat = (float*)(ws + kStatusBytes);
+  A.part = (float*)(ws + plan.part);
+  k_attend_stat<DT><<<std::max(1u, (rows + 3) / 4), 256, 0, s>>>(A);
+  A.pieces = plan.rows;
+  const Deal dq = deal_of(A.heads_kv, (uint32_t)(attend_tiles(A.tokens_q * A.group, A.sequences) * A.pieces.most));
+  if (rows > 0) k_attend_dq<DT, D><<<deal_grid(dq, A.heads_kv), 256, 4 * Panel<DT, D>::kBytes, s>>>(A, dq);
+  if (rows > 0 && A.pieces.most > 1) k_attend_dq_join<DT><<<rows, 256, 0, s>>>(A);
+  A.pieces = plan.keys;
+  const Deal dkv = deal_of(A.heads_kv, (uint32_t)(attend_tiles(A.tokens_k, A.sequences) * A.pieces.most));
+  if (keys > 0) k_attend_dkv<DT, D><<<deal_grid(dkv, A.heads_kv), 256, Dkv<DT, D>::kLds, s>>>(A, dkv);
+  if (keys > 0 && A.pieces.most > 1) k_attend_dkv_join<DT><<<keys, 256, 0, s>>>(A);
+  return hipGetLastError();
+}
+
+template <int DT>
+hipError_t backward(const AttnArgs& A, const AttendPlan& plan, uint8_t* ws, hipStream_t s) {
+  return A.dim > 64 ? backward<DT, 128>(A, plan, ws, s) : backward<DT, 64>(A, plan, ws, s);
+}
+
+}  // namespace
+
+hipError_t run_attend_grad(const iso_attn& a, int dt, uint8_t* ws, hipStream_t s) {
+  const AttnArgs A = args_of(a, ws);
+  const AttendPlan plan = plan_attend(a, true);
+  return dt == ISO_BF16 ? backward<ISO_BF16>(A, plan, ws, s) : backward<ISO_F32>(A, plan, ws, s);
+}
+
+}  // namespace iso

@@ -13,15 +13,15 @@ namespace iso {
 
 constexpr int kAttnWaves = 4;
 
-// Panels of kRows token rows of D dimensions (head dimensions up to D, the rest zero), 16 KiB; a row's 16-byte pieces are
+// Panels of kRows token rows of D dimensions (head dimensions up to D, the rest zero); a row's 16-byte pieces are
 // permuted (piece p at p ^ mix(row)), so that 16 successive rows have the same piece in different banks, and so have four
 // successive rows 64 bytes next to each other (bf16) or two rows four apart 128 bytes (fp32).
-template <int DT, int D>
+template <int DT, int D, int ROWS = DT == ISO_BF16 ? 64 : 32>
 struct Panel {
   static constexpr int kSize = DT == ISO_BF16 ? 2 : 4;
   static constexpr int kRowBytes = D * kSize;
   static constexpr int kPieces = kRowBytes / 16;
-  static constexpr int kRows = D == 128 ? (DT == ISO_BF16 ? 64 : 32) : (DT == ISO_BF16 ? 64 : 32);
+  static constexpr int kRows = ROWS;
   static constexpr int kBytes = kRows * kRowBytes;
   static constexpr int kLoads = kBytes / (1024 * kAttnWaves);   // 16-byte loads a lane
   static constexpr int kTiles = kRows / 32;                     // 32-row tiles
@@ -45,9 +45,9 @@ struct Panel {
 constexpr uint32_t kOutside = 0xC0000000u;   // an offset behind the end of every buffer
 
 // One operand's rows in memory, loaded panel by panel: `row` 0 of a kv head of a sequence and how many there are.
-template <int DT, int D>
+template <int DT, int D, class PANEL = Panel<DT, D>>
 struct Rows {
-  using P = Panel<DT, D>;
+  using P = PANEL;
   const uint8_t* base;
   int64_t step, bytes;   // bytes of a panel's rows, and from row 0 on to the end of the last row
   uint32_t offset[P::kLoads];
@@ -77,35 +77,33 @@ struct Rows {
 typedef __attribute__((address_space(3))) const u32x4_t* lds_piece;
 typedef __attribute__((address_space(3))) const float* lds_float;
 
-// Where a lane reads a panel's fragments: rows, 16 bytes a group, for the product that sums over dimensions; and columns, for
-// the one that sums over rows.
+// Where a lane reads fragments of panels: rows, 16 bytes a group, for products that sum over dimensions; and columns, for those
+// that sum over rows.  Groups, 32-dimension tiles and rows are bits of the permuted piece, so one exclusive or makes each address
+// from the lane's first, and which panel it is goes into the instruction.
 template <int DT, int D>
 struct Reader {
   using P = Panel<DT, D>;
-  uint32_t row0;        // its row and half, for tile 0
-  int key;              // mix of that row
-  uint32_t col0[P::kDims];
+  uint32_t row0, col0;
 
-  __device__ __forceinline__ explicit Reader(int lane) {
+  __device__ __forceinline__ Reader(uint32_t lds, int lane) {
     const int r = lane & 31, half = lane >> 5, i = lane & 15, g = lane >> 4;
-    row0 = r * P::kRowBytes;
-    key = P::mix(r) ^ half;
-#pragma unroll
-    for (int d = 0; d < P::kDims; ++d) {
-      if constexpr (DT == ISO_BF16) {
-        // 16 lanes read a block of four rows by 16 columns and get a column each
-        const int row = 4 * (g >> 1) + (i >> 2), byte = d * 64 + (g & 1) * 32 + (i & 3) * 8;
-        col0[d] = row * P::kRowBytes + ((byte / 16) ^ P::mix(row)) * 16 + byte % 16;
-      } else {
-        const int row = 4 * half;
-        col0[d] = row * P::kRowBytes + (((d * 32 + r) / 4) ^ P::mix(row)) * 16 + (r % 4) * 4;
-      }
+    row0 = lds + r * P::kRowBytes + (P::mix(r) ^ half) * 16;
+    if constexpr (DT == ISO_BF16) {
+      // 16 lanes read a block of four rows by 16 columns and get a column each
+      const int row = 4 * (g >> 1) + (i >> 2), byte = (g & 1) * 32 + (i & 3) * 8;
+      col0 = lds + row * P::kRowBytes + ((byte / 16) ^ P::mix(row)) * 16 + byte % 16;
+    } else {
+      const int row = 4 * half;
+      col0 = lds + row * P::kRowBytes + ((r / 4) ^ P::mix(row)) * 16 + (r % 4) * 4;
     }
   }
-  // 16 bytes of group g of the lane's row of tile t.
+  // Addresses are worked out where they are used: kept from one tile to the next they would take sixteen registers.
+  __device__ __forceinline__ void again() { asm volatile("" : "+v"(row0), "+v"(col0)); }
+  // Over to the panel `bytes` (a power of two) on, or back.
+  __device__ __forceinline__ void swap(uint32_t bytes) { row0 ^= bytes, col0 ^= bytes; }
+  // 16 bytes of group g of the lane's row of tile t of the panel `panel` bytes on.
   __device__ __forceinline__ u32x4_t row(uint32_t panel, int t, int g) const {
-    const int p = (2 * g) ^ key;   // half is part of key
-    return *(lds_piece)(uintptr_t)(panel + t * 32 * P::kRowBytes + row0 + p * 16);
+    return *(lds_piece)(uintptr_t)((row0 ^ (32 * g)) + (panel + t * 32 * P::kRowBytes));
   }
   // bf16: dimensions 32 d + lane % 32 of rows 16 s + 4 half + {0..3, 8..11} of tile t.
   __device__ __forceinline__ bf16x8_t col(uint32_t panel, int t, int s, int d) const {
@@ -114,16 +112,15 @@ struct Reader {
     } f;
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
-      // rows 16 s + 8 h on: mix changes by bit 3 of the row (bits 2 and 3 of a row are its lower bits)
-      const uint32_t at = panel + (t * 32 + 16 * s + 8 * h) * P::kRowBytes + (col0[d] ^ (h ? P::mix(8) * 16 : 0));
+      const uint32_t at = (col0 ^ (64 * d ^ (h ? P::mix(8) * 16 : 0))) + (panel + (t * 32 + 16 * s + 8 * h) * P::kRowBytes);
       f.h[h] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_frag)(uintptr_t)at);
     }
     return __builtin_bit_cast(bf16x8_t, f);
   }
   // fp32: dimension 32 d + lane % 32 of row 8 g + 4 half + e of tile t.
   __device__ __forceinline__ float one(uint32_t panel, int t, int g, int e, int d) const {
-    const uint32_t x = (uint32_t)(P::mix((8 * g) & 15) ^ P::mix(e)) * 16;
-    return *(lds_float)(uintptr_t)(panel + (t * 32 + 8 * g + e) * P::kRowBytes + (col0[d] ^ x));
+    const uint32_t x = (uint32_t)(P::mix((8 * g) & 15) ^ P::mix(e)) * 16 ^ 128 * d;
+    return *(lds_float)(uintptr_t)((col0 ^ x) + (panel + (t * 32 + 8 * g + e) * P::kRowBytes));
   }
 };
 
@@ -187,6 +184,11 @@ __device__ __forceinline__ void multiply_columns(const Reader<DT, D>& r, uint32_
   }
 }
 
+template <int N>
+struct Const {
+  static constexpr int value = N;
+};
+
 // All loads into LDS have landed and all LDS reads are done, of every wave.
 __device__ __forceinline__ void landed() { asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
 
@@ -196,8 +198,8 @@ __device__ __forceinline__ float other_half(float v) { return __shfl_xor(v, 32);
 // ---- which tile a workgroup has ------------------------------------------------------------------------------------
 
 // Work is a list of tiles of rows for every kv head.  Workgroup b runs on XCD b % 8: heads are dealt to as many classes of XCDs
-// as divide them evenly, so that a head's keys and values are read through few L2 caches, and a class takes the tiles of a head
-// from the last (which sees most under a causal mask) to the first, its XCDs in turn.
+// as divide them evenly, so that a head's keys and values are read through few L2 caches, and a class takes the tiles of a head,
+// its XCDs in turn, from those on that have most to do under a causal mask: the last rows, the first keys.
 struct Deal {
   int32_t classes, per;   // classes of XCDs, XCDs of a class
   uint32_t tiles;         // tiles of a head (or an upper bound), times the pieces of each
@@ -212,11 +214,12 @@ inline uint32_t deal_grid(const Deal& d, int heads) {
   const uint64_t n = (uint64_t)(heads / d.classes) * d.tiles;
   return (uint32_t)((n + d.per - 1) / d.per * 8);
 }
+template <bool KEYS>
 __device__ __forceinline__ bool dealt(const Deal& d, int heads, uint32_t b, int& head, uint32_t& tile) {
   const uint32_t x = b & 7u, c = x % d.classes, j = (b >> 3) * d.per + x / d.classes, h = j / d.tiles;
   if (h >= (uint32_t)(heads / d.classes)) return false;
   head = (int)(c + d.classes * h);
-  tile = d.tiles - 1 - (j - h * d.tiles);
+  tile = KEYS ? j - h * d.tiles : d.tiles - 1 - (j - h * d.tiles);
   return true;
 }
 
@@ -253,6 +256,43 @@ __device__ __forceinline__ bool find_tile(const AttnArgs& A, uint32_t tile, Seq&
     before += __shfl(sum, 63);
   }
   return false;
+}
+
+// The sequence whose range holds row t; a sequence without rows where there is none.
+__device__ __forceinline__ Seq seq_at(const AttnArgs& A, const int32_t* start, int64_t t) {
+  if (A.sequences == 0) return Seq{};
+  int32_t lo = 0, hi = A.sequences - 1;
+  while (lo < hi) {   // the first sequence that ends behind t
+    const int32_t m = (lo + hi) / 2;
+    if (gmem(start)[m + 1] > t) hi = m;
+    else lo = m + 1;
+  }
+  return seq_of(A, lo);
+}
+
+// Keys that the rows of a tile (or of a wave of it) see between them, and those that all of them see.
+struct Span {
+  int32_t lo, hi, lo_all, hi_all;
+};
+// Bounds grow with the query, so those of the first and last row do for all.
+__device__ __forceinline__ Span span_of(const AttnArgs& A, const Seq& s, int64_t first, int64_t last) {
+  Span x;
+  keys_of(A, s, first / A.group, x.lo, x.hi_all);
+  keys_of(A, s, last / A.group, x.lo_all, x.hi);
+  return x;
+}
+
+// The same of the rows of a group's list that see the keys of a tile.
+__device__ __forceinline__ Span list_span(const AttnArgs& A, const Seq& s, int32_t first, int32_t last) {
+  Span x;
+  queries_of(A, s, first, x.lo, x.hi_all);
+  queries_of(A, s, last, x.lo_all, x.hi);
+  return Span{x.lo * A.group, x.hi * A.group, x.lo_all * A.group, x.hi_all * A.group};
+}
+
+// Pieces that the keys (or rows) [lo, hi) of a tile are shared out to.
+__device__ __forceinline__ int pieces_of(const Span& x, const Pieces& p) {
+  return min(p.most, max(1, (x.hi - x.lo + p.keys - 1) / p.keys));
 }
 
 // Whether the values of a wave hold a NaN or an infinity: 0 times such a value is NaN, and a sum with one stays one.

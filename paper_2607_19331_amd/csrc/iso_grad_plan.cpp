@@ -2,6 +2,7 @@
 #include "iso_grad_plan.h"
 
 #include <algorithm>
+#include <cmath>
 
 namespace iso {
 
@@ -214,20 +215,56 @@ size_t weight_grad_workspace_bytes(const iso_weight_grad* g, int n, int dt) {
 bool attend_fits(const iso_attn& a) {
   // a row (query head) a wave of 64 lanes in launches of fewer than 2^32 threads
   const int64_t most = 1ll << 25;
+  if (a.heads / a.heads_kv > ISO_ATTN_MAX_GROUP) return false;
   return a.tokens_q <= most && a.tokens_k <= most && a.heads <= most && a.tokens_q * a.heads <= most && a.tokens_k * a.heads_kv <= most;
 }
 
-// Pieces where they fit into the partial sums' share of the workspace, which few rows do: a call of many rows fills the card.
-int attend_pieces(const iso_attn& a) {
-  const int64_t rows = std::max<int64_t>(1, a.tokens_q * a.heads), by_keys = (a.tokens_k + kPieceKeys - 1) / kPieceKeys;
-  return (int)std::max<int64_t>(1, std::min({(int64_t)kMostKeyPieces, by_keys, kPartRows / rows}));
+namespace {
+
+constexpr int kPieceKeys = 256;         // fewest keys of a piece
+constexpr int kMostPieces = 64;         // of a tile
+constexpr int64_t kFullTiles = 2048;    // four rounds of workgroups, two a CU: heavy tiles first, these balance by themselves
+
+// Tiles of `owners` rows walk over `length` keys on average.  In p pieces a tile's time falls by p, and every row writes and
+// reads p partial sums: the sum of both is least at p = f sqrt(length / owners), where f was measured to be about 12.8 for rows
+// and 9.1 for keys (twice the sums).  Microseconds, forward pass in 1 to 16 pieces: see the pieces' table in iso_attend.hip.
+Pieces share_out(int64_t owners, int64_t list, int64_t sequences, int64_t heads, double f) {
+  Pieces P;
+  if (owners <= 0 || list <= 0 || sequences <= 0) return P;
+  const int64_t tiles = std::max(owners / kAttnTileRows, sequences * heads), length = (list + sequences - 1) / sequences;
+  int64_t p = (int64_t)(f * std::sqrt((double)length / (double)owners));
+  p = std::min({p, kFullTiles / std::max<int64_t>(1, tiles), (list + kPieceKeys - 1) / kPieceKeys, (int64_t)kMostPieces});
+  if (p <= 1) return P;
+  P.most = (int32_t)p;
+  P.keys = (int32_t)std::max<int64_t>(kPieceKeys, length / (2 * p));   // sequences differ in length
+  return P;
+}
+// Partial sums that a call of up to so many owners and keys may take, whatever its sequences.
+size_t most_parts(int64_t owners, int64_t list, double f) {
+  if (owners <= 0 || list <= 0) return 0;
+  const double each = (double)std::min<int64_t>(kMostPieces, (list + kPieceKeys - 1) / kPieceKeys);
+  return (size_t)std::min({f * std::sqrt((double)list * (double)owners), (double)owners * each, (double)(kFullTiles + 1) * kAttnTileRows});
 }
 
-size_t attend_workspace_bytes(const iso_attn& a, int, bool grad) {
-  const int64_t rows = a.tokens_q * a.heads;
-  if (grad) return kStatusBytes + align_up(sizeof(float) * (size_t)rows, 256);
-  const int64_t by_keys = std::max<int64_t>(1, std::min<int64_t>(kMostKeyPieces, (a.tokens_k + kPieceKeys - 1) / kPieceKeys));
-  return kStatusBytes + align_up(sizeof(float) * kPartLd * (size_t)std::min(kPartRows, rows * by_keys), 256);
+}  // namespace
+
+AttendPlan plan_attend(const iso_attn& a, bool grad) {
+  const int64_t rows = a.tokens_q * a.heads, keys = a.tokens_k * a.heads_kv, list = a.tokens_q * (a.heads / a.heads_kv);
+  constexpr double kRows = 12.8, kKeys = 9.1;
+  AttendPlan P;
+  P.rows = share_out(rows, a.tokens_k, a.sequences, a.heads_kv, kRows);
+  size_t parts = most_parts(rows, a.tokens_k, kRows);
+  P.part = kStatusBytes;
+  if (grad) {
+    P.keys = share_out(keys, list, a.sequences, a.heads_kv, kKeys);
+    parts = std::max(parts, 2 * most_parts(keys, list, kKeys));
+    // a panel's rows are read whole: up to 32 behind the last one
+    P.part = align_up(kStatusBytes + sizeof(float) * (2 * (size_t)rows + 64), 256);
+  }
+  P.total = P.part + align_up(sizeof(float) * kPartLd * parts, 256);
+  return P;
 }
+
+size_t attend_workspace_bytes(const iso_attn& a, int, bool grad) { return plan_attend(a, grad).total; }
 
 }  // namespace iso

@@ -157,15 +157,22 @@ size_t weight_grad_workspace_bytes(const iso_weight_grad* g, int n, int dt);
 // Whether the rows of a call and its launches stay within 32 bits.
 bool attend_fits(const iso_attn& a);
 
-constexpr int kAttnTileRows = 128;     // rows (queries times the group) of a tile
-constexpr int kPieceKeys = 256;        // fewest keys of a piece of a tile
-constexpr int kMostKeyPieces = 64;     // of a tile
-constexpr int64_t kPartRows = 1 << 16; // rows of all pieces of a call
+constexpr int kAttnTileRows = 128;     // rows (queries times the group) or keys of a tile
 constexpr int kPartLd = 132;           // floats of a row's piece: its sums, maximum and sum of weights
 
 // Tiles of `rows` rows in `sequences` sequences at most.
 inline int64_t attend_tiles(int64_t rows, int64_t sequences) { return rows / kAttnTileRows + sequences; }
-int attend_pieces(const iso_attn& a);
+
+// How the keys (or rows) that a tile walks over are shared out: `most` pieces, each of at least `keys`.
+struct Pieces {
+  int32_t most = 1, keys = 1;
+};
+
+struct AttendPlan {
+  Pieces rows, keys;   // of tiles of rows (O, dQ) and of keys (dK and dV)
+  size_t part = 0, total = 0;
+};
+AttendPlan plan_attend(const iso_attn& a, bool grad);
 size_t attend_workspace_bytes(const iso_attn& a, int dt, bool grad);
 
 // ---- distillation --------------------------------------------------------------------------------------------------
