@@ -28,33 +28,46 @@ struct DistillArgs {
   void* grad;
   int64_t tokens, vocab, ld, ld_grad, pad_id;
   int32_t top, id_type, pieces;   // pieces: workgroups a row
-  float inv_t;                    // 1 / T
+  float inv_t, exp2_t;            // 1 / T and log2(e) / T
   double t;
   float* part;                    // maximum and sum of a piece (scaled by 1 / T), tokens x pieces
   uint32_t* status;
 };
 
-// Maximum of x and sum of 2^((x - maximum) log2 e), for values and for pairs of these.
+// Maximum m of some logits, and the sum of exp((z - m) / T) = 2^((z - m) c), c = log2(e) / T.
 struct Lse {
   float m = -INFINITY, s = 0.0f;
 };
-__device__ __forceinline__ float exp_of(float x) { return __builtin_amdgcn_exp2f(x * kLog2e); }
-__device__ __forceinline__ Lse join(Lse a, Lse b) {
-  const float m = fmaxf(a.m, b.m), ref = m == -INFINITY ? 0.0f : m;
-  // a NaN sum stays one; so does infinity, whose own term is exp(inf - inf)
-  return Lse{m, a.s * exp_of(a.m - ref) + b.s * exp_of(b.m - ref)};
+__device__ __forceinline__ float finite_or_zero(float m) { return m == -INFINITY ? 0.0f : m; }
+// A NaN sum stays one; so does infinity, whose own term is exp(inf - inf).
+__device__ __forceinline__ Lse join(Lse a, Lse b, float c) {
+  const float m = fmaxf(a.m, b.m), ref = finite_or_zero(m);
+  return Lse{m, a.s * __builtin_amdgcn_exp2f((a.m - ref) * c) + b.s * __builtin_amdgcn_exp2f((b.m - ref) * c)};
 }
 
 template <int N>
-__device__ __forceinline__ Lse block_lse(Lse v, float (*lds)[2]) {
+__device__ __forceinline__ Lse block_lse(Lse v, float c, float (*lds)[2]) {
 #pragma unroll
-  for (int d = 32; d > 0; d >>= 1) v = join(v, Lse{__shfl_xor(v.m, d), __shfl_xor(v.s, d)});
+  for (int d = 32; d > 0; d >>= 1) v = join(v, Lse{__shfl_xor(v.m, d), __shfl_xor(v.s, d)}, c);
   if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6][0] = v.m, lds[threadIdx.x >> 6][1] = v.s;
   __syncthreads();
   v = Lse{lds[0][0], lds[0][1]};
 #pragma unroll
-  for (int i = 1; i < N / 64; ++i) v = join(v, Lse{lds[i][0], lds[i][1]});
+  for (int i = 1; i < N / 64; ++i) v = join(v, Lse{lds[i][0], lds[i][1]}, c);
   return v;
+}
+
+// Adds values to a maximum and sum, which is scaled once for all of them.
+template <int N>
+__device__ __forceinline__ void add_to(Lse& l, const float* v, float c) {
+  float top = l.m;
+#pragma unroll
+  for (int j = 0; j < N; ++j) top = fmaxf(top, v[j]);
+  const float ref = finite_or_zero(top), ref2 = ref * c;
+  float s = l.s * __builtin_amdgcn_exp2f((l.m - ref) * c);
+#pragma unroll
+  for (int j = 0; j < N; ++j) s += __builtin_amdgcn_exp2f(fmaf(v[j], c, -ref2));
+  l = Lse{top, s};
 }
 
 __device__ __forceinline__ int64_t id_at(const DistillArgs& A, int64_t i) {
@@ -104,17 +117,17 @@ __device__ __forceinline__ Entry list_of(const DistillArgs& A, int64_t row, List
       if (A.tokens * A.top > kFewEntries) atomicOr(A.status, kStatusIndex);
     } else if (id != A.pad_id && v != -INFINITY) {
       r.id = (int32_t)id;
-      y = v * A.inv_t;
+      y = v;
     }
   }
   // the first four waves hold the entries
   Lse l{y, r.id >= 0 ? 1.0f : 0.0f};
   if (r.id >= 0 && !(fabsf(y) < INFINITY)) l.s = NAN;   // an infinite or NaN logit of the teacher
-  l = block_lse<256>(l, S.red);
+  l = block_lse<256>(l, A.exp2_t, S.red);
   any = l.s != 0.0f;
   if (r.id >= 0) {
-    r.log_t = (y - l.m) - logf(l.s);
-    r.t = exp_of(r.log_t);
+    r.log_t = (y - l.m) * A.inv_t - logf(l.s);
+    r.t = __builtin_amdgcn_exp2f(r.log_t * kLog2e);
   }
   if (e < ISO_DISTILL_MAX_TOP) S.id[e] = r.id, S.t[e] = r.t;
   __syncthreads();
@@ -157,71 +170,105 @@ __device__ __forceinline__ float load_z(const DistillArgs& A, int64_t i) {
   else return f32_from_bits(gmem((const uint32_t*)A.z)[i]);
 }
 
+// One piece of 16 bytes at the end of a row: minus infinity behind it, which has no part in a maximum or a sum.
+template <int DT>
+__device__ __forceinline__ u32x4_t load_end(const void* p, int64_t i, int64_t left) {
+  constexpr int V = kVec<DT>;
+  constexpr uint32_t none = DT == ISO_BF16 ? 0xFF80FF80u : 0xFF800000u;
+  u32x4_t w = {none, none, none, none};
+  if (left >= V) return load_raw<DT>(p, i);
+  if (left <= 0) return w;
+  const u32x4_t x = load_raw<DT>(p, i, left);
+#pragma unroll
+  for (int j = 0; j < V; ++j) {
+    const uint32_t m = DT == ISO_BF16 ? 0xFFFFu << (16 * (j & 1)) : 0xFFFFFFFFu;
+    if (j < left) w[j * 4 / V] = (w[j * 4 / V] & ~m) | (x[j * 4 / V] & m);
+  }
+  return w;
+}
+
 // Maximum and sum over columns [lo, hi) of a row, a workgroup of 256.
 template <int DT>
 __device__ __forceinline__ Lse row_lse(const DistillArgs& A, int64_t row, int64_t lo, int64_t hi, float (*lds)[2]) {
-  constexpr int V = kVec<DT>, U = 4;
+  constexpr int V = kVec<DT>, U = 4, kStride = 256 * V;
   const int64_t base = row * A.ld;
   Lse l;
-  auto add = [&](const float* v, int n) {
-    float top = l.m;
-#pragma unroll
-    for (int j = 0; j < U * V; ++j)
-      if (j < n) top = fmaxf(top, v[j] * A.inv_t);
-    const float ref = top == -INFINITY ? 0.0f : top;
-    float s = l.s * exp_of(l.m - ref);
-#pragma unroll
-    for (int j = 0; j < U * V; ++j)
-      if (j < n) s += exp_of(fmaf(v[j], A.inv_t, -ref));
-    l = Lse{top, s};
-  };
   int64_t c = lo + (int64_t)threadIdx.x * V;
-  for (; c + (U - 1) * 256 * V + V <= hi; c += U * 256 * V) {
+  for (; c + (U - 1) * kStride + V <= hi; c += U * kStride) {
     u32x4_t w[U];
 #pragma unroll
-    for (int u = 0; u < U; ++u) w[u] = load_raw<DT>(A.z, base + c + u * 256 * V);
+    for (int u = 0; u < U; ++u) w[u] = load_raw<DT>(A.z, base + c + u * kStride);
     float v[U * V];
 #pragma unroll
     for (int u = 0; u < U; ++u) unpack_raw<DT>(w[u], v + u * V);
-    add(v, U * V);
+    add_to<U * V>(l, v, A.exp2_t);
   }
-  for (; c < hi; c += 256 * V) {
-    float v[U * V];
-    unpack_raw<DT>(load_raw<DT>(A.z, base + c, hi - c), v);
-    add(v, (int)min((int64_t)V, hi - c));
+  for (; c < hi; c += kStride) {
+    float v[V];
+    unpack_raw<DT>(load_end<DT>(A.z, base + c, hi - c), v);
+    add_to<V>(l, v, A.exp2_t);
   }
-  return block_lse<256>(l, lds);
+  return block_lse<256>(l, A.exp2_t, lds);
 }
 
-// The gradient over columns [lo, hi) of a row, a workgroup of N.  Entries' own values are written after the others'.
-template <int DT, int N>
-__device__ __forceinline__ void row_grad(const DistillArgs& A, int64_t row, int64_t lo, int64_t hi, const Entry& r, float z, float lse,
-                                         bool any) {
-  constexpr int V = kVec<DT>;
-  const int64_t from = row * A.ld, to = row * A.ld_grad;
-  const float w = A.w != nullptr ? gmem(A.w)[row] : 1.0f, f = w * (float)A.t;
-  const bool zero = !any || w == 0.0f;
-  // the gradient may lie over the logits: entries have theirs before anything is written
-  asm volatile("s_waitcnt vmcnt(0)" ::"v"(z) : "memory");
-  __syncthreads();
-  for (int64_t c = lo + (int64_t)threadIdx.x * V; c < hi; c += N * V) {
-    float v[V];
-    load_elems<DT, V>(A.z, from + c, v, hi - c);
-#pragma unroll
-    for (int j = 0; j < V; ++j) v[j] = zero ? 0.0f : f * exp_of(fmaf(v[j], A.inv_t, -lse));
-    store_elems<DT, V>(A.grad, to + c, v, hi - c);
+// L of a row, in binary64: the loss takes differences of it.
+__device__ __forceinline__ double lse_of(const DistillArgs& A, Lse l) { return (double)l.m / A.t + log((double)l.s); }
+
+// A row's factor w T, and whether its gradient is zero.
+struct Factor {
+  float f;
+  bool zero;
+  __device__ __forceinline__ Factor(const DistillArgs& A, int64_t row, bool any) {
+    const float w = A.w != nullptr ? gmem(A.w)[row] : 1.0f;
+    f = w * (float)A.t;
+    zero = !any || w == 0.0f;
   }
+};
+
+// The gradients of 16 bytes of logits; lse2 = L log2(e).
+template <int DT>
+__device__ __forceinline__ void grads_of(const DistillArgs& A, float f, u32x4_t w, float lse2, float* v) {
+  unpack_raw<DT>(w, v);
+#pragma unroll
+  for (int j = 0; j < kVec<DT>; ++j) v[j] = f * __builtin_amdgcn_exp2f(fmaf(v[j], A.exp2_t, -lse2));
+}
+
+// Entries' own gradients, written after all of the row's: columns [lo, hi).
+template <int DT>
+__device__ __forceinline__ void put_entry(const DistillArgs& A, int64_t row, int64_t lo, int64_t hi, const Factor& F, const Entry& r, float z,
+                                          float lse2) {
   asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
   __syncthreads();
-  if (!zero && r.first && r.id >= lo && r.id < hi) {
-    const float v = f * (exp_of(fmaf(z, A.inv_t, -lse)) - r.t);
-    if constexpr (DT == ISO_BF16) gmem((uint16_t*)A.grad)[to + r.id] = (uint16_t)pack_bf16(v, 0.0f);
-    else gmem((uint32_t*)A.grad)[to + r.id] = bits_from_f32(v);
+  if (F.zero || !r.first || r.id < lo || r.id >= hi) return;
+  const float v = F.f * (__builtin_amdgcn_exp2f(fmaf(z, A.exp2_t, -lse2)) - r.t);
+  const int64_t to = row * A.ld_grad + r.id;
+  if constexpr (DT == ISO_BF16) gmem((uint16_t*)A.grad)[to] = (uint16_t)pack_bf16(v, 0.0f);
+  else gmem((uint32_t*)A.grad)[to] = bits_from_f32(v);
+}
+
+// The gradient of 16 bytes a lane from column c on, U of them 256 lanes apart, of a row of A.vocab columns.
+template <int DT, int U, bool STREAM>
+__device__ __forceinline__ void put_grads(const DistillArgs& A, int64_t row, int64_t c, const Factor& F, const u32x4_t* w, float lse2) {
+  constexpr int V = kVec<DT>, kStride = 256 * V;
+  const int64_t to = row * A.ld_grad;
+#pragma unroll
+  for (int u = 0; u < U; ++u) {
+    const int64_t at = c + u * kStride;
+    if (at >= A.vocab) continue;
+    float v[V] = {};
+    if (!F.zero) grads_of<DT>(A, F.f, w[u], lse2, v);
+    store_elems<DT, V, STREAM>(A.grad, to + at, v, A.vocab - at);
   }
+}
+
+// Every entry of the row has its logit before anything is written: the gradient may lie over the logits.
+__device__ __forceinline__ void before_writes(float z) {
+  asm volatile("s_waitcnt vmcnt(0)" ::"v"(z) : "memory");
+  __syncthreads();
 }
 
 // Loss (and gradient) of a row, one workgroup: two walks over the row where both are asked for.
-template <int DT>
+template <int DT, bool STREAM>
 __global__ void __launch_bounds__(256) k_distill_row(DistillArgs A) {
   __shared__ ListSpace S;
   __shared__ double sums[4];
@@ -232,11 +279,80 @@ __global__ void __launch_bounds__(256) k_distill_row(DistillArgs A) {
   bool any;
   Entry r = list_of<256>(A, row, S, any);
   const float z = r.id >= 0 ? load_z<DT>(A, row * A.ld + r.id) : 0.0f;
-  const double lse = (double)l.m + log((double)l.s);
+  const double lse = lse_of(A, l);
   store_loss<DT>(A, row, r, z, lse, any, sums);
   if (A.grad == nullptr) return;
+  constexpr int V = kVec<DT>, U = 4;
   merge(A, S, r);
-  row_grad<DT, 256>(A, row, 0, A.vocab, r, z, (float)lse, any);
+  const Factor F(A, row, any);
+  const float lse2 = (float)(lse * 1.4426950408889634);
+  before_writes(z);
+  for (int64_t c = (int64_t)threadIdx.x * V; c < A.vocab; c += U * 256 * V) {
+    u32x4_t w[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) w[u] = load_end<DT>(A.z, row * A.ld + c + u * 256 * V, A.vocab - (c + u * 256 * V));
+    put_grads<DT, U, STREAM>(A, row, c, F, w, lse2);
+  }
+  put_entry<DT>(A, row, 0, A.vocab, F, r, z, lse2);
+}
+
+// Loss and gradient of a row that a workgroup of N holds in registers, PER pieces of 16 bytes a lane: read once, written once.
+// All of a row is under way at once; what a CU does between its loads and its stores, other CUs' loads and stores fill.
+template <int DT, int N, int PER, bool STREAM>
+__global__ void __launch_bounds__(N) k_distill_held(DistillArgs A) {
+  constexpr int V = kVec<DT>;
+  __shared__ ListSpace S;
+  __shared__ double sums[4];
+  const int64_t row = blockIdx.x, from = row * A.ld, to = row * A.ld_grad;
+  const int32_t vocab = (int32_t)A.vocab;
+  if (row == 0 && A.tokens * A.top <= kFewEntries) check_ids(A);
+  // the first column of a round is the same in all lanes and goes into the instruction's base
+  using bits = typename Fmt<DT>::bits_t;
+  const uint32_t mine = threadIdx.x * V;
+  u32x4_t w[PER];
+#pragma unroll
+  for (int p = 0; p < PER; ++p) {
+    const bits* const at = (const bits*)A.z + from + p * N * V;
+    if ((p + 1) * N * V <= vocab) w[p] = load_raw<DT>(at, mine);
+    else w[p] = load_end<DT>(at, mine, vocab - p * N * V - (int32_t)mine);
+  }
+  // what is unpacked is unpacked again where it is needed next: there are registers for the row, not for its values twice over
+  auto again = [&] {
+#pragma unroll
+    for (int p = 0; p < PER; ++p) asm volatile("" : "+v"(w[p]));
+  };
+  Lse l;
+#pragma unroll
+  for (int p = 0; p < PER; p += 2) {   // as they come in, one after the other
+    asm volatile("" : "+v"(w[p]), "+v"(w[p + 1]), "+v"(l.s));
+    float v[2 * V];
+#pragma unroll
+    for (int u = 0; u < 2; ++u) unpack_raw<DT>(w[p + u], v + u * V);
+    add_to<2 * V>(l, v, A.exp2_t);
+  }
+  again();
+  bool any;
+  Entry r = list_of<N>(A, row, S, any);
+  const float z = r.id >= 0 ? load_z<DT>(A, from + r.id) : 0.0f;
+  __syncthreads();   // list_of's space again
+  const double lse = lse_of(A, block_lse<N>(l, A.exp2_t, S.red));
+  store_loss<DT>(A, row, r, z, lse, any, sums);
+  merge(A, S, r);
+  const Factor F(A, row, any);
+  const float lse2 = (float)(lse * 1.4426950408889634);
+  before_writes(z);
+#pragma unroll
+  for (int p = 0; p < PER; ++p) {
+    asm volatile("" : "+v"(w[p]));
+    bits* const at = (bits*)A.grad + to + p * N * V;
+    const int32_t left = vocab - p * N * V - (int32_t)mine;
+    if (left <= 0) continue;
+    float v[V] = {};
+    if (!F.zero) grads_of<DT>(A, F.f, w[p], lse2, v);
+    if ((p + 1) * N * V <= vocab) store_elems<DT, V, STREAM>(at, mine, v);
+    else store_elems<DT, V, STREAM>(at, mine, v, left);
+  }
+  put_entry<DT>(A, row, 0, vocab, F, r, z, lse2);
 }
 
 // A piece of a row: its share of the sum, and from these the loss.
@@ -257,26 +373,41 @@ __global__ void __launch_bounds__(256) k_distill_join(DistillArgs A) {
   Lse l;
   for (int i = threadIdx.x; i < A.pieces; i += 256) {
     const auto p = gmem((const float*)A.part) + 2 * (row * A.pieces + i);
-    l = join(l, Lse{p[0], p[1]});
+    l = join(l, Lse{p[0], p[1]}, A.exp2_t);
   }
-  l = block_lse<256>(l, S.red);
+  l = block_lse<256>(l, A.exp2_t, S.red);
   __syncthreads();
   bool any;
   const Entry r = list_of<256>(A, row, S, any);
   const float z = r.id >= 0 ? load_z<DT>(A, row * A.ld + r.id) : 0.0f;
-  store_loss<DT>(A, row, r, z, (double)l.m + log((double)l.s), any, sums);
+  store_loss<DT>(A, row, r, z, lse_of(A, l), any, sums);
 }
 
-// The gradient of a piece of a row from the row's L.
+// The gradient of a piece of a row from the row's L: kGradPiece columns a workgroup, four loads a lane, which are under way
+// while the list is looked at.
 template <int DT>
-__global__ void __launch_bounds__(256) k_distill_grad(DistillArgs A, int64_t each) {
+constexpr int kGradPiece = 4 * 256 * kVec<DT>;
+
+template <int DT, bool STREAM>
+__global__ void __launch_bounds__(256) k_distill_grad(DistillArgs A, uint32_t pieces, bool check) {
+  constexpr int V = kVec<DT>;
   __shared__ ListSpace S;
-  const int64_t row = blockIdx.x / A.pieces, lo = (blockIdx.x - row * A.pieces) * each;
+  if (blockIdx.x == 0 && check) check_ids(A);
+  const int64_t row = blockIdx.x / pieces, lo = (int64_t)(blockIdx.x - (uint32_t)row * pieces) * kGradPiece<DT>;
+  const int64_t c = lo + (int64_t)threadIdx.x * V;
+  u32x4_t w[4];
+#pragma unroll
+  for (int u = 0; u < 4; ++u) w[u] = load_end<DT>(A.z, row * A.ld + c + u * 256 * V, A.vocab - (c + u * 256 * V));
   bool any;
   Entry r = list_of<256>(A, row, S, any);
-  const float z = r.id >= 0 ? load_z<DT>(A, row * A.ld + r.id) : 0.0f;
-  merge(A, S, r);
-  row_grad<DT, 256>(A, row, lo, min(lo + each, A.vocab), r, z, gmem(A.lse)[row], any);
+  const bool here = r.id >= lo && r.id < lo + kGradPiece<DT>;
+  const float z = here ? load_z<DT>(A, row * A.ld + r.id) : 0.0f;
+  if (here) merge(A, S, r);
+  const Factor F(A, row, any);
+  const float lse2 = gmem(A.lse)[row] * kLog2e;
+  before_writes(z);
+  put_grads<DT, 4, STREAM>(A, row, c, F, w, lse2);
+  put_entry<DT>(A, row, lo, lo + kGradPiece<DT>, F, r, z, lse2);
 }
 
 DistillArgs args_of(const iso_distill& d, uint8_t* ws) {
@@ -284,36 +415,62 @@ DistillArgs args_of(const iso_distill& d, uint8_t* ws) {
   A.z = d.logits, A.ids = d.ids, A.y = d.teacher, A.w = d.weight, A.loss = d.loss, A.lse = d.lse, A.grad = d.grad;
   A.tokens = d.tokens, A.vocab = d.vocab, A.ld = d.ld, A.ld_grad = d.ld_grad, A.pad_id = d.pad_id;
   A.top = d.top, A.id_type = d.id_type;
-  A.inv_t = (float)(1.0 / d.temperature), A.t = d.temperature;
+  A.inv_t = (float)(1.0 / d.temperature), A.exp2_t = (float)(1.4426950408889634 / d.temperature), A.t = d.temperature;
   A.status = (uint32_t*)ws;
   A.part = (float*)(ws + kStatusBytes);
   return A;
 }
 
-template <int DT>
-void loss(const DistillArgs& A, hipStream_t s) {
-  k_distill_row<DT><<<(unsigned)A.tokens, 256, 0, s>>>(A);
+// Workgroups that a row is shared out to where there are few, a piece 8 KiB at least; and columns of a piece.
+int64_t share_out(DistillArgs& A, int dt) {
+  const int64_t least = 8192 / (dt == ISO_BF16 ? 2 : 4), most = std::max<int64_t>(1, kMostPieces / 2 / A.tokens);
+  A.pieces = (int32_t)std::min((A.vocab + least - 1) / least, most);
+  const int64_t each = (A.vocab + A.pieces - 1) / A.pieces;
+  return (each + 7) / 8 * 8;
 }
 
-template <int DT>
-void gradient(DistillArgs A, hipStream_t s) {
-  A.pieces = 1;
-  k_distill_grad<DT><<<(unsigned)A.tokens, 256, 0, s>>>(A, A.vocab);
+template <int DT, bool STREAM>
+void gradient(const DistillArgs& A, bool check, hipStream_t s) {
+  const uint32_t pieces = (uint32_t)((A.vocab + kGradPiece<DT> - 1) / kGradPiece<DT>);
+  k_distill_grad<DT, STREAM><<<(unsigned)(A.tokens * pieces), 256, 0, s>>>(A, pieces, check);
 }
+
+template <int DT, bool STREAM>
+void loss(DistillArgs A, hipStream_t s) {
+  constexpr int V = kVec<DT>;
+  const int64_t each = share_out(A, DT);
+  if (A.pieces > 4 || (A.pieces > 1 && A.grad == nullptr)) {
+    k_distill_part<DT><<<(unsigned)(A.tokens * A.pieces), 256, 0, s>>>(A, each);
+    k_distill_join<DT><<<(unsigned)A.tokens, 256, 0, s>>>(A);
+    if (A.grad != nullptr) gradient<DT, STREAM>(A, false, s);
+    return;
+  }
+  const unsigned n = (unsigned)A.tokens;
+  if (A.grad == nullptr || A.vocab > 1024 * 20 * V) k_distill_row<DT, STREAM><<<n, 256, 0, s>>>(A);
+  else if (A.vocab <= 256 * 4 * V) k_distill_held<DT, 256, 4, STREAM><<<n, 256, 0, s>>>(A);
+  else if (A.vocab <= 256 * 20 * V) k_distill_held<DT, 256, 20, STREAM><<<n, 256, 0, s>>>(A);
+  else if (A.vocab <= 512 * 20 * V) k_distill_held<DT, 512, 20, STREAM><<<n, 512, 0, s>>>(A);
+  else k_distill_held<DT, 1024, 20, STREAM><<<n, 1024, 0, s>>>(A);
+}
+
+bool streams(const DistillArgs& A, int dt) { return A.grad != nullptr && streamed(A.tokens * A.vocab * (dt == ISO_BF16 ? 2 : 4)); }
 
 }  // namespace
 
 hipError_t run_distill_loss(const iso_distill& d, int dt, uint8_t* ws, hipStream_t s) {
   const DistillArgs A = args_of(d, ws);
   if (A.tokens == 0 || A.tokens * A.top > kFewEntries) k_distill_clear<<<1, 1, 0, s>>>(A.status);
-  if (A.tokens > 0) dt == ISO_BF16 ? loss<ISO_BF16>(A, s) : loss<ISO_F32>(A, s);
+  if (A.tokens > 0) streams(A, dt) ? (dt == ISO_BF16 ? loss<ISO_BF16, true>(A, s) : loss<ISO_F32, true>(A, s))
+                                  : (dt == ISO_BF16 ? loss<ISO_BF16, false>(A, s) : loss<ISO_F32, false>(A, s));
   return hipGetLastError();
 }
 
 hipError_t run_distill_grad(const iso_distill& d, int dt, uint8_t* ws, hipStream_t s) {
   const DistillArgs A = args_of(d, ws);
-  if (A.tokens == 0 || A.tokens * A.top > kFewEntries) k_distill_clear<<<1, 1, 0, s>>>(A.status);
-  if (A.tokens > 0) dt == ISO_BF16 ? gradient<ISO_BF16>(A, s) : gradient<ISO_F32>(A, s);
+  const bool few = A.tokens * A.top <= kFewEntries;
+  if (A.tokens == 0 || !few) k_distill_clear<<<1, 1, 0, s>>>(A.status);
+  if (A.tokens > 0) streams(A, dt) ? (dt == ISO_BF16 ? gradient<ISO_BF16, true>(A, few, s) : gradient<ISO_F32, true>(A, few, s))
+                                  : (dt == ISO_BF16 ? gradient<ISO_BF16, false>(A, few, s) : gradient<ISO_F32, false>(A, few, s));
   return hipGetLastError();
 }
 
