@@ -9,7 +9,7 @@ namespace iso {
 namespace {
 
 template <int DT, int D>
-__global__ void __launch_bounds__(256, 2) k_attend(AttnArgs A, Deal deal) {
+__global__ void __launch_bounds__(256, (DT == ISO_F32 && D == 128 ? 1 : 2)) k_attend(AttnArgs A, Deal deal) {
   using P = Panel<DT, D>;
   constexpr int kRows = 32 * kAttnWaves, KT = P::kTiles;
   extern __shared__ __attribute__((aligned(1024))) uint8_t smem[];
@@ -59,6 +59,7 @@ __global__ void __launch_bounds__(256, 2) k_attend(AttnArgs A, Deal deal) {
 #pragma unroll
   for (int d = 0; d < D / 32; ++d) o[d] = 0.0f;
   float m = -INFINITY, l = 0.0f;   // running maximum (times log2 e) and sum of a lane's row, the sum of its half's keys
+  float top = -INFINITY;           // of the scores at hand, times log2 e
 
   auto scores = [&](f32x16_t (&x)[KT], int b) {
 #pragma unroll
@@ -68,16 +69,31 @@ __global__ void __launch_bounds__(256, 2) k_attend(AttnArgs A, Deal deal) {
       for (int g = 0; g < P::kGroups; ++g) multiply<DT>(rd.row(b * P::kBytes, j, g), q.g[g], x[j]);
     }
   };
-  auto needed = [&](int t) {   // keys of the tile that a row of the wave sees
-    const int32_t k0 = all.lo + t * P::kRows;
-    return busy && k0 < mine.hi && k0 + P::kRows > mine.lo;
+  auto most = [&](const f32x16_t (&x)[KT]) {
+    float v = x[0][0];
+#pragma unroll
+    for (int j = 0; j < KT; ++j)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) v = fmaxf(v, x[j][e]);
+    return both_halves(v) * A.scale2;
   };
+  auto follow = [&] {   // the sums so far are scaled to a new reference where the maximum has grown by much
+    if (__any(top > m + kSlack)) {
+      const float up = fmaxf(m, top), f = __builtin_amdgcn_exp2f(m - (up == -INFINITY ? 0.0f : up));
+      m = up;
+      l *= f;
+#pragma unroll
+      for (int d = 0; d < D / 32; ++d) o[d] *= f;
+    }
+    return m == -INFINITY ? 0.0f : m;
+  };
+  // Probabilities of a tile and their product with V, and the next tile's scores, under whose products the exponentials run; the
+  // next maximum is taken under the products with V.  Laid out by hand, one fragment read and a share of the rest a product.  One
+  // way through for all tiles (those that the wave sees nothing of as well): sums that meet from two ways cost registers.
   auto step = [&](f32x16_t (&x)[KT], f32x16_t (&next)[KT], int t, int b) {   // b: the tile's panels
     landed();   // K of t + 1 and V of t, loaded a step ago; K of t and V of t - 1 are free
     kr.load(t + 2, lds + b * P::kBytes, w);
     vr.load(t + 1, lds + kV + (b ^ 1) * P::kBytes, w);
-    if (needed(t + 1)) scores(next, b ^ 1);
-    if (!needed(t)) return;
     const int32_t k0 = all.lo + t * P::kRows;
     if (k0 < mine.lo_all || k0 + P::kRows > mine.hi_all) {
 #pragma unroll
@@ -87,45 +103,86 @@ __global__ void __launch_bounds__(256, 2) k_attend(AttnArgs A, Deal deal) {
           const int32_t key = k0 + 32 * j + 8 * (e / 4) + 4 * half + e % 4;
           x[j][e] = (uint32_t)(key - lo) < (uint32_t)(hi - lo) ? x[j][e] : -INFINITY;
         }
+      top = most(x);
     }
-    float top = x[0][0];
+    const float ref = follow();
+    if constexpr (DT == ISO_BF16) {
+      constexpr int G = P::kGroups, N = D / 32, kS = KT * G, kO = 2 * KT * N, kAhead = 3;
+      u32x4_t ring[kAhead];
+      auto read = [&](int n) {
+        if (n < kS) ring[n % kAhead] = rd.row((b ^ 1) * P::kBytes, n / G, n % G);
+        else if (n < kS + kO) ring[n % kAhead] = __builtin_bit_cast(u32x4_t, rd.col(kV + b * P::kBytes, (n - kS) / (2 * N), (n - kS) / N % 2, (n - kS) % N));
+      };
 #pragma unroll
-    for (int j = 0; j < KT; ++j)
+      for (int n = 0; n < kAhead; ++n) read(n);
+      Packed<DT> p[KT];
 #pragma unroll
-      for (int e = 0; e < 16; ++e) top = fmaxf(top, x[j][e]);
-    top = fmaxf(top, other_half(top)) * A.scale2;
-    if (__any(top > m + kSlack)) {   // the sums so far are scaled to a new reference
-      const float up = fmaxf(m, top), f = __builtin_amdgcn_exp2f(m - (up == -INFINITY ? 0.0f : up));
-      m = up;
-      l *= f;
+      for (int j = 0; j < KT; ++j) next[j] = 0.0f;
 #pragma unroll
-      for (int d = 0; d < D / 32; ++d) o[d] *= f;
-    }
-    const float ref = m == -INFINITY ? 0.0f : m;
+      for (int n = 0; n < kS; ++n) {
+        multiply<DT>(ring[n % kAhead], q.g[n % G], next[n / G]);
+        read(n + kAhead);
+        constexpr int E = KT * 16 / kS;
 #pragma unroll
-    for (int j = 0; j < KT; ++j) {
-      Packed<DT> p;
-#pragma unroll
-      for (int e = 0; e < 16; e += 2) {
-        const float a = __builtin_amdgcn_exp2f(fmaf(x[j][e], A.scale2, -ref)), b = __builtin_amdgcn_exp2f(fmaf(x[j][e + 1], A.scale2, -ref));
-        l += a;
-        l += b;
-        p.set(e / 2, a, b);
+        for (int e = E * n; e < E * (n + 1); e += 2) {
+          const float u = __builtin_amdgcn_exp2f(fmaf(x[e / 16][e % 16], A.scale2, -ref));
+          const float v = __builtin_amdgcn_exp2f(fmaf(x[e / 16][e % 16 + 1], A.scale2, -ref));
+          l += u;
+          l += v;
+          p[e / 16].set(e % 16 / 2, u, v);
+        }
+        __builtin_amdgcn_sched_barrier(0);
       }
-      multiply_columns<DT, D>(rd, kV + b * P::kBytes, j, p, o);
+      float v = next[0][0];
+#pragma unroll
+      for (int n = 0; n < kO; ++n) {
+        multiply<DT>(ring[(kS + n) % kAhead], p[n / (2 * N)].s[n / N % 2], o[n % N]);
+        read(kS + n + kAhead);
+        constexpr int E = KT * 16 / kO;
+#pragma unroll
+        for (int e = E * n; e < E * (n + 1); ++e) v = fmaxf(v, next[e / 16][e % 16]);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+      top = both_halves(v) * A.scale2;
+    } else {
+      scores(next, b ^ 1);
+#pragma unroll
+      for (int j = 0; j < KT; ++j) {
+        Packed<DT> p;
+#pragma unroll
+        for (int e = 0; e < 16; e += 2) {
+          const float u = __builtin_amdgcn_exp2f(fmaf(x[j][e], A.scale2, -ref)), v = __builtin_amdgcn_exp2f(fmaf(x[j][e + 1], A.scale2, -ref));
+          l += u;
+          l += v;
+          p.set(e / 2, u, v);
+        }
+        multiply_columns<DT, D>(rd, kV + b * P::kBytes, j, p, o);
+      }
+      top = most(next);
     }
   };
 
   if (first < last) {
     landed();
-    if (needed(first)) scores(x0, 0);
-    for (int t = first; t < last; t += 2) {
-      step(x0, x1, t, 0);
-      if (t + 1 < last) step(x1, x0, t + 1, 1);
+    if (busy) {
+      scores(x0, 0);
+      top = most(x0);
+      for (int t = first; t < last; t += 2) {
+        step(x0, x1, t, 0);
+        if (t + 1 == last) break;
+        step(x1, x0, t + 1, 1);
+      }
+    } else {   // a wave without rows has its share of the loads
+      for (int t = first; t < last; ++t) {
+        const int b = (t - first) & 1;
+        landed();
+        kr.load(t + 2, lds + b * P::kBytes, w);
+        vr.load(t + 1, lds + kV + (b ^ 1) * P::kBytes, w);
+      }
     }
   }
   asm volatile("s_waitcnt vmcnt(0)" ::: "memory");   // no load may reach LDS after the workgroup's end
-  l += other_half(l);
+  l = sum_of_halves(l);
 
   const int64_t to = s.q0 + i;
   if (pieces > 1) {   // k_attend_join adds the pieces up

@@ -192,8 +192,15 @@ struct Const {
 // All loads into LDS have landed and all LDS reads are done, of every wave.
 __device__ __forceinline__ void landed() { asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
 
-// The value of the lane with the same column in the other half.
-__device__ __forceinline__ float other_half(float v) { return __shfl_xor(v, 32); }
+// A value and that of the lane with the same column in the other half.
+__device__ __forceinline__ float both_halves(float v) {
+  const auto r = __builtin_amdgcn_permlane32_swap(bits_from_f32(v), bits_from_f32(v), false, false);
+  return fmaxf(f32_from_bits(r[0]), f32_from_bits(r[1]));
+}
+__device__ __forceinline__ float sum_of_halves(float v) {
+  const auto r = __builtin_amdgcn_permlane32_swap(bits_from_f32(v), bits_from_f32(v), false, false);
+  return f32_from_bits(r[0]) + f32_from_bits(r[1]);
+}
 
 // ---- which tile a workgroup has ------------------------------------------------------------------------------------
 
