@@ -41,16 +41,17 @@ __global__ void __launch_bounds__(256, (DT == ISO_F32 && D == 128 ? 1 : 2)) k_at
   if (row0 + 32 * w + 32 > end) mine.lo_all = INT32_MAX;   // rows past the end see nothing
 
   const int64_t col = (int64_t)head * A.dim;
-  const Rows<DT, D> kr(A.k, s.k0 + all.lo, A.ld_k, col, s.nk - all.lo, A.dim, w, lane);
-  const Rows<DT, D> vr(A.v, s.k0 + all.lo, A.ld_v, col, s.nk - all.lo, A.dim, w, lane);
+  Rows<DT, D> kr(A.k, s.k0 + all.lo, A.ld_k, col, s.nk - all.lo, A.dim, w, lane);
+  Rows<DT, D> vr(A.v, s.k0 + all.lo, A.ld_v, col, s.nk - all.lo, A.dim, w, lane);
   const uint32_t lds = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(lds_u8*)smem);
   constexpr uint32_t kV = 2 * P::kBytes;   // two panels of keys, then two of values
   const Reader<DT, D> rd(lds, lane);
 
+  kr.skip(first), vr.skip(first);
   if (first < last) {
-    kr.load(first, lds, w);
-    vr.load(first, lds + kV, w);
-    kr.load(first + 1, lds + P::kBytes, w);
+    kr.load(lds, w);
+    vr.load(lds + kV, w);
+    kr.load(lds + P::kBytes, w);
   }
   OwnRow<DT, D> q;
   q.load(A.q, (s.q0 + i) * A.ld_q + (int64_t)h * A.dim, A.dim, half, on);
@@ -92,8 +93,8 @@ __global__ void __launch_bounds__(256, (DT == ISO_F32 && D == 128 ? 1 : 2)) k_at
   // way through for all tiles (those that the wave sees nothing of as well): sums that meet from two ways cost registers.
   auto step = [&](f32x16_t (&x)[KT], f32x16_t (&next)[KT], int t, int b) {   // b: the tile's panels
     landed();   // K of t + 1 and V of t, loaded a step ago; K of t and V of t - 1 are free
-    kr.load(t + 2, lds + b * P::kBytes, w);
-    vr.load(t + 1, lds + kV + (b ^ 1) * P::kBytes, w);
+    kr.load(lds + b * P::kBytes, w);
+    vr.load(lds + kV + (b ^ 1) * P::kBytes, w);
     const int32_t k0 = all.lo + t * P::kRows;
     if (k0 < mine.lo_all || k0 + P::kRows > mine.hi_all) {
 #pragma unroll
@@ -176,8 +177,8 @@ __global__ void __launch_bounds__(256, (DT == ISO_F32 && D == 128 ? 1 : 2)) k_at
       for (int t = first; t < last; ++t) {
         const int b = (t - first) & 1;
         landed();
-        kr.load(t + 2, lds + b * P::kBytes, w);
-        vr.load(t + 1, lds + kV + (b ^ 1) * P::kBytes, w);
+        kr.load(lds + b * P::kBytes, w);
+        vr.load(lds + kV + (b ^ 1) * P::kBytes, w);
       }
     }
   }

@@ -75,27 +75,30 @@ __global__ void __launch_bounds__(256, (kDqWaves<DT, D>)) k_attend_dq(AttnArgs A
   if (row0 + 32 * w + 32 > end) mine.lo_all = INT32_MAX;
 
   const int64_t col = (int64_t)head * A.dim, to = s.q0 + i;
-  const Rows<DT, D> kr(A.k, s.k0 + all.lo, A.ld_k, col, s.nk - all.lo, A.dim, w, lane);
-  const Rows<DT, D> vr(A.v, s.k0 + all.lo, A.ld_v, col, s.nk - all.lo, A.dim, w, lane);
+  Rows<DT, D> kr(A.k, s.k0 + all.lo, A.ld_k, col, s.nk - all.lo, A.dim, w, lane);
+  Rows<DT, D> vr(A.v, s.k0 + all.lo, A.ld_v, col, s.nk - all.lo, A.dim, w, lane);
   const uint32_t lds = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(lds_u8*)smem);
   constexpr uint32_t kV = 2 * P::kBytes;   // two panels of keys, then two of values
   const Reader<DT, D> rd(lds, lane);
+  kr.skip(first), vr.skip(first);
   if (first < last) {
-    kr.load(first, lds, w);
-    vr.load(first, lds + kV, w);
+    kr.load(lds, w);
+    vr.load(lds + kV, w);
   }
   OwnRow<DT, D> q, g;
   q.load(A.q, to * A.ld_q + (int64_t)h * A.dim, A.dim, half, on);
   g.load(A.dout, to * A.ld_dout + (int64_t)h * A.dim, A.dim, half, on);
   const float lse = on ? gmem(A.stat)[list_of(A, s, head) + r] : 0.0f, delta = on ? delta_of(A, s, head, r) : 0.0f;
+  q.arrive(), g.arrive();
+  asm volatile("" ::"v"(lse), "v"(delta));
 
   f32x16_t dq[D / 32];
 #pragma unroll
   for (int d = 0; d < D / 32; ++d) dq[d] = 0.0f;
   auto step = [&](int t, int b) {   // b: the tile's panels
     landed();
-    kr.load(t + 1, lds + (b ^ 1) * P::kBytes, w);
-    vr.load(t + 1, lds + kV + (b ^ 1) * P::kBytes, w);
+    kr.load(lds + (b ^ 1) * P::kBytes, w);
+    vr.load(lds + kV + (b ^ 1) * P::kBytes, w);
     const int32_t k0 = all.lo + t * P::kRows;
     if (!busy || k0 >= mine.hi || k0 + P::kRows <= mine.lo) return;
     const bool whole = k0 >= mine.lo_all && k0 + P::kRows <= mine.hi_all;
@@ -188,27 +191,48 @@ __global__ void __launch_bounds__(256) k_attend_dq_join(AttnArgs A) {
 
 // ---- dK and dV -----------------------------------------------------------------------------------------------------
 
-// Panels of a group's list of rows.  Offsets within a panel come from the row that it starts at: row / group and what is left.
+// Panels of a group's list of rows, of q and of dO.  Offsets within a panel come from the row that it starts at, by its query and
+// its place in the group: row / group and what is left.
 template <class P>
 struct ListRows {
-  const uint8_t* base;
-  int64_t ld, bytes;    // bytes from a token to the next; of all tokens
-  int32_t dim;
+  const uint8_t *q, *g;           // at the first query of the panel
+  int64_t q_left, g_left;         // bytes from there on to the end of the last query's
+  int32_t q_ld, g_ld, dim, group, rest;
+  uint32_t byte[P::kLoads];
+  int32_t row[P::kLoads];
 
-  __device__ __forceinline__ ListRows(const void* p, int64_t first, int64_t ld_, int64_t col, const AttnArgs& A, int32_t tokens) {
-    base = (const uint8_t*)p + (first * ld_ + col) * P::kSize;
-    ld = ld_ * P::kSize;
-    bytes = tokens > 0 ? (tokens - 1) * ld + (int64_t)A.group * A.dim * P::kSize : 0;
-    dim = A.dim * P::kSize;
-  }
-  __device__ __forceinline__ u32x4_t buffer(int32_t token) const {
-    u32x4_t b = buffer_of(base + token * ld, min(bytes - token * ld, (int64_t)0x80000000ll));
+  __device__ __forceinline__ ListRows(const AttnArgs& A, const Seq& s, int head, int32_t first, int wave, int lane) {
+    const int32_t query = first / A.group;
+    group = A.group, rest = first - query * group, dim = A.dim * P::kSize;
+    q_ld = (int32_t)A.ld_q * P::kSize, g_ld = (int32_t)A.ld_dout * P::kSize;
+    const int64_t col = (int64_t)head * group * dim, left = s.nq - query;
+    q = (const uint8_t*)A.q + (s.q0 + query) * q_ld + col;
+    g = (const uint8_t*)A.dout + (s.q0 + query) * g_ld + col;
+    q_left = left > 0 ? (left - 1) * q_ld + group * dim : 0;
+    g_left = left > 0 ? (left - 1) * g_ld + group * dim : 0;
 #pragma unroll
-    for (int j = 0; j < 4; ++j) b[j] = __builtin_amdgcn_readfirstlane(b[j]);
-    return b;
+    for (int j = 0; j < P::kLoads; ++j) {
+      int b;
+      P::source(j, wave, lane, row[j], b);
+      byte[j] = b < dim ? b : kOutside;
+    }
   }
-  __device__ __forceinline__ uint32_t offset(uint32_t token, uint32_t in_group, int byte) const {
-    return byte < dim ? token * (uint32_t)ld + in_group * (uint32_t)dim + (uint32_t)byte : kOutside;
+  __device__ __forceinline__ void load(uint32_t q_lds, uint32_t g_lds, int wave) {
+    const u32x4_t qb = scalar_buffer_of(q, q_left), gb = scalar_buffer_of(g, g_left);
+    const uint32_t inverse = ((1u << 21) + group - 1) / group;   // x / group = x inverse / 2^21 for x < group + 32, group <= 1024
+    q_lds = __builtin_amdgcn_readfirstlane(q_lds), g_lds = __builtin_amdgcn_readfirstlane(g_lds);
+#pragma unroll
+    for (int j = 0; j < P::kLoads; ++j) {
+      const uint32_t x = rest + row[j], query = __umul24(x, inverse) >> 21;
+      const uint32_t at = __umul24(x - __umul24(query, group), dim) + byte[j];
+      load_lds(qb, q_lds + (j * kAttnWaves + wave) * 1024, at + __umul24(query, q_ld));
+      load_lds(gb, g_lds + (j * kAttnWaves + wave) * 1024, at + __umul24(query, g_ld));
+    }
+    rest += P::kRows % group;
+    int32_t queries = P::kRows / group;
+    if (rest >= group) rest -= group, ++queries;
+    const int64_t dq = (int64_t)queries * q_ld, dg = (int64_t)queries * g_ld;
+    q += dq, q_left -= dq, g += dg, g_left -= dg;
   }
 };
 
@@ -257,44 +281,30 @@ __global__ void __launch_bounds__(256, (Dkv<DT, D>::kWaves)) k_attend_dkv(AttnAr
   if (busy) mine = list_span(A, s, key0 + 32 * w, min(key0 + 32 * w + 32, end) - 1);
   if (key0 + 32 * w + 32 > end) mine.lo_all = INT32_MAX;
 
-  const int64_t col = (int64_t)head * A.dim, wide = (int64_t)head * A.group * A.dim, to = s.k0 + key;
-  const ListRows<P> qr(A.q, s.q0, A.ld_q, wide, A, s.nq), gr(A.dout, s.q0, A.ld_dout, wide, A, s.nq);
+  const int64_t col = (int64_t)head * A.dim, to = s.k0 + key;
   const uint32_t lds = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(lds_u8*)smem);
-  const float* const stat = A.stat + list_of(A, s, head) + all.lo;
+  ListRows<P> list(A, s, head, all.lo + first * P::kRows, w, lane);
+  const float* stat = A.stat + list_of(A, s, head) + all.lo + first * P::kRows;
   // of a panel's rows, L in eight lanes' pieces and D in the next eight
   const uint32_t stat_at = lane < 8 ? lane * 16 : lane < 16 ? (uint32_t)(A.tokens_q * A.heads * 4) + (lane - 8) * 16 : kOutside;
-  const uint32_t inverse = A.group > 1 ? 0xFFFFFFFFu / (uint32_t)A.group + 1 : 0;   // x / group = x inverse / 2^32 for small x
-  auto load = [&](int t, int b) {   // into panels b
-    if (t >= last) return;
-    const int32_t r0 = all.lo + t * P::kRows, token0 = r0 / A.group, rest = r0 - token0 * A.group;
-    const u32x4_t qb = qr.buffer(token0), gb = gr.buffer(token0);
-    const uint32_t to = lds + b * P::kBytes;
-#pragma unroll
-    for (int j = 0; j < P::kLoads; ++j) {
-      int row, byte;
-      P::source(j, w, lane, row, byte);
-      const uint32_t x = rest + row, token = A.group > 1 ? __umulhi(x, inverse) : x, in_group = x - token * A.group;
-      load_lds(qb, to + (j * kAttnWaves + w) * 1024, qr.offset(token, in_group, byte));
-      load_lds(gb, to + S::kG + (j * kAttnWaves + w) * 1024, gr.offset(token, in_group, byte));
-    }
-    if (w == 0 && lane < 16) {   // 256 bytes
-      u32x4_t sb = buffer_of((const uint8_t*)(stat + t * P::kRows), 0x80000000ll);
-#pragma unroll
-      for (int j = 0; j < 4; ++j) sb[j] = __builtin_amdgcn_readfirstlane(sb[j]);
-      load_lds(sb, lds + S::kStat + b * 256, stat_at);
-    }
+  auto load = [&](int b) {   // the next panel, into panels b
+    list.load(lds + b * P::kBytes, lds + S::kG + b * P::kBytes, w);
+    if (w == 0 && lane < 16) load_lds(scalar_buffer_of((const uint8_t*)stat, 0x80000000ll), lds + S::kStat + b * 256, stat_at);   // 256 bytes
+    stat += P::kRows;
   };
   Reader<DT, D> rd(lds, lane);
   OwnRow<DT, D> k, v;
   if constexpr (S::kValuesInLds) {
-    const Rows<DT, D, P> vr(A.v, s.k0 + key0, A.ld_v, col, end - key0, A.dim, w, lane);
+    Rows<DT, D, P> vr(A.v, s.k0 + key0, A.ld_v, col, end - key0, A.dim, w, lane);
 #pragma unroll
-    for (int j = 0; j < 4; ++j) vr.load(j, lds + S::kValues + j * P::kBytes, w);
+    for (int j = 0; j < 4; ++j) vr.load(lds + S::kValues + j * P::kBytes, w);
   } else {
     v.load(A.v, to * A.ld_v + col, A.dim, half, on);
   }
-  load(first, 0);
+  load(0);
   k.load(A.k, to * A.ld_k + col, A.dim, half, on);
+  k.arrive();
+  if constexpr (!S::kValuesInLds) v.arrive();
   const Reader<DT, D> own(lds + S::kValues + w * P::kBytes, lane);
 
   f32x16_t dk[D / 32], dv[D / 32];
@@ -306,7 +316,7 @@ __global__ void __launch_bounds__(256, (Dkv<DT, D>::kWaves)) k_attend_dkv(AttnAr
   constexpr uint32_t qp = 0, gp = S::kG;
   for (int t = first; t < last; ++t) {
     landed();
-    load(t + 1, (t - first + 1) & 1);
+    load((t - first + 1) & 1);
     const int32_t r0 = all.lo + t * P::kRows;
     if (!busy || r0 >= mine.hi || r0 + P::kRows <= mine.lo) {
       rd.swap(P::kBytes);

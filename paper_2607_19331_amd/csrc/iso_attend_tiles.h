@@ -44,18 +44,18 @@ struct Panel {
 
 constexpr uint32_t kOutside = 0xC0000000u;   // an offset behind the end of every buffer
 
-// One operand's rows in memory, loaded panel by panel: `row` 0 of a kv head of a sequence and how many there are.
+// One operand's rows in memory, loaded panel by panel: a kv head's from some row on, `rows` of them.
 template <int DT, int D, class PANEL = Panel<DT, D>>
 struct Rows {
   using P = PANEL;
-  const uint8_t* base;
-  int64_t step, bytes;   // bytes of a panel's rows, and from row 0 on to the end of the last row
+  const uint8_t* at;
+  int64_t step, left;   // bytes of a panel's rows, and from `at` on to the end of the last row
   uint32_t offset[P::kLoads];
 
   __device__ __forceinline__ Rows(const void* p, int64_t first, int64_t ld, int64_t col, int64_t rows, int dim, int wave, int lane) {
-    base = (const uint8_t*)p + (first * ld + col) * P::kSize;
+    at = (const uint8_t*)p + (first * ld + col) * P::kSize;
     step = P::kRows * ld * P::kSize;
-    bytes = rows > 0 ? ((rows - 1) * ld + dim) * P::kSize : 0;
+    left = rows > 0 ? ((rows - 1) * ld + dim) * P::kSize : 0;
 #pragma unroll
     for (int j = 0; j < P::kLoads; ++j) {
       int row, byte;
@@ -63,14 +63,14 @@ struct Rows {
       offset[j] = byte < dim * P::kSize ? (uint32_t)(row * (int)ld * P::kSize + byte) : kOutside;
     }
   }
-  // Panel t into LDS; one past the last, zeros.
-  __device__ __forceinline__ void load(int64_t t, uint32_t lds, int wave) const {
-    u32x4_t b = buffer_of(base + t * step, min(bytes - t * step, (int64_t)0x80000000ll));
-#pragma unroll
-    for (int j = 0; j < 4; ++j) b[j] = __builtin_amdgcn_readfirstlane(b[j]);
+  __device__ __forceinline__ void skip(int64_t panels) { at += panels * step, left -= panels * step; }
+  // The next panel into LDS; behind the last row, zeros.
+  __device__ __forceinline__ void load(uint32_t lds, int wave) {
+    const u32x4_t b = scalar_buffer_of(at, left);
     lds = __builtin_amdgcn_readfirstlane(lds);
 #pragma unroll
     for (int j = 0; j < P::kLoads; ++j) load_lds(b, lds + (j * kAttnWaves + wave) * 1024, offset[j]);
+    at += step, left -= step;
   }
 };
 
@@ -148,6 +148,12 @@ struct OwnRow {
       g[i] = u32x4_t{0, 0, 0, 0};
       if (on && c < dim) g[i] = load_raw<DT>(p, at + c);
     }
+  }
+  // The loads have come back.  Before a loop that loads into LDS: the first use, if it were in there, would wait for those too,
+  // each time round.
+  __device__ __forceinline__ void arrive() {
+#pragma unroll
+    for (int i = 0; i < Panel<DT, D>::kGroups; ++i) asm volatile("" : "+v"(g[i]));
   }
 };
 

@@ -22,6 +22,17 @@ __device__ __forceinline__ u32x4_t buffer_of(const uint8_t* p, int64_t left) {
   return u32x4_t{(uint32_t)a, (uint32_t)(a >> 32) & 0xFFFFu, n, 0x00027000u};
 }
 
+// The same with the scalar unit alone (it compares no 64 bits), for at most 2 GiB: offsets from there on are outside.
+__device__ __forceinline__ u32x4_t scalar_buffer_of(const uint8_t* p, int64_t left) {
+  const uint64_t a = (uint64_t)p;
+  const int32_t hi = (int32_t)(left >> 32);
+  const uint32_t lo = (uint32_t)left, n = hi < 0 ? 0u : hi > 0 || lo > 0x80000000u ? 0x80000000u : lo;
+  u32x4_t b = {(uint32_t)a, (uint32_t)(a >> 32) & 0xFFFFu, n, 0x00027000u};
+#pragma unroll
+  for (int j = 0; j < 4; ++j) b[j] = __builtin_amdgcn_readfirstlane(b[j]);
+  return b;
+}
+
 // 16 bytes a lane from the buffer into LDS, the wave's 1024 bytes one after another from byte `lds` on.  An instruction
 // of its own because the compiler waits for every such load before the next LDS read, whatever that reads; the kernels
 // count them themselves.  It has no destination register; m0 needs one instruction between its write and its use.
