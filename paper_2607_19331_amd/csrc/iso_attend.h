@@ -35,8 +35,8 @@ struct AttnArgs {
   void *dq, *dk, *dv;
   int64_t ld_dq, ld_dk, ld_dv;
   float* stat;                        // for every row of a group's list, kv head by kv head: L log2(e), then D
-  Pieces pieces;                      // that a tile's keys are shared out to
-  float* part;                        // their sums: pieces x tokens_q x heads x kPartLd
+  Pieces pieces, key_pieces;          // that a tile's keys are shared out to, and the rows of a tile of keys
+  float *part, *key_part;             // their sums: pieces x tokens_q x heads (tokens_k x heads_kv x 2) x kPartLd
   uint32_t* status;
 };
 

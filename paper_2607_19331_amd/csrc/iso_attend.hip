@@ -1,6 +1,4 @@
 // Attention over packed sequences, forward: O = softmax(scale Q K^T) V and the log-sum-exp of its rows.
-#include <algorithm>
-
 #include "iso_attend_tiles.h"
 #include "iso_grad.h"
 
@@ -13,16 +11,16 @@ __global__ void __launch_bounds__(256, (DT == ISO_F32 && D == 128 ? 1 : 2)) k_at
   using P = Panel<DT, D>;
   constexpr int kRows = 32 * kAttnWaves, KT = P::kTiles;
   extern __shared__ __attribute__((aligned(1024))) uint8_t smem[];
-  if (blockIdx.x == 0) check_starts(A);
+  if (blockIdx.x == gridDim.x - 1) return check_starts(A);
   int head;
-  uint32_t tile, at;
-  Seq s;
-  if (!dealt<false>(deal, A.heads_kv, blockIdx.x, head, tile)) return;
-  const int piece = (int)(tile % (uint32_t)A.pieces.most);
-  if (!find_tile<false, kRows>(A, tile / (uint32_t)A.pieces.most, s, at)) return;
+  uint32_t item;
+  Item it;
+  if (!dealt(deal, A.heads_kv, blockIdx.x, head, item) || !find_item<false, kRows>(A, A.pieces, item, it)) return;
+  const Seq s = it.s;
+  const int piece = it.piece;
 
   const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, half = lane >> 5;
-  const int32_t rows = s.nq * A.group, row0 = (int32_t)at * kRows, end = min(row0 + kRows, rows);
+  const int32_t rows = s.nq * A.group, row0 = (int32_t)it.tile * kRows, end = min(row0 + kRows, rows);
   const Span all = span_of(A, s, row0, end - 1);
   const int pieces = pieces_of(all, A.pieces);
   if (piece >= pieces) return;
@@ -221,47 +219,61 @@ __global__ void __launch_bounds__(256, (DT == ISO_F32 && D == 128 ? 1 : 2)) k_at
   }
 }
 
-// Adds up the pieces of a row, one wave a row.
+// Adds up the pieces of a row, half a wave a row.
 template <int DT>
 __global__ void __launch_bounds__(256) k_attend_join(AttnArgs A) {
-  const int64_t at = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6), t = at / A.heads;
-  if (t >= A.tokens_q) return;
-  const Seq s = seq_at(A, A.start_q, t);
-  if (t < s.q0 || t >= s.q0 + s.nq) return;
   constexpr int kRows = 32 * kAttnWaves;
-  const int h = (int)(at - t * A.heads), head = h / A.group, lane = threadIdx.x & 63;
-  const int32_t r = (int32_t)(t - s.q0) * A.group + h % A.group, row0 = r / kRows * kRows;
-  const Span all = span_of(A, s, row0, min(row0 + kRows, s.nq * A.group) - 1);
+  const int lane = threadIdx.x & 63, l32 = lane & 31, c = 4 * l32;
+  const JoinRow j(A, (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5));
+  const Span all = j.on ? span_of(A, j.s, j.r / kRows * kRows, min(j.r / kRows * kRows + kRows, j.s.nq * A.group) - 1) : Span{0, 0, 0, 0};
   const int pieces = pieces_of(all, A.pieces);
-  if (pieces == 1) return;
-  const auto part = gmem((const float*)A.part) + at * kPartLd;
+  const bool on = j.on && pieces > 1;
+  const auto part = gmem((const float*)A.part) + j.at * kPartLd;
   const int64_t next = A.tokens_q * A.heads * kPartLd;
-  const float mine = lane < pieces ? part[lane * next + 128] : -INFINITY;
-  const float m = wave_max(mine), f = __builtin_amdgcn_exp2f(mine - (m == -INFINITY ? 0.0f : m));
-  const float l = wave_sum(lane < pieces ? part[lane * next + 129] * f : 0.0f);
-  int32_t lo, hi;
-  keys_of(A, s, r / A.group, lo, hi);
-  float o[2] = {0.0f, 0.0f};
-#pragma unroll 4
-  for (int p = 0; p < pieces; ++p) {
-    const float g = __shfl(f, p);
+  float m[2], l[2], f[2];   // of pieces l32 and l32 + 32
 #pragma unroll
-    for (int c = 0; c < 2; ++c)
-      if (lane + 64 * c < A.dim) o[c] = fmaf(part[p * next + lane + 64 * c], g, o[c]);
+  for (int i = 0; i < 2; ++i) {
+    const bool has = on && l32 + 32 * i < pieces;
+    m[i] = has ? part[(l32 + 32 * i) * next + 128] : -INFINITY;
+    l[i] = has ? part[(l32 + 32 * i) * next + 129] : 0.0f;
   }
-  const float inv = hi > lo ? 1.0f / l : 0.0f;
-  if (__any(fmaf(o[0] * inv, 0.0f, o[1] * inv * 0.0f) != 0.0f)) return attend_row<DT>(A, s, head, r, lane);
+  float top = fmaxf(m[0], m[1]);
 #pragma unroll
-  for (int c = 0; c < 2; ++c)
-    if (lane + 64 * c < A.dim) store_one<DT>(A.out, t * A.ld_out + (int64_t)h * A.dim + lane + 64 * c, o[c] * inv);
-  if (lane == 0) gmem(A.lse)[at] = hi > lo ? (m + __builtin_amdgcn_logf(l)) * kLn2 : -INFINITY;
+  for (int d = 16; d > 0; d >>= 1) top = fmaxf(top, __shfl_xor(top, d));
+  float sum = 0.0f;
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    f[i] = __builtin_amdgcn_exp2f(m[i] - (top == -INFINITY ? 0.0f : top));
+    sum += l[i] * f[i];
+  }
+#pragma unroll
+  for (int d = 16; d > 0; d >>= 1) sum += __shfl_xor(sum, d);
+  float o[4] = {};
+  add_parts(part, next, c, on && c < A.dim ? pieces : 0, [&](int p) { return __shfl(p < 32 ? f[0] : f[1], (lane & 32) | (p & 31)); }, o);
+  int32_t lo = 0, hi = 0;
+  if (on) keys_of(A, j.s, j.r / A.group, lo, hi);
+  const float inv = hi > lo ? 1.0f / sum : 0.0f;
+  float t = 0.0f;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) o[i] *= inv, t = fmaf(o[i], 0.0f, t);
+  const uint64_t bad = __ballot(t != 0.0f);
+  if (on && (uint32_t)(bad >> (lane & 32)) == 0) {
+    if (c < A.dim) store_elems<DT, 4>(A.out, j.t * A.ld_out + (int64_t)j.h * A.dim + c, o);
+    if (l32 == 0) gmem(A.lse)[j.at] = hi > lo ? (top + __builtin_amdgcn_logf(sum)) * kLn2 : -INFINITY;
+  }
+#pragma unroll 1
+  for (int i = 0; i < 2; ++i)
+    if ((uint32_t)(bad >> (32 * i)) != 0) {
+      const JoinRow row = j.of(32 * i);
+      attend_row<DT>(A, row.s, row.h / A.group, row.r, lane);
+    }
 }
 
 template <int DT, int D>
 hipError_t forward(const AttnArgs& A, hipStream_t s) {
-  const Deal deal = deal_of(A.heads_kv, (uint32_t)(attend_tiles(A.tokens_q * A.group, A.sequences) * A.pieces.most));
-  k_attend<DT, D><<<std::max(1u, deal_grid(deal, A.heads_kv)), 256, 4 * Panel<DT, D>::kBytes, s>>>(A, deal);
-  if (A.pieces.most > 1) k_attend_join<DT><<<(unsigned)((A.tokens_q * A.heads + 3) / 4), 256, 0, s>>>(A);
+  const Deal deal = deal_of(A.heads_kv, attend_items(A.tokens_q * A.group, A.tokens_k, A.sequences, A.pieces));
+  k_attend<DT, D><<<deal_grid(deal, A.heads_kv) + 1, 256, 4 * Panel<DT, D>::kBytes, s>>>(A, deal);   // one looks at the offsets
+  if (A.pieces.most > 1) k_attend_join<DT><<<(unsigned)((A.tokens_q * A.heads + 7) / 8), 256, 0, s>>>(A);
   return hipGetLastError();
 }
 

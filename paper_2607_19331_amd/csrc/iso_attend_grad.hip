@@ -1,8 +1,8 @@
 // Attention over packed sequences, backward: with P = exp(scale Q K^T - L) worked out again, D = sum of dO O over a row and
 // S = P (dO V^T - D),  dV = P^T dO,  dK = scale S^T Q,  dQ = scale S K.
 //
-// Two kernels form P and S each for itself: k_attend_dkv has keys and walks over the rows that see them, k_attend_dq has rows
-// and walks over the keys that they see.  That is seven products of rows x keys x dim where one kernel would need five, but each
+// Two kinds of workgroups form P and S each for themselves: those of dkv have keys and walk over the rows that see them, those of
+// dq have rows and walk over the keys that they see.  That is seven products of rows x keys x dim where one kernel would need five, but each
 // result has one owner who adds in a fixed order: no atomics, the same bits every time.
 #include <algorithm>
 
@@ -16,7 +16,7 @@ namespace {
 // L log2(e) and D of every row, 16 lanes a row.
 template <int DT>
 __global__ void __launch_bounds__(256) k_attend_stat(AttnArgs A) {
-  if (blockIdx.x == 0) check_starts(A);
+  if (blockIdx.x == gridDim.x - 1) return check_starts(A);
   const int64_t at = (int64_t)blockIdx.x * 16 + (threadIdx.x >> 4), t = at / A.heads;
   if (t >= A.tokens_q) return;
   const Seq s = seq_at(A, A.start_q, t);
@@ -42,22 +42,18 @@ __global__ void __launch_bounds__(256) k_attend_stat(AttnArgs A) {
 // ---- dQ ------------------------------------------------------------------------------------------------------------
 
 template <int DT, int D>
-constexpr int kDqWaves = DT == ISO_F32 && D == 128 ? 1 : 2;
-
-template <int DT, int D>
-__global__ void __launch_bounds__(256, (kDqWaves<DT, D>)) k_attend_dq(AttnArgs A, Deal deal) {
+__device__ __forceinline__ void dq_tile(const AttnArgs& A, const Deal& deal, uint32_t block, uint8_t* smem) {
   using P = Panel<DT, D>;
   constexpr int kRows = 32 * kAttnWaves, KT = P::kTiles;
-  extern __shared__ __attribute__((aligned(1024))) uint8_t smem[];
   int head;
-  uint32_t tile, at;
-  Seq s;
-  if (!dealt<false>(deal, A.heads_kv, blockIdx.x, head, tile)) return;
-  const int piece = (int)(tile % (uint32_t)A.pieces.most);
-  if (!find_tile<false, kRows>(A, tile / (uint32_t)A.pieces.most, s, at)) return;
+  uint32_t item;
+  Item it;
+  if (!dealt(deal, A.heads_kv, block, head, item) || !find_item<false, kRows>(A, A.pieces, item, it)) return;
+  const Seq s = it.s;
+  const int piece = it.piece;
 
   const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, half = lane >> 5;
-  const int32_t rows = s.nq * A.group, row0 = (int32_t)at * kRows, end = min(row0 + kRows, rows);
+  const int32_t rows = s.nq * A.group, row0 = (int32_t)it.tile * kRows, end = min(row0 + kRows, rows);
   const Span all = span_of(A, s, row0, end - 1);
   const int pieces = pieces_of(all, A.pieces);
   if (piece >= pieces) return;
@@ -102,26 +98,75 @@ __global__ void __launch_bounds__(256, (kDqWaves<DT, D>)) k_attend_dq(AttnArgs A
     const int32_t k0 = all.lo + t * P::kRows;
     if (!busy || k0 >= mine.hi || k0 + P::kRows <= mine.lo) return;
     const bool whole = k0 >= mine.lo_all && k0 + P::kRows <= mine.hi_all;
+    auto hide = [&](f32x16_t& x, int j) {   // 0 times what is not seen may be NaN
 #pragma unroll
-    for (int j = 0; j < KT; ++j) {
-      f32x16_t x = 0.0f, y = -delta;
+      for (int e = 0; e < 16; ++e) {
+        const int32_t key = k0 + 32 * j + 8 * (e / 4) + 4 * half + e % 4;
+        x[e] = (uint32_t)(key - lo) < (uint32_t)(hi - lo) ? x[e] : 0.0f;
+      }
+    };
+    if constexpr (DT == ISO_BF16) {
+      // as in dkv_tile: fragments three products ahead, S and dP by rows, dQ by columns, one tile of 32 keys after the other
+      constexpr int G = P::kGroups, N = P::kDims, kAhead = 3;
+      static_assert(G == 2 * N, "as many products each");
+      u32x4_t ring[kAhead];
+      auto read = [&](int n) {
+        const int j = n / (3 * G), i = n % (3 * G);
+        if (j >= KT) return;
+        if (i < G) ring[n % kAhead] = rd.row(b * P::kBytes, j, i);
+        else if (i < 2 * G) ring[n % kAhead] = rd.row(kV + b * P::kBytes, j, i - G);
+        else ring[n % kAhead] = __builtin_bit_cast(u32x4_t, rd.col(b * P::kBytes, j, (i - 2 * G) / N, (i - 2 * G) % N));
+      };
 #pragma unroll
-      for (int e = 0; e < P::kGroups; ++e) multiply<DT>(rd.row(b * P::kBytes, j, e), q.g[e], x);
+      for (int n = 0; n < kAhead; ++n) read(n);
 #pragma unroll
-      for (int e = 0; e < P::kGroups; ++e) multiply<DT>(rd.row(kV + b * P::kBytes, j, e), g.g[e], y);
-      Packed<DT> ds;
+      for (int j = 0; j < KT; ++j) {
+        const int n0 = 3 * G * j;
+        f32x16_t x = 0.0f, y = -delta;
 #pragma unroll
-      for (int e = 0; e < 16; ++e) x[e] = __builtin_amdgcn_exp2f(fmaf(x[e], A.scale2, -lse)) * y[e];
-      if (!whole) {
+        for (int n = 0; n < G; ++n) {
+          multiply<DT>(ring[(n0 + n) % kAhead], q.g[n], x);
+          read(n0 + n + kAhead);
+          __builtin_amdgcn_sched_barrier(0);
+        }
 #pragma unroll
-        for (int e = 0; e < 16; ++e) {
-          const int32_t key = k0 + 32 * j + 8 * (e / 4) + 4 * half + e % 4;
-          x[e] = (uint32_t)(key - lo) < (uint32_t)(hi - lo) ? x[e] : 0.0f;
+        for (int n = 0; n < G; ++n) {
+          multiply<DT>(ring[(n0 + G + n) % kAhead], g.g[n], y);
+          read(n0 + G + n + kAhead);
+#pragma unroll
+          for (int e = 16 / G * n; e < 16 / G * (n + 1); ++e) x[e] = __builtin_amdgcn_exp2f(fmaf(x[e], A.scale2, -lse));
+          __builtin_amdgcn_sched_barrier(0);
+        }
+#pragma unroll
+        for (int e = 0; e < 16; ++e) x[e] *= y[e];
+        if (!whole) hide(x, j);
+        Packed<DT> ds;
+#pragma unroll
+        for (int e = 0; e < 16; e += 2) ds.set(e / 2, x[e], x[e + 1]);
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int n = 0; n < G; ++n) {
+          multiply<DT>(ring[(n0 + 2 * G + n) % kAhead], ds.s[n / N], dq[n % N]);
+          read(n0 + 2 * G + n + kAhead);
+          __builtin_amdgcn_sched_barrier(0);
         }
       }
+    } else {
 #pragma unroll
-      for (int e = 0; e < 16; e += 2) ds.set(e / 2, x[e], x[e + 1]);
-      multiply_columns<DT, D>(rd, b * P::kBytes, j, ds, dq);
+      for (int j = 0; j < KT; ++j) {
+        f32x16_t x = 0.0f, y = -delta;
+#pragma unroll
+        for (int e = 0; e < P::kGroups; ++e) multiply<DT>(rd.row(b * P::kBytes, j, e), q.g[e], x);
+#pragma unroll
+        for (int e = 0; e < P::kGroups; ++e) multiply<DT>(rd.row(kV + b * P::kBytes, j, e), g.g[e], y);
+        Packed<DT> ds;
+#pragma unroll
+        for (int e = 0; e < 16; ++e) x[e] = __builtin_amdgcn_exp2f(fmaf(x[e], A.scale2, -lse)) * y[e];
+        if (!whole) hide(x, j);
+#pragma unroll
+        for (int e = 0; e < 16; e += 2) ds.set(e / 2, x[e], x[e + 1]);
+        multiply_columns<DT, D>(rd, b * P::kBytes, j, ds, dq);
+      }
     }
   };
   for (int t = first; t < last; t += 2) {
@@ -161,32 +206,28 @@ __global__ void __launch_bounds__(256, (kDqWaves<DT, D>)) k_attend_dq(AttnArgs A
   }
 }
 
-// Adds up the pieces of a row, one wave a row.
+// Adds up the pieces of a row, half a wave a row.
 template <int DT>
-__global__ void __launch_bounds__(256) k_attend_dq_join(AttnArgs A) {
-  const int64_t at = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6), t = at / A.heads;
-  if (t >= A.tokens_q) return;
-  const Seq s = seq_at(A, A.start_q, t);
-  if (t < s.q0 || t >= s.q0 + s.nq) return;
+__device__ __forceinline__ void dq_join(const AttnArgs& A, uint32_t block) {
   constexpr int kRows = 32 * kAttnWaves;
-  const int h = (int)(at - t * A.heads), head = h / A.group, lane = threadIdx.x & 63;
-  const int32_t r = (int32_t)(t - s.q0) * A.group + h % A.group, row0 = r / kRows * kRows;
-  const Span all = span_of(A, s, row0, min(row0 + kRows, s.nq * A.group) - 1);
+  const int lane = threadIdx.x & 63, c = 4 * (lane & 31);
+  const JoinRow j(A, (int64_t)block * 8 + (threadIdx.x >> 5));
+  const Span all = j.on ? span_of(A, j.s, j.r / kRows * kRows, min(j.r / kRows * kRows + kRows, j.s.nq * A.group) - 1) : Span{0, 0, 0, 0};
   const int pieces = pieces_of(all, A.pieces);
-  if (pieces == 1) return;
-  const auto part = gmem((const float*)A.part) + at * kPartLd;
-  const int64_t next = A.tokens_q * A.heads * kPartLd;
-  float v[2] = {0.0f, 0.0f};
-#pragma unroll 4
-  for (int p = 0; p < pieces; ++p)
+  const bool on = j.on && pieces > 1;
+  float v[4] = {}, t = 0.0f;
+  add_parts(gmem((const float*)A.part) + j.at * kPartLd, A.tokens_q * A.heads * kPartLd, c, on && c < A.dim ? pieces : 0,
+            [](int) { return 1.0f; }, v);
 #pragma unroll
-    for (int c = 0; c < 2; ++c)
-      if (lane + 64 * c < A.dim) v[c] += part[p * next + lane + 64 * c];
-  v[0] *= A.scale, v[1] *= A.scale;
-  if (__any(fmaf(v[0], 0.0f, v[1] * 0.0f) != 0.0f)) return dq_row<DT>(A, s, head, r, lane);
-#pragma unroll
-  for (int c = 0; c < 2; ++c)
-    if (lane + 64 * c < A.dim) store_one<DT>(A.dq, t * A.ld_dq + (int64_t)h * A.dim + lane + 64 * c, v[c]);
+  for (int i = 0; i < 4; ++i) v[i] *= A.scale, t = fmaf(v[i], 0.0f, t);
+  const uint64_t bad = __ballot(t != 0.0f);
+  if (on && (uint32_t)(bad >> (lane & 32)) == 0 && c < A.dim) store_elems<DT, 4>(A.dq, j.t * A.ld_dq + (int64_t)j.h * A.dim + c, v);
+#pragma unroll 1
+  for (int i = 0; i < 2; ++i)
+    if ((uint32_t)(bad >> (32 * i)) != 0) {
+      const JoinRow row = j.of(32 * i);
+      dq_row<DT>(A, row.s, row.h / A.group, row.r, lane);
+    }
 }
 
 // ---- dK and dV -----------------------------------------------------------------------------------------------------
@@ -248,22 +289,21 @@ struct Dkv {
 };
 
 template <int DT, int D>
-__global__ void __launch_bounds__(256, (Dkv<DT, D>::kWaves)) k_attend_dkv(AttnArgs A, Deal deal) {
+__device__ __forceinline__ void dkv_tile(const AttnArgs& A, const Deal& deal, uint32_t block, uint8_t* smem) {
   using S = Dkv<DT, D>;
   using P = typename S::P;
   constexpr int kKeys = 32 * kAttnWaves;
-  extern __shared__ __attribute__((aligned(32768))) uint8_t smem[];   // panels in turn are one bit of an address apart
   int head;
-  uint32_t tile, at;
-  Seq s;
-  if (!dealt<true>(deal, A.heads_kv, blockIdx.x, head, tile)) return;
-  const int piece = (int)(tile % (uint32_t)A.pieces.most);
-  if (!find_tile<true, kKeys>(A, tile / (uint32_t)A.pieces.most, s, at)) return;
+  uint32_t item;
+  Item it;
+  if (!dealt(deal, A.heads_kv, block, head, item) || !find_item<true, kKeys>(A, A.key_pieces, item, it)) return;
+  const Seq s = it.s;
+  const int piece = it.piece;
 
   const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, half = lane >> 5;
-  const int32_t key0 = (int32_t)at * kKeys, end = min(key0 + kKeys, s.nk);
+  const int32_t key0 = (int32_t)it.tile * kKeys, end = min(key0 + kKeys, s.nk);
   const Span all = list_span(A, s, key0, end - 1);
-  const int pieces = pieces_of(all, A.pieces);
+  const int pieces = pieces_of(all, A.key_pieces);
   if (piece >= pieces) return;
   const int tiles = (all.hi - all.lo + P::kRows - 1) / P::kRows;
   const int first = __builtin_amdgcn_readfirstlane((int)((int64_t)tiles * piece / pieces));
@@ -418,7 +458,7 @@ __global__ void __launch_bounds__(256, (Dkv<DT, D>::kWaves)) k_attend_dkv(AttnAr
 
   if (pieces > 1) {
     if (!on) return;
-    float* const part = A.part + (((int64_t)piece * A.tokens_k + to) * A.heads_kv + head) * (2 * kPartLd);
+    float* const part = A.key_part + (((int64_t)piece * A.tokens_k + to) * A.heads_kv + head) * (2 * kPartLd);
 #pragma unroll
     for (int d = 0; d < D / 32; ++d)
 #pragma unroll
@@ -450,51 +490,63 @@ __global__ void __launch_bounds__(256, (Dkv<DT, D>::kWaves)) k_attend_dkv(AttnAr
   }
 }
 
-// Adds up the pieces of a key, one wave a key and kv head.
+// Adds up the pieces of a key, a wave a key and kv head: dK in its first half, dV in its second.
 template <int DT>
-__global__ void __launch_bounds__(256) k_attend_dkv_join(AttnArgs A) {
-  const int64_t at = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6), t = at / A.heads_kv;
+__device__ __forceinline__ void dkv_join(const AttnArgs& A, uint32_t block) {
+  constexpr int kKeys = 32 * kAttnWaves;
+  const int64_t at = (int64_t)block * 4 + (threadIdx.x >> 6), t = at / A.heads_kv;
   if (t >= A.tokens_k) return;
   const Seq s = seq_at(A, A.start_k, t);
   if (t < s.k0 || t >= s.k0 + s.nk) return;
-  constexpr int kKeys = 32 * kAttnWaves;
-  const int head = (int)(at - t * A.heads_kv), lane = threadIdx.x & 63;
+  const int head = (int)(at - t * A.heads_kv), lane = threadIdx.x & 63, c = 4 * (lane & 31);
   const int32_t key = (int32_t)(t - s.k0), key0 = key / kKeys * kKeys;
-  const Span all = list_span(A, s, key0, min(key0 + kKeys, s.nk) - 1);
-  const int pieces = pieces_of(all, A.pieces);
+  const int pieces = pieces_of(list_span(A, s, key0, min(key0 + kKeys, s.nk) - 1), A.key_pieces);
   if (pieces == 1) return;
-  const auto part = gmem((const float*)A.part) + at * (2 * kPartLd);
-  const int64_t next = A.tokens_k * A.heads_kv * (2 * kPartLd), col = (int64_t)head * A.dim;
-  float v[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll 4
-  for (int p = 0; p < pieces; ++p)
+  const bool values = lane >= 32;
+  float v[4] = {}, bad = 0.0f;
+  add_parts(gmem((const float*)A.key_part) + at * (2 * kPartLd) + (values ? kPartLd : 0), A.tokens_k * A.heads_kv * (2 * kPartLd), c,
+            c < A.dim ? pieces : 0, [](int) { return 1.0f; }, v);
 #pragma unroll
-    for (int c = 0; c < 4; ++c)
-      if (lane + 64 * (c & 1) < A.dim) v[c] += part[p * next + (c >> 1) * kPartLd + lane + 64 * (c & 1)];
-  v[0] *= A.scale, v[1] *= A.scale;
-  if (__any(v[0] * 0.0f + v[1] * 0.0f + v[2] * 0.0f + v[3] * 0.0f != 0.0f)) return dkv_row<DT>(A, s, head, key, lane);
-#pragma unroll
-  for (int c = 0; c < 2; ++c) {
-    if (lane + 64 * c >= A.dim) continue;
-    store_one<DT>(A.dk, t * A.ld_dk + col + lane + 64 * c, v[c]);
-    store_one<DT>(A.dv, t * A.ld_dv + col + lane + 64 * c, v[2 + c]);
+  for (int i = 0; i < 4; ++i) {
+    if (!values) v[i] *= A.scale;
+    bad = fmaf(v[i], 0.0f, bad);
   }
+  if (__any(bad != 0.0f)) return dkv_row<DT>(A, s, head, key, lane);
+  if (c >= A.dim) return;
+  if (values) store_elems<DT, 4>(A.dv, t * A.ld_dv + (int64_t)head * A.dim + c, v);
+  else store_elems<DT, 4>(A.dk, t * A.ld_dk + (int64_t)head * A.dim + c, v);
+}
+
+// ---- both ----------------------------------------------------------------------------------------------------------
+
+// Workgroups up to `keys` have keys, the others rows: in one launch, where the ones' last round leaves room for the others.
+template <int DT, int D>
+__global__ void __launch_bounds__(256, (Dkv<DT, D>::kWaves)) k_attend_grad(AttnArgs A, Deal dkv, Deal dq, uint32_t keys) {
+  extern __shared__ __attribute__((aligned(32768))) uint8_t smem[];   // panels in turn are one bit of an address apart
+  if (blockIdx.x < keys) dkv_tile<DT, D>(A, dkv, blockIdx.x, smem);
+  else dq_tile<DT, D>(A, dq, blockIdx.x - keys, smem);
+}
+
+template <int DT>
+__global__ void __launch_bounds__(256) k_attend_grad_join(AttnArgs A, uint32_t keys) {
+  if (blockIdx.x < keys) dkv_join<DT>(A, blockIdx.x);
+  else dq_join<DT>(A, blockIdx.x - keys);
 }
 
 template <int DT, int D>
 hipError_t backward(AttnArgs A, const AttendPlan& plan, uint8_t* ws, hipStream_t s) {
-  const unsigned rows = (unsigned)((A.tokens_q * A.heads + 3) / 4), keys = (unsigned)((A.tokens_k * A.heads_kv + 3) / 4);
+  const int64_t rows = A.tokens_q * A.heads, keys = A.tokens_k * A.heads_kv, list = A.tokens_q * A.group;
   A.stat = (float*)(ws + kStatusBytes);
-  A.part = (float*)(ws + plan.part);
-  k_attend_stat<DT><<<std::max(1u, (rows + 3) / 4), 256, 0, s>>>(A);
-  A.pieces = plan.rows;
-  const Deal dq = deal_of(A.heads_kv, (uint32_t)(attend_tiles(A.tokens_q * A.group, A.sequences) * A.pieces.most));
-  if (rows > 0) k_attend_dq<DT, D><<<deal_grid(dq, A.heads_kv), 256, 4 * Panel<DT, D>::kBytes, s>>>(A, dq);
-  if (rows > 0 && A.pieces.most > 1) k_attend_dq_join<DT><<<rows, 256, 0, s>>>(A);
-  A.pieces = plan.keys;
-  const Deal dkv = deal_of(A.heads_kv, (uint32_t)(attend_tiles(A.tokens_k, A.sequences) * A.pieces.most));
-  if (keys > 0) k_attend_dkv<DT, D><<<deal_grid(dkv, A.heads_kv), 256, Dkv<DT, D>::kLds, s>>>(A, dkv);
-  if (keys > 0 && A.pieces.most > 1) k_attend_dkv_join<DT><<<keys, 256, 0, s>>>(A);
+  A.pieces = plan.rows, A.part = (float*)(ws + plan.part);
+  A.key_pieces = plan.keys, A.key_part = (float*)(ws + plan.key_part);
+  k_attend_stat<DT><<<(unsigned)((rows + 15) / 16) + 1, 256, 0, s>>>(A);   // one looks at the offsets
+  const Deal dkv = deal_of(A.heads_kv, attend_items(A.tokens_k, list, A.sequences, A.key_pieces));
+  const Deal dq = deal_of(A.heads_kv, attend_items(list, A.tokens_k, A.sequences, A.pieces));
+  const uint32_t of_keys = keys > 0 ? deal_grid(dkv, A.heads_kv) : 0, of_rows = rows > 0 ? deal_grid(dq, A.heads_kv) : 0;
+  constexpr uint32_t lds = std::max((uint32_t)(4 * Panel<DT, D>::kBytes), Dkv<DT, D>::kLds);
+  if (of_keys + of_rows > 0) k_attend_grad<DT, D><<<of_keys + of_rows, 256, lds, s>>>(A, dkv, dq, of_keys);
+  const uint32_t join_keys = A.key_pieces.most > 1 ? (uint32_t)((keys + 3) / 4) : 0, join_rows = A.pieces.most > 1 ? (uint32_t)((rows + 7) / 8) : 0;
+  if (join_keys + join_rows > 0) k_attend_grad_join<DT><<<join_keys + join_rows, 256, 0, s>>>(A, join_keys);
   return hipGetLastError();
 }
 

@@ -210,63 +210,84 @@ __device__ __forceinline__ float sum_of_halves(float v) {
 
 // ---- which tile a workgroup has ------------------------------------------------------------------------------------
 
-// Work is a list of tiles of rows for every kv head.  Workgroup b runs on XCD b % 8: heads are dealt to as many classes of XCDs
-// as divide them evenly, so that a head's keys and values are read through few L2 caches, and a class takes the tiles of a head,
-// its XCDs in turn, from those on that have most to do under a causal mask: the last rows, the first keys.
+// Work is a list of items for every kv head: tiles of rows (or keys), the keys (rows) that a tile walks over shared out to the
+// pieces of its sequence.  Workgroup b runs on XCD b % 8: heads are dealt to as many classes of XCDs as divide them evenly, so
+// that a head's keys and values are read through few L2 caches, and a class takes the items of a head, its XCDs in turn.
 struct Deal {
   int32_t classes, per;   // classes of XCDs, XCDs of a class
-  uint32_t tiles;         // tiles of a head (or an upper bound), times the pieces of each
+  uint32_t items;         // of a head, or an upper bound
 };
 
-inline Deal deal_of(int heads, uint32_t tiles) {
+inline Deal deal_of(int heads, uint32_t items) {
   int c = 8;
   while (heads % c != 0) c /= 2;
-  return Deal{c, 8 / c, tiles};
+  return Deal{c, 8 / c, items};
 }
 inline uint32_t deal_grid(const Deal& d, int heads) {
-  const uint64_t n = (uint64_t)(heads / d.classes) * d.tiles;
+  const uint64_t n = (uint64_t)(heads / d.classes) * d.items;
   return (uint32_t)((n + d.per - 1) / d.per * 8);
 }
-template <bool KEYS>
-__device__ __forceinline__ bool dealt(const Deal& d, int heads, uint32_t b, int& head, uint32_t& tile) {
-  const uint32_t x = b & 7u, c = x % d.classes, j = (b >> 3) * d.per + x / d.classes, h = j / d.tiles;
+__device__ __forceinline__ bool dealt(const Deal& d, int heads, uint32_t b, int& head, uint32_t& item) {
+  const uint32_t x = b & 7u, c = x % d.classes, j = (b >> 3) * d.per + x / d.classes, h = j / d.items;
   if (h >= (uint32_t)(heads / d.classes)) return false;
   head = (int)(c + d.classes * h);
-  tile = KEYS ? j - h * d.tiles : d.tiles - 1 - (j - h * d.tiles);
+  item = j - h * d.items;
   return true;
 }
 
-// The sequence that has tile `tile` of the list of all sequences' tiles of kTile rows each (rows: queries times the group, or
-// keys), and which of its tiles that is.  Every lane of a wave takes part, each with a sequence.
+// A tile of a sequence and a piece of it.
+struct Item {
+  Seq s;
+  uint32_t tile;
+  int32_t piece;
+};
+
+// Item `item` of the list of all sequences' items: of tiles of TILE rows (queries times the group) from the last on, or of keys
+// from the first on, either way beginning with those that have most to do under a causal mask.  Every lane of a wave takes part,
+// each with a sequence.
 template <bool KEYS, int TILE>
-__device__ __forceinline__ bool find_tile(const AttnArgs& A, uint32_t tile, Seq& s, uint32_t& at) {
+__device__ __forceinline__ bool find_item(const AttnArgs& A, const Pieces& p, uint32_t item, Item& found) {
   const int lane = threadIdx.x & 63;
-  uint32_t before = 0;
-  for (int32_t s0 = 0; s0 < A.sequences; s0 += 64) {
-    Seq mine{0, 0, 0, 0};
+  auto count = [&](int32_t s0, Seq& mine, uint32_t& tiles, uint32_t& pieces) {   // items up to the lane's sequence
+    mine = Seq{0, 0, 0, 0};
     if (s0 + lane < A.sequences) mine = seq_of(A, s0 + lane);
-    const uint32_t rows = KEYS ? (uint32_t)mine.nk : (uint32_t)mine.nq * (uint32_t)A.group;
-    uint32_t sum = (rows + TILE - 1) / TILE;
-    const uint32_t own = sum;
+    const uint32_t rows = (uint32_t)mine.nq * (uint32_t)A.group, keys = (uint32_t)mine.nk;
+    tiles = ((KEYS ? keys : rows) + TILE - 1) / TILE;
+    pieces = min((uint32_t)p.most, max(1u, ((KEYS ? rows : keys) + p.keys - 1) / p.keys));
+    uint32_t sum = tiles * pieces;
 #pragma unroll
     for (int d = 1; d < 64; d <<= 1) {
       const uint32_t up = __shfl_up(sum, d);
       if (lane >= d) sum += up;
     }
-    const uint64_t behind = __ballot(before + sum > tile);
+    return sum;
+  };
+  // what is the same in every lane is said to be so: the code behind then branches for the whole wave
+  auto of = [](auto v, int src) { return (decltype(v))__builtin_amdgcn_readlane((int32_t)v, src); };
+  Seq mine;
+  uint32_t tiles, pieces, before = 0, sum = 0;
+  if (A.sequences <= 64) sum = count(0, mine, tiles, pieces);
+  if (!KEYS) {
+    uint32_t all = of(sum, 63);
+    if (A.sequences > 64) {
+      all = 0;
+      for (int32_t s0 = 0; s0 < A.sequences; s0 += 64) all += of(count(s0, mine, tiles, pieces), 63);
+    }
+    if (item >= all) return false;
+    item = all - 1 - item;
+  }
+  for (int32_t s0 = 0; s0 < A.sequences; s0 += 64) {
+    if (A.sequences > 64) sum = count(s0, mine, tiles, pieces);
+    const uint64_t behind = __ballot(before + sum > item);
     if (behind != 0) {
       const int src = __builtin_ctzll(behind);
-      s.q0 = __shfl(mine.q0, src), s.k0 = __shfl(mine.k0, src);
-      s.nq = __shfl(mine.nq, src), s.nk = __shfl(mine.nk, src);
-      at = tile - before - __shfl(sum - own, src);
-      // the same in every lane; say so
-      s.q0 = (int64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int32_t)s.q0);
-      s.k0 = (int64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int32_t)s.k0);
-      s.nq = __builtin_amdgcn_readfirstlane(s.nq), s.nk = __builtin_amdgcn_readfirstlane(s.nk);
-      at = __builtin_amdgcn_readfirstlane(at);
-      return at < ((KEYS ? (uint32_t)s.nk : (uint32_t)s.nq * (uint32_t)A.group) + TILE - 1) / TILE;
+      const uint32_t in = item - before - of(sum - tiles * pieces, src), each = of(pieces, src);
+      found.s = Seq{of(mine.q0, src), of(mine.k0, src), of(mine.nq, src), of(mine.nk, src)};
+      found.tile = in / each;
+      found.piece = (int32_t)(in - found.tile * each);
+      return found.tile < of(tiles, src);
     }
-    before += __shfl(sum, 63);
+    before += of(sum, 63);
   }
   return false;
 }
@@ -306,6 +327,48 @@ __device__ __forceinline__ Span list_span(const AttnArgs& A, const Seq& s, int32
 // Pieces that the keys (or rows) [lo, hi) of a tile are shared out to.
 __device__ __forceinline__ int pieces_of(const Span& x, const Pieces& p) {
   return min(p.most, max(1, (x.hi - x.lo + p.keys - 1) / p.keys));
+}
+
+// A row (of tokens_q x heads) whose pieces half a wave adds up.
+struct JoinRow {
+  int64_t at, t;
+  Seq s;
+  int32_t h, r;   // head, and row of its group's list
+  bool on;
+  __device__ __forceinline__ JoinRow(const AttnArgs& A, int64_t at_) : at(at_), t(at_ / A.heads), s(), h(0), r(0), on(t < A.tokens_q) {
+    if (on) s = seq_at(A, A.start_q, t);
+    on = on && t >= s.q0 && t < s.q0 + s.nq;
+    h = (int32_t)(at - t * A.heads);
+    if (on) r = (int32_t)(t - s.q0) * A.group + h % A.group;
+  }
+  // That of the half with lane `src`, for the whole wave.
+  __device__ __forceinline__ JoinRow of(int src) const {
+    JoinRow x = *this;
+    x.at = __shfl(at, src), x.t = __shfl(t, src), x.h = __shfl(h, src), x.r = __shfl(r, src);
+    x.s.q0 = __shfl(s.q0, src), x.s.k0 = __shfl(s.k0, src), x.s.nq = __shfl(s.nq, src), x.s.nk = __shfl(s.nk, src);
+    return x;
+  }
+};
+
+// sum[0..3] += weight(p) part[p next + c + 0..3] over the pieces, eight of them under way at once.
+template <class W>
+__device__ __forceinline__ void add_parts(const __attribute__((address_space(1))) float* part, int64_t next, int c, int pieces, W weight,
+                                          float* sum) {
+  for (int p0 = 0; __any(p0 < pieces); p0 += 8) {
+    f32x4_t v[8];
+#pragma unroll
+    for (int p = 0; p < 8; ++p) {
+      v[p] = 0.0f;
+      if (p0 + p < pieces) v[p] = *(global_ptr<const f32x4_t>)(part + (p0 + p) * next + c);
+    }
+#pragma unroll
+    for (int p = 0; p < 8; ++p) {
+      const float w = weight(p0 + p);
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        if (p0 + p < pieces) sum[i] = fmaf(v[p][i], w, sum[i]);
+    }
+  }
 }
 
 // Whether the values of a wave hold a NaN or an infinity: 0 times such a value is NaN, and a sum with one stays one.

@@ -248,20 +248,25 @@ size_t most_parts(int64_t owners, int64_t list, double f) {
 
 }  // namespace
 
+uint32_t attend_items(int64_t rows, int64_t list, int64_t sequences, const Pieces& p) {
+  // a sequence of n tiles and length m has n min(most, m / keys + 1) items at most
+  const int64_t tiles = rows / kAttnTileRows + sequences, longest = rows / kAttnTileRows + 1;
+  if (p.most == 1) return (uint32_t)tiles;
+  return (uint32_t)std::min(tiles * p.most, longest * (list / p.keys + sequences));
+}
+
 AttendPlan plan_attend(const iso_attn& a, bool grad) {
   const int64_t rows = a.tokens_q * a.heads, keys = a.tokens_k * a.heads_kv, list = a.tokens_q * (a.heads / a.heads_kv);
   constexpr double kRows = 12.8, kKeys = 9.1;
   AttendPlan P;
+  auto parts = [](size_t n) { return align_up(sizeof(float) * kPartLd * n, 256); };
   P.rows = share_out(rows, a.tokens_k, a.sequences, a.heads_kv, kRows);
-  size_t parts = most_parts(rows, a.tokens_k, kRows);
-  P.part = kStatusBytes;
-  if (grad) {
-    P.keys = share_out(keys, list, a.sequences, a.heads_kv, kKeys);
-    parts = std::max(parts, 2 * most_parts(keys, list, kKeys));
-    // a panel's rows are read whole: up to 32 behind the last one
-    P.part = align_up(kStatusBytes + sizeof(float) * (2 * (size_t)rows + 64), 256);
-  }
-  P.total = P.part + align_up(sizeof(float) * kPartLd * parts, 256);
+  // a panel's rows are read whole, and one panel too many: up to 64 behind the last one
+  P.part = grad ? align_up(kStatusBytes + sizeof(float) * (2 * (size_t)rows + 64), 256) : kStatusBytes;
+  P.key_part = P.total = P.part + parts(most_parts(rows, a.tokens_k, kRows));
+  if (!grad) return P;
+  P.keys = share_out(keys, list, a.sequences, a.heads_kv, kKeys);
+  P.total = P.key_part + parts(2 * most_parts(keys, list, kKeys));
   return P;
 }
 

@@ -160,17 +160,17 @@ bool attend_fits(const iso_attn& a);
 constexpr int kAttnTileRows = 128;     // rows (queries times the group) or keys of a tile
 constexpr int kPartLd = 132;           // floats of a row's piece: its sums, maximum and sum of weights
 
-// Tiles of `rows` rows in `sequences` sequences at most.
-inline int64_t attend_tiles(int64_t rows, int64_t sequences) { return rows / kAttnTileRows + sequences; }
-
 // How the keys (or rows) that a tile walks over are shared out: `most` pieces, each of at least `keys`.
 struct Pieces {
   int32_t most = 1, keys = 1;
 };
 
+// Pieces of tiles of `rows` rows in `sequences` sequences that walk over `list` keys (or the other way round) at most, a head.
+uint32_t attend_items(int64_t rows, int64_t list, int64_t sequences, const Pieces& p);
+
 struct AttendPlan {
   Pieces rows, keys;   // of tiles of rows (O, dQ) and of keys (dK and dV)
-  size_t part = 0, total = 0;
+  size_t part = 0, key_part = 0, total = 0;
 };
 AttendPlan plan_attend(const iso_attn& a, bool grad);
 size_t attend_workspace_bytes(const iso_attn& a, int dt, bool grad);
