@@ -76,6 +76,7 @@ struct Rows {
 
 typedef __attribute__((address_space(3))) const u32x4_t* lds_piece;
 typedef __attribute__((address_space(3))) const float* lds_float;
+typedef __attribute__((address_space(3))) uint32_t* lds_word;
 
 // Where a lane reads fragments of panels: rows, 16 bytes a group, for products that sum over dimensions; and columns, for those
 // that sum over rows.  Groups, 32-dimension tiles and rows are bits of the permuted piece, so one exclusive or makes each address

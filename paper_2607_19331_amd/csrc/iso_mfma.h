@@ -15,6 +15,12 @@ typedef __attribute__((address_space(3))) f32x4_t* lds_f32x4;
 typedef __bf16 bf16x8_t __attribute__((ext_vector_type(8)));
 typedef float f32x16_t __attribute__((ext_vector_type(16)));
 
+// v minus both bf16 values of a pair.
+__device__ __forceinline__ float minus_pair(uint32_t pair, float v) {
+  typedef __bf16 bf16x2_t __attribute__((ext_vector_type(2)));
+  return __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2_t, pair), __builtin_bit_cast(bf16x2_t, 0xBF80BF80u), v, false);
+}
+
 // Descriptor of a buffer of `left` bytes: reads past its end give zeros.
 __device__ __forceinline__ u32x4_t buffer_of(const uint8_t* p, int64_t left) {
   const uint64_t a = (uint64_t)p;

@@ -4,7 +4,10 @@ Bounds.  Scores are dot products of d terms in binary32, off by at most (d + 8) 
 products' sum, the scale, the subtraction of a maximum or of L, and the exponential (an error of its own of 2^-23).  That is a
 relative error `ep` of a probability.  The forward pass divides by a sum of them, which is off by the largest ep too and by
 (m + 8) 2^-24 for m terms; bf16 adds half a step, 2^-8, for the rounding of each P (of P and of S in the gradient), and the
-result its own rounding u.  dP - D is off by (d + 8) 2^-24 of its terms' magnitudes.  1 + 2^-5 covers the products of bounds."""
+result its own rounding u.  dP - D is off by (d + 8) 2^-24 of its terms' magnitudes.  1 + 2^-5 covers the products of bounds.
+
+dQ in bf16 is sum round(S_j) k_j + c sum (S_j - round(S_j)), c the mean of some keys that the query sees: off by
+sum (S_j - round(S_j)) (k_j - c), at most 2^-8 sum |S_j| (|k_j| + max |k|), the maximum over the keys that the query sees."""
 import numpy as np
 
 from oracle import gradients as gr
@@ -127,6 +130,9 @@ class Case:
                 eds = np.abs(ds) * (ep + ur + (max(n * self.heads // self.kv, m) + 8) * E24) + p * edp
                 edv = p * (ep + ur + (n * self.heads // self.kv + 8) * E24)
                 tol[0][rows, c] = self.scale * eds @ np.abs(k)
+                if ur and m:
+                    widest = np.stack([np.abs(k)[see[i]].max(0, initial=0.0) for i in range(n)]) if n else np.zeros((0, self.dim))
+                    tol[0][rows, c] += self.scale * ur * np.abs(ds).sum(1, keepdims=True) * widest
                 tol[1][keys, e] += self.scale * eds.T @ np.abs(q)
                 tol[2][keys, e] += edv.T @ np.abs(do)
         for x, w, t, at in zip(got, want, tol, (self.at_q, self.at_k, self.at_k)):
