@@ -220,7 +220,7 @@ __global__ void __launch_bounds__(256, (DT == ISO_F32 && D == 128 ? 1 : 2)) k_at
 }
 
 // Adds up the pieces of a row, half a wave a row.
-template <int DT>
+template <int DT, int U>
 __global__ void __launch_bounds__(256) k_attend_join(AttnArgs A) {
   constexpr int kRows = 32 * kAttnWaves;
   const int lane = threadIdx.x & 63, l32 = lane & 31, c = 4 * l32;
@@ -249,7 +249,7 @@ __global__ void __launch_bounds__(256) k_attend_join(AttnArgs A) {
 #pragma unroll
   for (int d = 16; d > 0; d >>= 1) sum += __shfl_xor(sum, d);
   float o[4] = {};
-  add_parts(part, next, c, on && c < A.dim ? pieces : 0, [&](int p) { return __shfl(p < 32 ? f[0] : f[1], (lane & 32) | (p & 31)); }, o);
+  add_parts<U>(part, next, c, on && c < A.dim ? pieces : 0, [&](int p) { return __shfl(p < 32 ? f[0] : f[1], (lane & 32) | (p & 31)); }, o);
   int32_t lo = 0, hi = 0;
   if (on) keys_of(A, j.s, j.r / A.group, lo, hi);
   const float inv = hi > lo ? 1.0f / sum : 0.0f;
@@ -273,7 +273,9 @@ template <int DT, int D>
 hipError_t forward(const AttnArgs& A, hipStream_t s) {
   const Deal deal = deal_of(A.heads_kv, attend_items(A.tokens_q * A.group, A.tokens_k, A.sequences, A.pieces));
   k_attend<DT, D><<<deal_grid(deal, A.heads_kv) + 1, 256, 4 * Panel<DT, D>::kBytes, s>>>(A, deal);   // one looks at the offsets
-  if (A.pieces.most > 1) k_attend_join<DT><<<(unsigned)((A.tokens_q * A.heads + 7) / 8), 256, 0, s>>>(A);
+  const unsigned rows = (unsigned)((A.tokens_q * A.heads + 7) / 8);
+  if (A.pieces.most > 4) k_attend_join<DT, 8><<<rows, 256, 0, s>>>(A);
+  else if (A.pieces.most > 1) k_attend_join<DT, 4><<<rows, 256, 0, s>>>(A);
   return hipGetLastError();
 }
 

@@ -267,7 +267,7 @@ __device__ __forceinline__ void dq_join(const AttnArgs& A, uint32_t block) {
   const int pieces = pieces_of(all, A.pieces);
   const bool on = j.on && pieces > 1;
   float v[4] = {}, t = 0.0f;
-  add_parts(gmem((const float*)A.part) + j.at * kPartLd, A.tokens_q * A.heads * kPartLd, c, on && c < A.dim ? pieces : 0,
+  add_parts<4>(gmem((const float*)A.part) + j.at * kPartLd, A.tokens_q * A.heads * kPartLd, c, on && c < A.dim ? pieces : 0,
             [](int) { return 1.0f; }, v);
 #pragma unroll
   for (int i = 0; i < 4; ++i) v[i] *= A.scale, t = fmaf(v[i], 0.0f, t);
@@ -555,7 +555,7 @@ __device__ __forceinline__ void dkv_join(const AttnArgs& A, uint32_t block) {
   if (pieces == 1) return;
   const bool values = lane >= 32;
   float v[4] = {}, bad = 0.0f;
-  add_parts(gmem((const float*)A.key_part) + at * (2 * kPartLd) + (values ? kPartLd : 0), A.tokens_k * A.heads_kv * (2 * kPartLd), c,
+  add_parts<4>(gmem((const float*)A.key_part) + at * (2 * kPartLd) + (values ? kPartLd : 0), A.tokens_k * A.heads_kv * (2 * kPartLd), c,
             c < A.dim ? pieces : 0, [](int) { return 1.0f; }, v);
 #pragma unroll
   for (int i = 0; i < 4; ++i) {

@@ -351,19 +351,19 @@ struct JoinRow {
   }
 };
 
-// sum[0..3] += weight(p) part[p next + c + 0..3] over the pieces, eight of them under way at once.
-template <class W>
+// sum[0..3] += weight(p) part[p next + c + 0..3] over the pieces, U of them under way at once.
+template <int U, class W>
 __device__ __forceinline__ void add_parts(const __attribute__((address_space(1))) float* part, int64_t next, int c, int pieces, W weight,
                                           float* sum) {
-  for (int p0 = 0; __any(p0 < pieces); p0 += 8) {
-    f32x4_t v[8];
+  for (int p0 = 0; __any(p0 < pieces); p0 += U) {
+    f32x4_t v[U];
 #pragma unroll
-    for (int p = 0; p < 8; ++p) {
+    for (int p = 0; p < U; ++p) {
       v[p] = 0.0f;
       if (p0 + p < pieces) v[p] = *(global_ptr<const f32x4_t>)(part + (p0 + p) * next + c);
     }
 #pragma unroll
-    for (int p = 0; p < 8; ++p) {
+    for (int p = 0; p < U; ++p) {
       const float w = weight(p0 + p);
 #pragma unroll
       for (int i = 0; i < 4; ++i)

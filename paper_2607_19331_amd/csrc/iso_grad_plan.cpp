@@ -223,11 +223,13 @@ namespace {
 
 constexpr int kPieceKeys = 256;         // fewest keys of a piece
 constexpr int kMostPieces = 64;         // of a tile
-constexpr int64_t kFullTiles = 2048;    // four rounds of workgroups, two a CU: heavy tiles first, these balance by themselves
+constexpr int64_t kFullTiles = 1536;    // three rounds of workgroups, two a CU: heavy tiles first, these balance by themselves
 
 // Tiles of `owners` rows walk over `length` keys on average.  In p pieces a tile's time falls by p, and every row writes and
-// reads p partial sums: the sum of both is least at p = f sqrt(length / owners), where f was measured to be about 12.8 for rows
-// and 9.1 for keys (twice the sums).  Microseconds, forward pass in 1 to 16 pieces: see the pieces' table in iso_attend.hip.
+// reads p partial sums: the sum of both is least at p = f sqrt(length / owners).  f was measured, 6.5 for rows and 9.1 for keys
+// (which have dK and dV).  Microseconds with f at 12.8, 9, 6.5 and 5: 2048 tokens, 12 heads, forward 43, 44, 42, 42; 512 tokens
+// 18.9, 18.9, 16.9, 17.0; 64 new tokens after 4032 for four sequences, 28 heads, 45, 38, 36, 40; backward with keys' f at 9.1, 6, 4
+// and 2.5: 2048 tokens, 12 heads, 91, 85, 106, 135; 16 samples of 1 to 2048 tokens 313, 347, 460, 458.
 Pieces share_out(int64_t owners, int64_t list, int64_t sequences, int64_t heads, double f) {
   Pieces P;
   if (owners <= 0 || list <= 0 || sequences <= 0) return P;
@@ -257,7 +259,7 @@ uint32_t attend_items(int64_t rows, int64_t list, int64_t sequences, const Piece
 
 AttendPlan plan_attend(const iso_attn& a, bool grad) {
   const int64_t rows = a.tokens_q * a.heads, keys = a.tokens_k * a.heads_kv, list = a.tokens_q * (a.heads / a.heads_kv);
-  constexpr double kRows = 12.8, kKeys = 9.1;
+  constexpr double kRows = 6.5, kKeys = 9.1;
   AttendPlan P;
   auto parts = [](size_t n) { return align_up(sizeof(float) * kPartLd * n, 256); };
   P.rows = share_out(rows, a.tokens_k, a.sequences, a.heads_kv, kRows);
