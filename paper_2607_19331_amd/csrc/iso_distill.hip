@@ -45,16 +45,24 @@ __device__ __forceinline__ Lse join(Lse a, Lse b, float c) {
   return Lse{m, a.s * __builtin_amdgcn_exp2f((a.m - ref) * c) + b.s * __builtin_amdgcn_exp2f((b.m - ref) * c)};
 }
 
-template <int N>
-__device__ __forceinline__ Lse block_lse(Lse v, float c, float (*lds)[2]) {
+// Of a workgroup of N: every wave puts its own into LDS, and after a barrier all of them are joined.
+__device__ __forceinline__ void put_lse(Lse v, float c, float (*lds)[2]) {
 #pragma unroll
   for (int d = 32; d > 0; d >>= 1) v = join(v, Lse{__shfl_xor(v.m, d), __shfl_xor(v.s, d)}, c);
   if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6][0] = v.m, lds[threadIdx.x >> 6][1] = v.s;
-  __syncthreads();
-  v = Lse{lds[0][0], lds[0][1]};
+}
+template <int N>
+__device__ __forceinline__ Lse get_lse(float c, const float (*lds)[2]) {
+  Lse v{lds[0][0], lds[0][1]};
 #pragma unroll
   for (int i = 1; i < N / 64; ++i) v = join(v, Lse{lds[i][0], lds[i][1]}, c);
   return v;
+}
+template <int N>
+__device__ __forceinline__ Lse block_lse(Lse v, float c, float (*lds)[2]) {
+  put_lse(v, c, lds);
+  __syncthreads();
+  return get_lse<N>(c, lds);
 }
 
 // Adds values to a maximum and sum, which is scaled once for all of them.
@@ -296,63 +304,135 @@ __global__ void __launch_bounds__(256) k_distill_row(DistillArgs A) {
   put_entry<DT>(A, row, 0, A.vocab, F, r, z, lse2);
 }
 
+// A list before it is looked at: thread e has entry e.
+struct RawEntry {
+  int64_t id = 0;
+  float y = 0.0f;
+  __device__ __forceinline__ void load(const DistillArgs& A, int64_t row) {
+    if ((int)threadIdx.x >= A.top) return;
+    id = id_at(A, row * A.top + threadIdx.x);
+    y = gmem(A.y)[row * A.top + threadIdx.x];
+  }
+};
+
+template <int N>
+struct HeldSpace {
+  ListSpace list;
+  float red[16][2], value[ISO_DISTILL_MAX_TOP];
+  double sums[4];
+  int16_t next[ISO_DISTILL_MAX_TOP];
+  int32_t head[N];   // the first of the entries that lie in a lane's columns; -1: none
+};
+
 // Loss and gradient of a row that a workgroup of N holds in registers, PER pieces of 16 bytes a lane: read once, written once.
-// All of a row is under way at once; what a CU does between its loads and its stores, other CUs' loads and stores fill.
+// All of a row is under way at once; what a CU does between its loads and its stores, other CUs' loads and stores fill.  Entries
+// change the pieces they lie in before these are stored (a lane has a list of its own): written after them they would have to
+// wait for the stores.  Workgroups that walk over rows and load a piece of the next row where one of this is stored were tried:
+// the registers for it cost more than it gave (4096 x 152064 bf16: 577 us).
 template <int DT, int N, int PER, bool STREAM>
 __global__ void __launch_bounds__(N) k_distill_held(DistillArgs A) {
   constexpr int V = kVec<DT>;
-  __shared__ ListSpace S;
-  __shared__ double sums[4];
-  const int64_t row = blockIdx.x, from = row * A.ld, to = row * A.ld_grad;
-  const int32_t vocab = (int32_t)A.vocab;
-  if (row == 0 && A.tokens * A.top <= kFewEntries) check_ids(A);
-  // the first column of a round is the same in all lanes and goes into the instruction's base
   using bits = typename Fmt<DT>::bits_t;
+  __shared__ HeldSpace<N> S;
+  const int32_t vocab = (int32_t)A.vocab;
+  const int e = threadIdx.x;
   const uint32_t mine = threadIdx.x * V;
+  const int64_t row = blockIdx.x;
+  if (row == 0 && A.tokens * A.top <= kFewEntries) check_ids(A);
   u32x4_t w[PER];
+  // the first column of a round is the same in all lanes and goes into the instruction's base
+  RawEntry raw;
+  raw.load(A, row);
 #pragma unroll
   for (int p = 0; p < PER; ++p) {
-    const bits* const at = (const bits*)A.z + from + p * N * V;
+    const bits* const at = (const bits*)A.z + row * A.ld + p * N * V;
     if ((p + 1) * N * V <= vocab) w[p] = load_raw<DT>(at, mine);
     else w[p] = load_end<DT>(at, mine, vocab - p * N * V - (int32_t)mine);
   }
-  // what is unpacked is unpacked again where it is needed next: there are registers for the row, not for its values twice over
-  auto again = [&] {
-#pragma unroll
-    for (int p = 0; p < PER; ++p) asm volatile("" : "+v"(w[p]));
-  };
+  // the list, and the logits of its entries behind the row's own
+  Entry r;
+  float y = -INFINITY;
+  if (e < A.top) {
+    if (outside(A, raw.id)) {
+      if (A.tokens * A.top > kFewEntries) atomicOr(A.status, kStatusIndex);
+    } else if (raw.id != A.pad_id && raw.y != -INFINITY) {
+      r.id = (int32_t)raw.id;
+      y = raw.y;
+    }
+  }
+  const float z = r.id >= 0 ? load_z<DT>(A, row * A.ld + r.id) : 0.0f;
+  const float weight = A.w != nullptr ? gmem(A.w)[row] : 1.0f;
+  // the row, as it comes in, one piece after the other
   Lse l;
 #pragma unroll
-  for (int p = 0; p < PER; p += 2) {   // as they come in, one after the other
+  for (int p = 0; p < PER; p += 2) {
     asm volatile("" : "+v"(w[p]), "+v"(w[p + 1]), "+v"(l.s));
     float v[2 * V];
 #pragma unroll
     for (int u = 0; u < 2; ++u) unpack_raw<DT>(w[p + u], v + u * V);
     add_to<2 * V>(l, v, A.exp2_t);
   }
-  again();
-  bool any;
-  Entry r = list_of<N>(A, row, S, any);
-  const float z = r.id >= 0 ? load_z<DT>(A, from + r.id) : 0.0f;
-  __syncthreads();   // list_of's space again
-  const double lse = lse_of(A, block_lse<N>(l, A.exp2_t, S.red));
-  store_loss<DT>(A, row, r, z, lse, any, sums);
-  merge(A, S, r);
-  const Factor F(A, row, any);
-  const float lse2 = (float)(lse * 1.4426950408889634);
-  before_writes(z);
+  put_lse(l, A.exp2_t, S.red);
+  Lse t{y, r.id >= 0 ? 1.0f : 0.0f};
+  if (r.id >= 0 && !(fabsf(y) < INFINITY)) t.s = NAN;   // an infinite or NaN logit of the teacher
+  put_lse(t, A.exp2_t, S.list.red);
+  if (e < ISO_DISTILL_MAX_TOP) S.list.id[e] = r.id, S.list.t[e] = y;
+  S.head[e] = -1;
+  __syncthreads();
+  l = get_lse<N>(A.exp2_t, S.red);
+  t = get_lse<256>(A.exp2_t, S.list.red);   // the first four waves hold the entries
+  const bool any = t.s != 0.0f;
+  const float log_s = logf(t.s);
+  auto share = [&](float v) { return (v - t.m) * A.inv_t - log_s; };
+  if (r.id >= 0) r.log_t = share(y), r.t = __builtin_amdgcn_exp2f(r.log_t * kLog2e);
+  const double lse = lse_of(A, l);
+  const float lse2 = (float)(lse * 1.4426950408889634), f = weight * (float)A.t;
+  const bool zero = !any || weight == 0.0f;
+  double part = r.id >= 0 && r.t != 0.0f ? (double)r.t * ((double)r.log_t - (double)z / A.t + lse) : 0.0;
+#pragma unroll
+  for (int d = 32; d > 0; d >>= 1) part += __shfl_xor(part, d);
+  if ((e & 63) == 0 && e < 256) S.sums[e >> 6] = part;
+  if (!zero && r.id >= 0) {   // as merge(), but for the logits in LDS; the first of the entries adds in their order
+    r.first = true;
+    for (int i = 0; i < A.top; ++i)
+      if (S.list.id[i] == r.id && i != e) {
+        if (i < e) r.first = false;
+        r.t += __builtin_amdgcn_exp2f(share(S.list.t[i]) * kLog2e);
+      }
+  }
+  if (r.first) {
+    S.value[e] = f * (__builtin_amdgcn_exp2f(fmaf(z, A.exp2_t, -lse2)) - r.t);
+    S.next[e] = (int16_t)atomicExch(&S.head[r.id / V % N], e);
+  }
+  // every entry has its logit: the gradient may lie over the logits
+  asm volatile("s_waitcnt vmcnt(0)" ::"v"(z) : "memory");
+  __syncthreads();
+  if (e == 0) {
+    part = S.sums[0] + S.sums[1] + S.sums[2] + S.sums[3];
+    gmem(A.loss)[row] = zero ? 0.0f : (float)(weight * A.t * A.t * part);
+    gmem(A.lse)[row] = (float)lse;
+  }
+  const int head = S.head[e];
+  uint32_t has = 0;
+  for (int i = head; i >= 0; i = S.next[i]) has |= 1u << (S.list.id[i] / (N * V));
 #pragma unroll
   for (int p = 0; p < PER; ++p) {
-    asm volatile("" : "+v"(w[p]));
-    bits* const at = (bits*)A.grad + to + p * N * V;
+    asm volatile("" : "+v"(w[p]));   // unpacked again: there are registers for the row, not for its values twice over
+    bits* const at = (bits*)A.grad + row * A.ld_grad + p * N * V;
     const int32_t left = vocab - p * N * V - (int32_t)mine;
     if (left <= 0) continue;
     float v[V] = {};
-    if (!F.zero) grads_of<DT>(A, F.f, w[p], lse2, v);
+    if (!zero) grads_of<DT>(A, f, w[p], lse2, v);
+    if (has >> p & 1u)
+      for (int i = head; i >= 0; i = S.next[i]) {
+        const int32_t id = S.list.id[i];
+        if (id / (N * V) != p) continue;
+#pragma unroll
+        for (int j = 0; j < V; ++j) v[j] = id % V == j ? S.value[i] : v[j];
+      }
     if ((p + 1) * N * V <= vocab) store_elems<DT, V, STREAM>(at, mine, v);
     else store_elems<DT, V, STREAM>(at, mine, v, left);
   }
-  put_entry<DT>(A, row, 0, vocab, F, r, z, lse2);
 }
 
 // A piece of a row: its share of the sum, and from these the loss.
