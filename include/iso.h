@@ -627,15 +627,16 @@ iso_status iso_ckpt_weight_grad(const iso_weight_grad* g, int n, int dt, int dt_
  *  - Offsets are device memory, sequences + 1 values each, ascending, 0 <= start <= tokens.  A sequence whose
  *    offsets are no range of the rows is left out, and reported by iso_read_device_status (ISO_ERR_INDEX).
  *  - Rows of q, k and v that belong to no sequence are not read, and those of the outputs not written.
+ *  - Sizes past the limits below are ISO_ERR_UNSUPPORTED.
  *  - A result depends on the keys (or queries) that are seen and on no others: what non-finite values others
  *    hold does not reach it.  Calls that meet non-finite values in a result work that part out once more, row
  *    by row and slowly.
  */
 #define ISO_ATTN_MAX_DIM 128
 #define ISO_ATTN_MAX_LD (1 << 21)
-#define ISO_ATTN_MAX_SEQUENCES (1 << 20)
-#define ISO_ATTN_MAX_GROUP 1024
-#define ISO_ATTN_MAX_ROWS (1 << 25)      /* tokens_q * heads, and tokens_k * heads_kv */
+#define ISO_ATTN_MAX_SEQUENCES (1 << 16)
+#define ISO_ATTN_MAX_GROUP 1024          /* heads / heads_kv */
+#define ISO_ATTN_MAX_ROWS (1 << 25)      /* tokens_q * heads, tokens_k * heads_kv; sequences * heads_kv is an eighth */
 
 /* Which pointers (and strides) are read depends on the call. */
 typedef struct iso_attn {
@@ -695,10 +696,11 @@ iso_status iso_attend_grad(const iso_attn* a, int dt, void* ws, size_t ws_bytes,
  *  - logits and grad are of type dt with any row strides.  grad may be logits itself (same stride).
  */
 #define ISO_DISTILL_MAX_TOP 256
+#define ISO_DISTILL_MAX_TOKENS (1 << 23)
 
 typedef struct iso_distill {
   const void* logits;        /* z: tokens x vocab, row stride ld                                     */
-  int64_t tokens, vocab, ld; /* tokens < 2^31, 1 <= vocab <= ISO_EMBED_MAX_VOCAB                     */
+  int64_t tokens, vocab, ld; /* up to ISO_DISTILL_MAX_TOKENS, 1 <= vocab <= ISO_EMBED_MAX_VOCAB         */
   const void* ids;           /* tokens x top, contiguous, of id_type                                 */
   int32_t id_type;
   int32_t top;               /* 1 <= top <= ISO_DISTILL_MAX_TOP                                      */

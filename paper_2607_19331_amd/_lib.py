@@ -14,8 +14,8 @@ I32, I64 = 0, 1
 NO_PAD = -(1 << 63)
 CKPT_GROUP = 32
 EMBED_MAX_VOCAB = 1 << 20
-ATTN_MAX_DIM, ATTN_MAX_LD, ATTN_MAX_SEQUENCES = 128, 1 << 21, 1 << 20
-DISTILL_MAX_TOP = 256
+ATTN_MAX_DIM, ATTN_MAX_LD, ATTN_MAX_SEQUENCES, ATTN_MAX_GROUP, ATTN_MAX_ROWS = 128, 1 << 21, 1 << 16, 1024, 1 << 25
+DISTILL_MAX_TOP, DISTILL_MAX_TOKENS = 256, 1 << 23
 MERGE_TA, MERGE_TIES, MERGE_RAM = 0, 1, 2
 UPDATE_APPLY, UPDATE_FUSED, UPDATE_SPECTRAL, UPDATE_ORTHO = 0, 1, 2, 3
 (OP_TOPK, OP_SIGN, OP_MERGE, OP_UPDATE_APPLY, OP_UPDATE_FUSED, OP_UPDATE_FUSED_SELECT, OP_UPDATE_SPECTRAL,

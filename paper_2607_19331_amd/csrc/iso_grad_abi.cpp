@@ -146,7 +146,7 @@ iso_status check_attn(const iso_attn* a, int dt, int grad, bool pointers) {
 iso_status check_distill_sizes(const iso_distill* d) {
   if (d == nullptr || d->tokens < 0 || d->vocab < 1 || d->top < 1) return ISO_ERR_INVALID_ARG;
   if (d->id_type != ISO_I32 && d->id_type != ISO_I64) return ISO_ERR_INVALID_ARG;
-  if (d->tokens >= (1ll << 31) || d->vocab > ISO_EMBED_MAX_VOCAB || d->top > ISO_DISTILL_MAX_TOP) return ISO_ERR_UNSUPPORTED;
+  if (d->tokens > ISO_DISTILL_MAX_TOKENS || d->vocab > ISO_EMBED_MAX_VOCAB || d->top > ISO_DISTILL_MAX_TOP) return ISO_ERR_UNSUPPORTED;
   return ISO_OK;
 }
 

@@ -213,10 +213,11 @@ size_t weight_grad_workspace_bytes(const iso_weight_grad* g, int n, int dt) {
 // ---- attention -----------------------------------------------------------------------------------------------------
 
 bool attend_fits(const iso_attn& a) {
-  // a row (query head) a wave of 64 lanes in launches of fewer than 2^32 threads
-  const int64_t most = 1ll << 25;
-  if (a.heads / a.heads_kv > ISO_ATTN_MAX_GROUP) return false;
-  return a.tokens_q <= most && a.tokens_k <= most && a.heads <= most && a.tokens_q * a.heads <= most && a.tokens_k * a.heads_kv <= most;
+  // launches hold fewer than 2^32 threads: a workgroup of 256 for up to 128 rows or keys of a sequence and kv head, and for eight
+  // rows that are joined
+  const int64_t most = ISO_ATTN_MAX_ROWS;
+  if (a.heads / a.heads_kv > ISO_ATTN_MAX_GROUP || a.tokens_q > most || a.tokens_k > most) return false;
+  return a.tokens_q * a.heads <= most && a.tokens_k * a.heads_kv <= most && a.sequences * a.heads_kv <= most / 8;
 }
 
 namespace {

@@ -41,7 +41,9 @@ def test_attend_refusals(call):
                dict(start_k=FAKE + 1), dict(ld_q=260), dict(ld_k=129), dict(ld_v=132), dict(ld_out=257)):
         assert call(attn(**kw)) == _lib.ERR_ALIGNMENT, kw
     for kw in (dict(dim=60), dict(dim=136), dict(sequences=_lib.ATTN_MAX_SEQUENCES + 1), dict(ld_q=_lib.ATTN_MAX_LD + 8),
-               dict(heads=1 << 16, heads_kv=1), dict(tokens_q=1 << 40), dict(tokens_k=1 << 31), dict(tokens_q=(1 << 63) - 1)):
+               dict(heads=1 << 16, heads_kv=1), dict(heads=1025, heads_kv=1, dim=8), dict(tokens_q=(_lib.ATTN_MAX_ROWS >> 2) + 1),
+               dict(tokens_k=(_lib.ATTN_MAX_ROWS >> 1) + 1), dict(heads=512, heads_kv=512, dim=8, sequences=(1 << 13) + 1),
+               dict(tokens_q=1 << 40), dict(tokens_k=1 << 31), dict(tokens_q=(1 << 63) - 1)):
         assert call(attn(**kw)) == _lib.ERR_UNSUPPORTED, kw
     assert call(attn(), ws=None) == _lib.ERR_WORKSPACE
     assert call(attn(), ws_bytes=255) == _lib.ERR_WORKSPACE
@@ -113,7 +115,7 @@ def test_distill_refusals(call):
     for kw in (dict(logits=FAKE + 8), dict(ids=FAKE + 4), dict(teacher=FAKE + 4), dict(lse=FAKE + 8), dict(weight=FAKE + 2),
                dict(grad=FAKE + 2)):
         assert call(distill(**kw)) == _lib.ERR_ALIGNMENT, kw
-    for kw in (dict(tokens=1 << 31), dict(vocab=_lib.EMBED_MAX_VOCAB + 1), dict(top=_lib.DISTILL_MAX_TOP + 1), dict(ld=1 << 60),
+    for kw in (dict(tokens=1 << 31), dict(tokens=_lib.DISTILL_MAX_TOKENS + 1), dict(vocab=_lib.EMBED_MAX_VOCAB + 1), dict(top=_lib.DISTILL_MAX_TOP + 1), dict(ld=1 << 60),
                dict(ld_grad=1 << 60)):
         assert call(distill(**kw)) == _lib.ERR_UNSUPPORTED, kw
     assert call(distill(), ws=None) == _lib.ERR_WORKSPACE
