@@ -417,15 +417,13 @@ class Attn:
 
 def _attn(a: Attn):
     wide, narrow = a.heads * a.dim, a.heads_kv * a.dim
-
-    def ld(x, default):
-        return default if x is None else x
-
-    return _lib.IsoAttn(_ptr(a.q), _ptr(a.k), _ptr(a.v), ld(a.ld_q, wide), ld(a.ld_k, narrow), ld(a.ld_v, narrow),
-                        _ptr(a.start_q), _ptr(a.start_k), a.sequences, a.tokens_q, a.tokens_k, a.heads, a.heads_kv, a.dim,
-                        1 if a.causal else 0, a.window or 0, a.scale, _ptr(a.out), ld(a.ld_out, wide), _ptr(a.lse),
-                        _ptr(a.dout), ld(a.ld_dout, wide), _ptr(a.dq), _ptr(a.dk), _ptr(a.dv), ld(a.ld_dq, wide),
-                        ld(a.ld_dk, narrow), ld(a.ld_dv, narrow))
+    return _lib.IsoAttn(_ptr(a.q), _ptr(a.k), _ptr(a.v), wide if a.ld_q is None else a.ld_q,
+                        narrow if a.ld_k is None else a.ld_k, narrow if a.ld_v is None else a.ld_v, _ptr(a.start_q),
+                        _ptr(a.start_k), a.sequences, a.tokens_q, a.tokens_k, a.heads, a.heads_kv, a.dim, 1 if a.causal else 0,
+                        a.window or 0, a.scale, _ptr(a.out), wide if a.ld_out is None else a.ld_out, _ptr(a.lse), _ptr(a.dout),
+                        wide if a.ld_dout is None else a.ld_dout, _ptr(a.dq), _ptr(a.dk), _ptr(a.dv),
+                        wide if a.ld_dq is None else a.ld_dq, narrow if a.ld_dk is None else a.ld_dk,
+                        narrow if a.ld_dv is None else a.ld_dv)
 
 
 def attend_workspace(a: Attn, dtype, grad=False, device="cuda"):
