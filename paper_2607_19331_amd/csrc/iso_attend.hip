@@ -228,8 +228,9 @@ __global__ void __launch_bounds__(256) k_attend_join(AttnArgs A) {
   const Span all = j.on ? span_of(A, j.s, j.r / kRows * kRows, min(j.r / kRows * kRows + kRows, j.s.nq * A.group) - 1) : Span{0, 0, 0, 0};
   const int pieces = pieces_of(all, A.pieces);
   const bool on = j.on && pieces > 1;
-  const auto part = gmem((const float*)A.part) + j.at * kPartLd;
   const int64_t next = A.tokens_q * A.heads * kPartLd;
+  Parts<U> parts(A.part + j.at * kPartLd, next, c, on && c < A.dim ? pieces : 0);
+  const auto part = gmem((const float*)A.part) + j.at * kPartLd;
   float m[2], l[2], f[2];   // of pieces l32 and l32 + 32
 #pragma unroll
   for (int i = 0; i < 2; ++i) {
@@ -249,7 +250,7 @@ __global__ void __launch_bounds__(256) k_attend_join(AttnArgs A) {
 #pragma unroll
   for (int d = 16; d > 0; d >>= 1) sum += __shfl_xor(sum, d);
   float o[4] = {};
-  add_parts<U>(part, next, c, on && c < A.dim ? pieces : 0, [&](int p) { return __shfl(p < 32 ? f[0] : f[1], (lane & 32) | (p & 31)); }, o);
+  parts.add([&](int p) { return __shfl(p < 32 ? f[0] : f[1], (lane & 32) | (p & 31)); }, o);
   int32_t lo = 0, hi = 0;
   if (on) keys_of(A, j.s, j.r / A.group, lo, hi);
   const float inv = hi > lo ? 1.0f / sum : 0.0f;

@@ -267,8 +267,8 @@ __device__ __forceinline__ void dq_join(const AttnArgs& A, uint32_t block) {
   const int pieces = pieces_of(all, A.pieces);
   const bool on = j.on && pieces > 1;
   float v[4] = {}, t = 0.0f;
-  add_parts<4>(gmem((const float*)A.part) + j.at * kPartLd, A.tokens_q * A.heads * kPartLd, c, on && c < A.dim ? pieces : 0,
-            [](int) { return 1.0f; }, v);
+  Parts<4> parts(A.part + j.at * kPartLd, A.tokens_q * A.heads * kPartLd, c, on && c < A.dim ? pieces : 0);
+  parts.add([](int) { return 1.0f; }, v);
 #pragma unroll
   for (int i = 0; i < 4; ++i) v[i] *= A.scale, t = fmaf(v[i], 0.0f, t);
   const uint64_t bad = __ballot(t != 0.0f);
@@ -555,8 +555,8 @@ __device__ __forceinline__ void dkv_join(const AttnArgs& A, uint32_t block) {
   if (pieces == 1) return;
   const bool values = lane >= 32;
   float v[4] = {}, bad = 0.0f;
-  add_parts<4>(gmem((const float*)A.key_part) + at * (2 * kPartLd) + (values ? kPartLd : 0), A.tokens_k * A.heads_kv * (2 * kPartLd), c,
-            c < A.dim ? pieces : 0, [](int) { return 1.0f; }, v);
+  Parts<4> parts(A.key_part + at * (2 * kPartLd) + (values ? kPartLd : 0), A.tokens_k * A.heads_kv * (2 * kPartLd), c, c < A.dim ? pieces : 0);
+  parts.add([](int) { return 1.0f; }, v);
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
     if (!values) v[i] *= A.scale;

@@ -305,6 +305,19 @@ __device__ __forceinline__ Seq seq_at(const AttnArgs& A, const int32_t* start, i
   return seq_of(A, lo);
 }
 
+// The same where half a wave asks for one row: up to 64 sequences are looked at at once.
+__device__ __forceinline__ Seq seq_at_half(const AttnArgs& A, const int32_t* start, int64_t t) {
+  if (A.sequences > 64) return seq_at(A, start, t);
+  const int lane = threadIdx.x & 31, side = threadIdx.x & 32;
+  uint64_t ends = 0;
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    const bool behind = lane + 32 * i < A.sequences && gmem(start)[lane + 32 * i + 1] > t;
+    ends |= (__ballot(behind) >> side & 0xFFFFFFFFull) << (32 * i);
+  }
+  return ends != 0 ? seq_of(A, __builtin_ctzll(ends)) : Seq{};
+}
+
 // Keys that the rows of a tile (or of a wave of it) see between them, and those that all of them see.
 struct Span {
   int32_t lo, hi, lo_all, hi_all;
@@ -337,7 +350,7 @@ struct JoinRow {
   int32_t h, r;   // head, and row of its group's list
   bool on;
   __device__ __forceinline__ JoinRow(const AttnArgs& A, int64_t at_) : at(at_), t(at_ / A.heads), s(), h(0), r(0), on(t < A.tokens_q) {
-    if (on) s = seq_at(A, A.start_q, t);
+    if (on) s = seq_at_half(A, A.start_q, t);
     on = on && t >= s.q0 && t < s.q0 + s.nq;
     h = (int32_t)(at - t * A.heads);
     if (on) r = (int32_t)(t - s.q0) * A.group + h % A.group;
@@ -351,26 +364,36 @@ struct JoinRow {
   }
 };
 
-// sum[0..3] += weight(p) part[p next + c + 0..3] over the pieces, U of them under way at once.
-template <int U, class W>
-__device__ __forceinline__ void add_parts(const __attribute__((address_space(1))) float* part, int64_t next, int c, int pieces, W weight,
-                                          float* sum) {
-  for (int p0 = 0; __any(p0 < pieces); p0 += U) {
-    f32x4_t v[U];
+// sum[0..3] += weight(p) part[p next + c + 0..3] over the pieces, U of them under way at once: the first from the start.
+template <int U>
+struct Parts {
+  const __attribute__((address_space(1))) float* part;
+  int64_t next;
+  int pieces;
+  f32x4_t v[U];
+
+  __device__ __forceinline__ void load(int p0) {
 #pragma unroll
     for (int p = 0; p < U; ++p) {
       v[p] = 0.0f;
-      if (p0 + p < pieces) v[p] = *(global_ptr<const f32x4_t>)(part + (p0 + p) * next + c);
-    }
-#pragma unroll
-    for (int p = 0; p < U; ++p) {
-      const float w = weight(p0 + p);
-#pragma unroll
-      for (int i = 0; i < 4; ++i)
-        if (p0 + p < pieces) sum[i] = fmaf(v[p][i], w, sum[i]);
+      if (p0 + p < pieces) v[p] = *(global_ptr<const f32x4_t>)(part + (p0 + p) * next);
     }
   }
-}
+  __device__ __forceinline__ Parts(const float* at, int64_t next_, int c, int pieces_) : part(gmem(at) + c), next(next_), pieces(pieces_) { load(0); }
+  template <class W>
+  __device__ __forceinline__ void add(W weight, float* sum) {
+    for (int p0 = 0; __any(p0 < pieces); p0 += U) {
+      if (p0 > 0) load(p0);
+#pragma unroll
+      for (int p = 0; p < U; ++p) {
+        const float w = weight(p0 + p);
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          if (p0 + p < pieces) sum[i] = fmaf(v[p][i], w, sum[i]);
+      }
+    }
+  }
+};
 
 // Whether the values of a wave hold a NaN or an infinity: 0 times such a value is NaN, and a sum with one stays one.
 template <int N>
