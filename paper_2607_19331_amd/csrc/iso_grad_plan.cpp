@@ -225,6 +225,7 @@ namespace {
 constexpr int kPieceKeys = 256;         // fewest keys of a piece
 constexpr int kMostPieces = 64;         // of a tile
 constexpr double kSparse = 2.0;
+constexpr int64_t kRound = 512;         // workgroups at once
 constexpr int64_t kFullTiles = 1536;    // three rounds of workgroups, two a CU: heavy tiles first, these balance by themselves
 
 // Tiles of `owners` rows walk over `length` keys on average.  In p pieces a tile's time falls by p, and every row writes and
@@ -232,17 +233,23 @@ constexpr int64_t kFullTiles = 1536;    // three rounds of workgroups, two a CU:
 // (which have dK and dV).  Microseconds with f at 12.8, 9, 6.5 and 5: 2048 tokens, 12 heads, forward 43, 44, 42, 42; 512 tokens
 // 18.9, 18.9, 16.9, 17.0; 64 new tokens after 4032 for four sequences, 28 heads, 45, 38, 36, 40; backward with keys' f at 9.1, 6, 4
 // and 2.5: 2048 tokens, 12 heads, 91, 85, 106, 135; 16 samples of 1 to 2048 tokens 313, 347, 460, 458.  Tiles that are mostly
-// empty (one new token a sequence) write little: twice as many pieces (16 tokens over 77 to 8192 keys: 36 us, otherwise 40).
+// empty (one new token a sequence) write little and are bound by what a workgroup waits for at its start and each panel: twice as
+// many pieces, but all of them at once (16 tokens over 77 to 8192 keys, 28 heads: pieces of 256 keys 37.5 us, 512 30.0, 640 30.1).
 Pieces share_out(int64_t owners, int64_t list, int64_t sequences, int64_t heads, double f) {
   Pieces P;
   if (owners <= 0 || list <= 0 || sequences <= 0) return P;
   const int64_t tiles = std::max(owners / kAttnTileRows, sequences * heads), length = (list + sequences - 1) / sequences;
-  if (owners < sequences * heads * (kAttnTileRows / 2)) f *= kSparse;
+  const bool sparse = owners < sequences * heads * (kAttnTileRows / 2);
+  if (sparse) f *= kSparse;
   int64_t p = (int64_t)(f * std::sqrt((double)length / (double)owners));
   p = std::min({p, kFullTiles / std::max<int64_t>(1, tiles), (list + kPieceKeys - 1) / kPieceKeys, (int64_t)kMostPieces});
   if (p <= 1) return P;
   P.most = (int32_t)p;
   P.keys = (int32_t)std::max<int64_t>(kPieceKeys, length / (2 * p));   // sequences differ in length
+  if (sparse) {   // in one round, a sequence's last piece half full
+    const int64_t full = std::max<int64_t>(kRound / 4, kRound - tiles / 2), keys = (list * heads + full - 1) / full;
+    P.keys = std::max(P.keys, (int32_t)std::min<int64_t>((keys + 63) / 64 * 64, 1 << 30));
+  }
   return P;
 }
 // Partial sums that a call of up to so many owners and keys may take, whatever its sequences.
