@@ -25,11 +25,11 @@ __global__ void __launch_bounds__(256, (DT == ISO_F32 && D == 128 ? 1 : 2)) k_at
   const int pieces = pieces_of(all, A.pieces);
   if (piece >= pieces) return;
   const int tiles = (all.hi - all.lo + P::kRows - 1) / P::kRows;
-  const int first = __builtin_amdgcn_readfirstlane((int)((int64_t)tiles * piece / pieces));
-  const int last = __builtin_amdgcn_readfirstlane((int)((int64_t)tiles * (piece + 1) / pieces));
+  const int first = __builtin_amdgcn_readfirstlane((int)((uint32_t)tiles * (uint32_t)piece / (uint32_t)pieces));
+  const int last = __builtin_amdgcn_readfirstlane((int)((uint32_t)tiles * (uint32_t)(piece + 1) / (uint32_t)pieces));
 
   // a lane has one row of its wave's 32, the halves of a wave different keys
-  const int32_t r = row0 + 32 * w + (lane & 31), i = r / A.group;
+  const int32_t r = row0 + 32 * w + (lane & 31), i = (int32_t)((uint32_t)r / (uint32_t)A.group);
   const int h = head * A.group + r - i * A.group;
   const bool on = r < end, busy = row0 + 32 * w < end;
   int32_t lo = 0, hi = 0;

@@ -99,10 +99,10 @@ __device__ __forceinline__ void dq_tile(const AttnArgs& A, const Deal& deal, uin
   const int pieces = pieces_of(all, A.pieces);
   if (piece >= pieces) return;
   const int tiles = (all.hi - all.lo + P::kRows - 1) / P::kRows;
-  const int first = __builtin_amdgcn_readfirstlane((int)((int64_t)tiles * piece / pieces));
-  const int last = __builtin_amdgcn_readfirstlane((int)((int64_t)tiles * (piece + 1) / pieces));
+  const int first = __builtin_amdgcn_readfirstlane((int)((uint32_t)tiles * (uint32_t)piece / (uint32_t)pieces));
+  const int last = __builtin_amdgcn_readfirstlane((int)((uint32_t)tiles * (uint32_t)(piece + 1) / (uint32_t)pieces));
 
-  const int32_t r = row0 + 32 * w + (lane & 31), i = r / A.group;
+  const int32_t r = row0 + 32 * w + (lane & 31), i = (int32_t)((uint32_t)r / (uint32_t)A.group);
   const int h = head * A.group + r - i * A.group;
   const bool on = r < end, busy = row0 + 32 * w < end;
   int32_t lo = 0, hi = 0;
@@ -357,8 +357,8 @@ __device__ __forceinline__ void dkv_tile(const AttnArgs& A, const Deal& deal, ui
   const int pieces = pieces_of(all, A.key_pieces);
   if (piece >= pieces) return;
   const int tiles = (all.hi - all.lo + P::kRows - 1) / P::kRows;
-  const int first = __builtin_amdgcn_readfirstlane((int)((int64_t)tiles * piece / pieces));
-  const int last = __builtin_amdgcn_readfirstlane((int)((int64_t)tiles * (piece + 1) / pieces));
+  const int first = __builtin_amdgcn_readfirstlane((int)((uint32_t)tiles * (uint32_t)piece / (uint32_t)pieces));
+  const int last = __builtin_amdgcn_readfirstlane((int)((uint32_t)tiles * (uint32_t)(piece + 1) / (uint32_t)pieces));
 
   // a lane has one key of its wave's 32, the halves of a wave different rows
   const int32_t key = key0 + 32 * w + (lane & 31);

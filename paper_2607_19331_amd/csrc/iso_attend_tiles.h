@@ -323,10 +323,10 @@ struct Span {
   int32_t lo, hi, lo_all, hi_all;
 };
 // Bounds grow with the query, so those of the first and last row do for all.
-__device__ __forceinline__ Span span_of(const AttnArgs& A, const Seq& s, int64_t first, int64_t last) {
+__device__ __forceinline__ Span span_of(const AttnArgs& A, const Seq& s, int32_t first, int32_t last) {
   Span x;
-  keys_of(A, s, first / A.group, x.lo, x.hi_all);
-  keys_of(A, s, last / A.group, x.lo_all, x.hi);
+  keys_of(A, s, (uint32_t)first / (uint32_t)A.group, x.lo, x.hi_all);
+  keys_of(A, s, (uint32_t)last / (uint32_t)A.group, x.lo_all, x.hi);
   return x;
 }
 
@@ -340,7 +340,7 @@ __device__ __forceinline__ Span list_span(const AttnArgs& A, const Seq& s, int32
 
 // Pieces that the keys (or rows) [lo, hi) of a tile are shared out to.
 __device__ __forceinline__ int pieces_of(const Span& x, const Pieces& p) {
-  return min(p.most, max(1, (x.hi - x.lo + p.keys - 1) / p.keys));
+  return min(p.most, max(1, (int32_t)((uint32_t)(x.hi - x.lo + p.keys - 1) / (uint32_t)p.keys)));
 }
 
 // A row (of tokens_q x heads) whose pieces half a wave adds up.
