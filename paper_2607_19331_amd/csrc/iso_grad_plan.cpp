@@ -223,7 +223,7 @@ bool attend_fits(const iso_attn& a) {
 namespace {
 
 constexpr int kPieceKeys = 256;         // fewest keys of a piece
-constexpr int kMostPieces = 64;         // of a tile
+constexpr int kMostTilePieces = 64;         // of a tile
 constexpr double kSparse = 2.0;
 constexpr int64_t kRound = 512;         // workgroups at once
 constexpr int64_t kFullTiles = 1536;    // three rounds of workgroups, two a CU: heavy tiles first, these balance by themselves
@@ -242,7 +242,7 @@ Pieces share_out(int64_t owners, int64_t list, int64_t sequences, int64_t heads,
   const bool sparse = owners < sequences * heads * (kAttnTileRows / 2);
   if (sparse) f *= kSparse;
   int64_t p = (int64_t)(f * std::sqrt((double)length / (double)owners));
-  p = std::min({p, kFullTiles / std::max<int64_t>(1, tiles), (list + kPieceKeys - 1) / kPieceKeys, (int64_t)kMostPieces});
+  p = std::min({p, kFullTiles / std::max<int64_t>(1, tiles), (list + kPieceKeys - 1) / kPieceKeys, (int64_t)kMostTilePieces});
   if (p <= 1) return P;
   P.most = (int32_t)p;
   P.keys = (int32_t)std::max<int64_t>(kPieceKeys, length / (2 * p));   // sequences differ in length
@@ -252,11 +252,12 @@ Pieces share_out(int64_t owners, int64_t list, int64_t sequences, int64_t heads,
   }
   return P;
 }
-// Partial sums that a call of up to so many owners and keys may take, whatever its sequences.
+// Partial sums that a call of up to so many owners and keys may take, whatever its sequences.  t whole tiles are up to
+// (t + 1) kAttnTileRows owners with at most kFullTiles / t pieces, and kMostTilePieces.
 size_t most_parts(int64_t owners, int64_t list, double f) {
   if (owners <= 0 || list <= 0) return 0;
-  const double each = (double)std::min<int64_t>(kMostPieces, (list + kPieceKeys - 1) / kPieceKeys);
-  return (size_t)std::min({kSparse * f * std::sqrt((double)list * (double)owners), (double)owners * each, (double)(kFullTiles + 1) * kAttnTileRows});
+  const double each = (double)std::min<int64_t>(kMostTilePieces, (list + kPieceKeys - 1) / kPieceKeys);
+  return (size_t)std::min({kSparse * f * std::sqrt((double)list * (double)owners), (double)owners * each, (double)(kFullTiles + kMostTilePieces) * kAttnTileRows});
 }
 
 }  // namespace
