@@ -5,6 +5,8 @@
 #include <math.h>
 #include <stdint.h>
 
+#include <algorithm>
+
 #include "iso.h"
 #include "iso_device.h"
 #include "iso_grad_device.h"
@@ -45,7 +47,7 @@ inline AttnArgs args_of(const iso_attn& a, uint8_t* ws) {
   A.q = a.q, A.k = a.k, A.v = a.v, A.ld_q = a.ld_q, A.ld_k = a.ld_k, A.ld_v = a.ld_v;
   A.start_q = a.start_q, A.start_k = a.start_k, A.tokens_q = a.tokens_q, A.tokens_k = a.tokens_k;
   A.sequences = (int32_t)a.sequences, A.heads = a.heads, A.heads_kv = a.heads_kv, A.group = a.heads / a.heads_kv, A.dim = a.dim;
-  A.causal = a.causal, A.window = a.window;
+  A.causal = a.causal, A.window = std::min(a.window, (int64_t)1 << 30);   // past every distance, and sums with it hold
   A.scale = (float)a.scale, A.scale2 = (float)(a.scale * 1.4426950408889634);
   A.out = a.out, A.ld_out = a.ld_out, A.lse = a.lse, A.dout = a.dout, A.ld_dout = a.ld_dout;
   A.dq = a.dq, A.dk = a.dk, A.dv = a.dv, A.ld_dq = a.ld_dq, A.ld_dk = a.ld_dk, A.ld_dv = a.ld_dv;

@@ -153,7 +153,7 @@ iso_status check_distill_sizes(const iso_distill* d) {
 iso_status check_distill(const iso_distill* d, int dt, bool loss, bool grad) {
   iso_status st = check_distill_sizes(d);
   if (st != ISO_OK) return st;
-  const float t = (float)d->temperature, inv = (float)(1.0 / d->temperature);
+  const float t = (float)d->temperature, inv = (float)(1.4426950408889634 / d->temperature);   // log2(e) / T, the kernels' factor
   if (!is_dtype(dt) || !std::isfinite(t) || !(t > 0.0f) || !std::isfinite(inv) || !(inv > 0.0f)) return ISO_ERR_INVALID_ARG;
   if (d->tokens == 0) return ISO_OK;
   if (d->ids == nullptr || d->ld < d->vocab) return ISO_ERR_INVALID_ARG;

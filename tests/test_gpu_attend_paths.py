@@ -50,6 +50,39 @@ def test_long_walks_shared_out(dtype, q, k, window, causal):
     run(Case(dtype, q, k, 2, 1, 64, causal, window))
 
 
+@pytest.mark.parametrize("causal", [False, True])
+@pytest.mark.parametrize("window", [70, 1 << 30, (1 << 31) + 5, 1 << 62, (1 << 63) - 1])
+def test_windows_wider_than_a_sequence(window, causal):
+    say(f"attend window {window} {causal}")
+    run(Case("f32", [33, 9], [70, 3], 2, 1, 16, causal, window))
+
+
+def test_partial_sums_stay_in_the_workspace():
+    """3199 rows over 400000 keys: 25 tiles of 64 pieces, the most that a workspace has to hold."""
+    import torch
+    say("attend workspace's end")
+    tokens, keys, heads, dim = 457, 400000, 7, 8
+    g = torch.Generator("cuda").manual_seed(3)
+    new = lambda *shape: torch.randn(*shape, device="cuda", generator=g)  # noqa: E731
+    dev = lambda n: torch.tensor([0, n], dtype=torch.int32, device="cuda")  # noqa: E731
+    q, k, v, dout = new(tokens, heads * dim), new(keys, dim), new(keys, dim), new(tokens, heads * dim)
+    a = iso.Attn(q=q, k=k, v=v, ld_q=heads * dim, ld_k=dim, ld_v=dim, start_q=dev(tokens), start_k=dev(keys), sequences=1,
+                 tokens_q=tokens, tokens_k=keys, heads=heads, heads_kv=1, dim=dim, scale=0.3, causal=False, window=0,
+                 out=torch.empty_like(q), ld_out=heads * dim, lse=torch.empty(tokens, heads, device="cuda"), dout=dout, ld_dout=heads * dim,
+                 dq=torch.empty_like(q), dk=torch.empty_like(k), dv=torch.empty_like(v), ld_dq=heads * dim, ld_dk=dim, ld_dv=dim)
+    for grad, call in ((False, iso.iso_attend), (True, iso.iso_attend_grad)):
+        size = iso.attend_workspace(a, iso.F32, grad).numel()
+        ws = torch.full((size + (1 << 23),), 0x5A, dtype=torch.uint8, device="cuda")
+        call(a, iso.F32, ws=ws[:size])
+        assert iso.iso_read_device_status(ws) == 0
+        assert bool((ws[size:] == 0x5A).all())
+    # The first query's row.  A lane adds up 3200 terms at most in binary32, with pieces and halves: 3300 2^-24 of a sum of weights
+    # times |v| (below 1); scores are off by 16 2^-24 times 20: together below 3e-4.
+    x = (k.double() @ q[0, :dim].double()) * 0.3
+    want = torch.softmax(x, 0) @ v.double()
+    assert torch.allclose(a.out[0, :dim].double(), want, rtol=0, atol=3e-4)
+
+
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 def test_non_finite_values_in_pieces(dtype):
     say(f"attend pieces non-finite {dtype}")

@@ -108,7 +108,8 @@ def gradient(d, dt=iso.BF16, ws=WS, ws_bytes=1 << 30):
 def test_distill_refusals(call):
     for kw in (dict(tokens=-1), dict(vocab=0), dict(top=0), dict(id_type=2), dict(ids=None), dict(logits=None), dict(teacher=None),
                dict(lse=None), dict(ld=99), dict(ld_grad=99), dict(temperature=0.0), dict(temperature=-1.0),
-               dict(temperature=float("nan")), dict(temperature=float("inf")), dict(temperature=1e-300), dict(temperature=1e300),
+               dict(temperature=float("nan")), dict(temperature=float("inf")), dict(temperature=1e-300), dict(temperature=4e-39),
+               dict(temperature=1e300),
                dict(grad=FAKE, ld_grad=104)):
         assert call(distill(**kw)) == _lib.ERR_INVALID_ARG, kw
     assert call(distill(), dt=3) == _lib.ERR_INVALID_ARG
