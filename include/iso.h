@@ -678,7 +678,8 @@ iso_status iso_attend(const iso_attn* a, int dt, void* ws, size_t ws_bytes, void
  * S_ij = P_ij (dout_i.v_j - D_i),
  *   dv_j = sum_i P_ij dout_i,   dk_j = scale sum_i S_ij q_i,   dq_i = scale sum_j S_ij k_j,
  * the first two over the heads of a group too.  All three are written.  With bf16, P and S are rounded to bf16 in
- * the products.
+ * the products; dq also has the sum of what S lost times the mean of up to 16 keys that the query sees, which takes out
+ * most of that error where keys have a common part (a projection's bias).
  */
 iso_status iso_attend_grad(const iso_attn* a, int dt, void* ws, size_t ws_bytes, void* stream);
 

@@ -191,11 +191,6 @@ __device__ __forceinline__ void multiply_columns(const Reader<DT, D>& r, uint32_
   }
 }
 
-template <int N>
-struct Const {
-  static constexpr int value = N;
-};
-
 // All loads into LDS have landed and all LDS reads are done, of every wave.
 __device__ __forceinline__ void landed() { asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
 

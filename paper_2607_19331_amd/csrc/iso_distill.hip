@@ -1,8 +1,8 @@
 // Distillation from a teacher's top entries: with t = softmax(y / T) over a token's list and L = logsumexp(z / T) over the
 // vocabulary, loss = w T^2 sum t (log t - z_id / T + L) and grad_v = w T (exp(z_v / T - L) - sum of t at id v).
 //
-// Bound by memory: 2 (or 4) bytes of a logit read, as many written for a gradient, against one exponential each.  The list
-// (up to 256 entries, one a thread) is a few microseconds of latency a row, hidden under other rows.
+// Bound by memory: 2 (or 4) bytes of a logit read, as many written for a gradient, against one exponential each (two for both in
+// one call).  The list (up to 256 entries, one a thread) is a few microseconds of latency a row, hidden under other rows.
 #include <hip/hip_runtime.h>
 #include <math.h>
 #include <stdint.h>
@@ -275,8 +275,9 @@ __device__ __forceinline__ void before_writes(float z) {
   __syncthreads();
 }
 
-// Loss (and gradient) of a row, one workgroup: two walks over the row where both are asked for.
-template <int DT, bool STREAM>
+// Loss of a row, one workgroup: the row's maximum and sum, then its list.  Bound by memory where there are many (4096 x 152064 bf16:
+// 217 us, 5.7 TB/s), else by its own walk, four loads a lane under way.
+template <int DT>
 __global__ void __launch_bounds__(256) k_distill_row(DistillArgs A) {
   __shared__ ListSpace S;
   __shared__ double sums[4];
@@ -285,23 +286,9 @@ __global__ void __launch_bounds__(256) k_distill_row(DistillArgs A) {
   const Lse l = row_lse<DT>(A, row, 0, A.vocab, S.red);
   __syncthreads();
   bool any;
-  Entry r = list_of<256>(A, row, S, any);
+  const Entry r = list_of<256>(A, row, S, any);
   const float z = r.id >= 0 ? load_z<DT>(A, row * A.ld + r.id) : 0.0f;
-  const double lse = lse_of(A, l);
-  store_loss<DT>(A, row, r, z, lse, any, sums);
-  if (A.grad == nullptr) return;
-  constexpr int V = kVec<DT>, U = 4;
-  merge(A, S, r);
-  const Factor F(A, row, any);
-  const float lse2 = (float)(lse * 1.4426950408889634);
-  before_writes(z);
-  for (int64_t c = (int64_t)threadIdx.x * V; c < A.vocab; c += U * 256 * V) {
-    u32x4_t w[U];
-#pragma unroll
-    for (int u = 0; u < U; ++u) w[u] = load_end<DT>(A.z, row * A.ld + c + u * 256 * V, A.vocab - (c + u * 256 * V));
-    put_grads<DT, U, STREAM>(A, row, c, F, w, lse2);
-  }
-  put_entry<DT>(A, row, 0, A.vocab, F, r, z, lse2);
+  store_loss<DT>(A, row, r, z, lse_of(A, l), any, sums);
 }
 
 // A list before it is looked at: thread e has entry e.
@@ -324,7 +311,8 @@ struct HeldSpace {
   int32_t head[N];   // the first of the entries that lie in a lane's columns; -1: none
 };
 
-// Loss and gradient of a row that a workgroup of N holds in registers, PER pieces of 16 bytes a lane: read once, written once.
+// Loss and gradient of a row that a workgroup of N holds in registers, PER pieces of 16 bytes a lane: read once, written once
+// (4096 x 152064 bf16: 513 us, 4.9 TB/s, the rate of a plain copy).
 // All of a row is under way at once; what a CU does between its loads and its stores, other CUs' loads and stores fill.  Entries
 // change the pieces they lie in before these are stored (a lane has a list of its own): written after them they would have to
 // wait for the stores.  Workgroups that walk over rows and load a piece of the next row where one of this is stored were tried:
@@ -435,7 +423,7 @@ __global__ void __launch_bounds__(N) k_distill_held(DistillArgs A) {
   }
 }
 
-// A piece of a row: its share of the sum, and from these the loss.
+// A piece of a row: its share of the sum, and from these the loss.  Both are latency: 3.4 and 3.5 us for one token of 151936.
 template <int DT>
 __global__ void __launch_bounds__(256) k_distill_part(DistillArgs A, int64_t each) {
   __shared__ ListSpace S;
@@ -464,7 +452,7 @@ __global__ void __launch_bounds__(256) k_distill_join(DistillArgs A) {
 }
 
 // The gradient of a piece of a row from the row's L: kGradPiece columns a workgroup, four loads a lane, which are under way
-// while the list is looked at.
+// while the list is looked at (4096 x 152064 bf16: 473 us, 5.3 TB/s).
 template <int DT>
 constexpr int kGradPiece = 4 * 256 * kVec<DT>;
 
@@ -515,22 +503,32 @@ void gradient(const DistillArgs& A, bool check, hipStream_t s) {
   k_distill_grad<DT, STREAM><<<(unsigned)(A.tokens * pieces), 256, 0, s>>>(A, pieces, check);
 }
 
+// Rows with a gradient that fit into a workgroup's registers are read once (k_distill_held), others' loss is formed before their
+// gradient: both in one kernel, with two walks over a row, took 7 to 17% longer (2048 x 152064 fp32: 737 us for 665).  Few long rows
+// are shared out, loss and join and gradient in a launch each; microseconds for rows of 304 KB, shared out and whole, with the
+// gradient 1 token 17, 25; 64 27, 28; 128 39, 29; the loss alone 1 token 13.1, 13.7; 64 13.3, 16.5; 128 20, 27; 256 21.7, 21.7, and for
+// rows of 608 KB 26, 33 of 128 and 32, 28 of 256; rows of 128 KB 18, 19 with the gradient and 13, 11 without.
 template <int DT, bool STREAM>
 void loss(DistillArgs A, hipStream_t s) {
   constexpr int V = kVec<DT>;
-  const int64_t each = share_out(A, DT);
-  if (A.pieces > 4 || (A.pieces > 1 && A.grad == nullptr)) {
-    k_distill_part<DT><<<(unsigned)(A.tokens * A.pieces), 256, 0, s>>>(A, each);
-    k_distill_join<DT><<<(unsigned)A.tokens, 256, 0, s>>>(A);
-    if (A.grad != nullptr) gradient<DT, STREAM>(A, false, s);
+  const unsigned n = (unsigned)A.tokens;
+  const bool held = A.grad != nullptr && A.vocab <= 1024 * 20 * V;
+  const bool shared = A.vocab > (256 << 10) * V / 16 && A.tokens <= (held ? 64 : 128);
+  if (held && !shared) {
+    if (A.vocab <= 256 * 4 * V) k_distill_held<DT, 256, 4, STREAM><<<n, 256, 0, s>>>(A);
+    else if (A.vocab <= 256 * 20 * V) k_distill_held<DT, 256, 20, STREAM><<<n, 256, 0, s>>>(A);
+    else if (A.vocab <= 512 * 20 * V) k_distill_held<DT, 512, 20, STREAM><<<n, 512, 0, s>>>(A);
+    else k_distill_held<DT, 1024, 20, STREAM><<<n, 1024, 0, s>>>(A);
     return;
   }
-  const unsigned n = (unsigned)A.tokens;
-  if (A.grad == nullptr || A.vocab > 1024 * 20 * V) k_distill_row<DT, STREAM><<<n, 256, 0, s>>>(A);
-  else if (A.vocab <= 256 * 4 * V) k_distill_held<DT, 256, 4, STREAM><<<n, 256, 0, s>>>(A);
-  else if (A.vocab <= 256 * 20 * V) k_distill_held<DT, 256, 20, STREAM><<<n, 256, 0, s>>>(A);
-  else if (A.vocab <= 512 * 20 * V) k_distill_held<DT, 512, 20, STREAM><<<n, 512, 0, s>>>(A);
-  else k_distill_held<DT, 1024, 20, STREAM><<<n, 1024, 0, s>>>(A);
+  if (shared) {
+    const int64_t each = share_out(A, DT);
+    k_distill_part<DT><<<n * A.pieces, 256, 0, s>>>(A, each);
+    k_distill_join<DT><<<n, 256, 0, s>>>(A);
+  } else {
+    k_distill_row<DT><<<n, 256, 0, s>>>(A);
+  }
+  if (A.grad != nullptr) gradient<DT, STREAM>(A, false, s);
 }
 
 bool streams(const DistillArgs& A, int dt) { return A.grad != nullptr && streamed(A.tokens * A.vocab * (dt == ISO_BF16 ? 2 : 4)); }

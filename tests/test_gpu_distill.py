@@ -118,6 +118,21 @@ def test_distill(dtype, shape):
         case.check(what)
 
 
+@pytest.mark.parametrize("dtype,n,vocab", [("f32", 130, 82001), ("bf16", 129, 163841), ("bf16", 66, 131073), ("bf16", 5, 100003),
+                                           ("f32", 66, 66001), ("f32", 129, 65600)])
+@pytest.mark.parametrize("in_place", [False, True])
+def test_long_rows(dtype, n, vocab, in_place):
+    """Rows that fit into a workgroup's registers and rows that do not, shared out and whole."""
+    say(f"distill long rows {dtype} {n} {vocab} {in_place}")
+    c = Case(dtype, n, vocab, 12, 2.0, pad=-1, in_place=in_place)
+    c.call("loss")
+    assert c.status() == 0
+    c.check("loss")
+    c.call("both")
+    assert c.status() == 0
+    c.check("both")
+
+
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("n,vocab", [(2, 700), (4, 70001), (1, 152064), (600, 515)])
 @pytest.mark.parametrize("how", ["both", "grad"])
