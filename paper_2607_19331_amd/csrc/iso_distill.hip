@@ -195,10 +195,10 @@ __device__ __forceinline__ u32x4_t load_end(const void* p, int64_t i, int64_t le
   return w;
 }
 
-// Maximum and sum over columns [lo, hi) of a row, a workgroup of 256.
-template <int DT>
+// Maximum and sum over columns [lo, hi) of a row, a workgroup of N.
+template <int DT, int N>
 __device__ __forceinline__ Lse row_lse(const DistillArgs& A, int64_t row, int64_t lo, int64_t hi, float (*lds)[2]) {
-  constexpr int V = kVec<DT>, U = 4, kStride = 256 * V;
+  constexpr int V = kVec<DT>, U = 4, kStride = N * V;
   const int64_t base = row * A.ld;
   Lse l;
   int64_t c = lo + (int64_t)threadIdx.x * V;
@@ -216,7 +216,7 @@ __device__ __forceinline__ Lse row_lse(const DistillArgs& A, int64_t row, int64_
     unpack_raw<DT>(load_end<DT>(A.z, base + c, hi - c), v);
     add_to<V>(l, v, A.exp2_t);
   }
-  return block_lse<256>(l, A.exp2_t, lds);
+  return block_lse<N>(l, A.exp2_t, lds);
 }
 
 // L of a row, in binary64: the loss takes differences of it.
@@ -277,13 +277,13 @@ __device__ __forceinline__ void before_writes(float z) {
 
 // Loss of a row, one workgroup: the row's maximum and sum, then its list.  Bound by memory where there are many (4096 x 152064 bf16:
 // 217 us, 5.7 TB/s), else by its own walk, four loads a lane under way.
-template <int DT>
-__global__ void __launch_bounds__(256) k_distill_row(DistillArgs A) {
+template <int DT, int N>
+__global__ void __launch_bounds__(N) k_distill_row(DistillArgs A) {
   __shared__ ListSpace S;
   __shared__ double sums[4];
   const int64_t row = blockIdx.x;
   if (row == 0 && A.tokens * A.top <= kFewEntries) check_ids(A);
-  const Lse l = row_lse<DT>(A, row, 0, A.vocab, S.red);
+  const Lse l = row_lse<DT, N>(A, row, 0, A.vocab, S.red);
   __syncthreads();
   bool any;
   const Entry r = list_of<256>(A, row, S, any);
@@ -429,7 +429,7 @@ __global__ void __launch_bounds__(256) k_distill_part(DistillArgs A, int64_t eac
   __shared__ ListSpace S;
   if (blockIdx.x == 0 && A.tokens * A.top <= kFewEntries) check_ids(A);
   const int64_t row = blockIdx.x / A.pieces, lo = (blockIdx.x - row * A.pieces) * each;
-  const Lse l = row_lse<DT>(A, row, lo, min(lo + each, A.vocab), S.red);
+  const Lse l = row_lse<DT, 256>(A, row, lo, min(lo + each, A.vocab), S.red);
   if (threadIdx.x == 0) gmem(A.part)[2 * blockIdx.x] = l.m, gmem(A.part)[2 * blockIdx.x + 1] = l.s;
 }
 
@@ -506,14 +506,15 @@ void gradient(const DistillArgs& A, bool check, hipStream_t s) {
 // Rows with a gradient that fit into a workgroup's registers are read once (k_distill_held), others' loss is formed before their
 // gradient: both in one kernel, with two walks over a row, took 7 to 17% longer (2048 x 152064 fp32: 737 us for 665).  Few long rows
 // are shared out, loss and join and gradient in a launch each; microseconds for rows of 304 KB, shared out and whole, with the
-// gradient 1 token 17, 25; 64 27, 28; 128 39, 29; the loss alone 1 token 13.1, 13.7; 64 13.3, 16.5; 128 20, 27; 256 21.7, 21.7, and for
-// rows of 608 KB 26, 33 of 128 and 32, 28 of 256; rows of 128 KB 18, 19 with the gradient and 13, 11 without.
+// gradient 1 token 17, 25; 64 27, 28; 128 39, 29; the loss alone 1 token 13.1, 13.7; 64 13.4, 14.6; 128 20.6, 17.2; rows of 128 KB 18, 19
+// with the gradient and 13, 11 without.  Where there is no more than a row a CU, 1024 threads have it (608 KB, 128 rows: 20 us, with 256
+// threads 33; 512 rows: 59 and 52).
 template <int DT, bool STREAM>
 void loss(DistillArgs A, hipStream_t s) {
   constexpr int V = kVec<DT>;
   const unsigned n = (unsigned)A.tokens;
   const bool held = A.grad != nullptr && A.vocab <= 1024 * 20 * V;
-  const bool shared = A.vocab > (256 << 10) * V / 16 && A.tokens <= (held ? 64 : 128);
+  const bool shared = A.vocab > (256 << 10) * V / 16 && A.tokens <= 64;
   if (held && !shared) {
     if (A.vocab <= 256 * 4 * V) k_distill_held<DT, 256, 4, STREAM><<<n, 256, 0, s>>>(A);
     else if (A.vocab <= 256 * 20 * V) k_distill_held<DT, 256, 20, STREAM><<<n, 256, 0, s>>>(A);
@@ -525,8 +526,10 @@ void loss(DistillArgs A, hipStream_t s) {
     const int64_t each = share_out(A, DT);
     k_distill_part<DT><<<n * A.pieces, 256, 0, s>>>(A, each);
     k_distill_join<DT><<<n, 256, 0, s>>>(A);
+  } else if (n <= 256) {
+    k_distill_row<DT, 1024><<<n, 1024, 0, s>>>(A);
   } else {
-    k_distill_row<DT><<<n, 256, 0, s>>>(A);
+    k_distill_row<DT, 256><<<n, 256, 0, s>>>(A);
   }
   if (A.grad != nullptr) gradient<DT, STREAM>(A, false, s);
 }
