@@ -25,7 +25,7 @@ template <int DT>
 __global__ void __launch_bounds__(256) k_attend_stat(AttnArgs A) {
   if (blockIdx.x == gridDim.x - 1) return check_starts(A);
   const int64_t at = (int64_t)blockIdx.x * 16 + (threadIdx.x >> 4), t = at / A.heads;
-  if (t >= A.tokens_q) return;
+  if (t >= A.tokens_q || A.sequences == 0) return;   // without sequences, pointers may be null
   const int h = (int)(at - t * A.heads), head = h / A.group, c = (threadIdx.x & 15) * 8;
   float o[8] = {}, g[8] = {}, sum = 0.0f;
   if (c < A.dim) {   // under way while the sequence is looked up

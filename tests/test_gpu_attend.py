@@ -142,6 +142,18 @@ def test_no_sequences_and_no_rows(dtype):
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("tokens", [1, 300])
+def test_rows_without_sequences_need_no_pointers(dtype, tokens):
+    say(f"attend no sequences {dtype} {tokens}")
+    a = iso.Attn(q=None, k=None, v=None, start_q=None, start_k=None, sequences=0, tokens_q=tokens, tokens_k=tokens, heads=4, heads_kv=2,
+                 dim=64, scale=1.0, out=None, lse=None)
+    for grad, call in ((False, iso.iso_attend), (True, iso.iso_attend_grad)):
+        ws = iso.attend_workspace(a, code(dtype), grad=grad)
+        call(a, code(dtype), ws=ws)
+        assert iso.iso_read_device_status(ws) == 0
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
 def test_captured_and_on_another_stream(dtype):
     """Forward and backward captured into one graph, replayed after new inputs and between eager calls on another stream."""
     import torch
