@@ -287,7 +287,8 @@ __global__ void __launch_bounds__(256) k_attend_join(AttnArgs A) {
 
 template <int DT, int D>
 hipError_t forward(const AttnArgs& A, hipStream_t s) {
-  const Deal deal = deal_of(A.heads_kv, attend_items(A.tokens_q * A.group, A.tokens_k, A.sequences, A.pieces));
+  Deal deal = deal_of(A.heads_kv, attend_items(A.tokens_q * A.group, A.tokens_k, A.sequences, A.pieces));
+  if (A.pieces.most == 1 && !(DT == ISO_F32 && D == 128)) deal = folded(deal, A.heads_kv, A.tokens_q * A.heads / kAttnTileRows);   // two a CU
   k_attend<DT, D><<<deal_grid(deal, A.heads_kv) + 1, 256, 4 * Panel<DT, D>::kBytes, s>>>(A, deal);   // one looks at the offsets
   const unsigned rows = (unsigned)((A.tokens_q * A.heads + 7) / 8);
   if (A.pieces.most > 4) k_attend_join<DT, 8><<<rows, 256, 0, s>>>(A);

@@ -6,6 +6,8 @@
 // both operands agree, so the other operand is read from LDS in the order that the result has.
 #pragma once
 
+#include <algorithm>
+
 #include "iso_attend.h"
 #include "iso_mfma.h"
 
@@ -212,22 +214,37 @@ __device__ __forceinline__ float sum_of_halves(float v) {
 struct Deal {
   int32_t classes, per;   // classes of XCDs, XCDs of a class
   uint32_t items;         // of a head, or an upper bound
+  uint32_t fold, end;     // places [fold, end) of a class are taken from the end, and heads in turn; 0: neither
 };
 
 inline Deal deal_of(int heads, uint32_t items) {
   int c = 8;
   while (heads % c != 0) c /= 2;
-  return Deal{c, 8 / c, items};
+  return Deal{c, 8 / c, items, 0, 0};
+}
+// Items of falling length that all start at once, two a CU: the second half from its end on, so that the shortest go with the longest.
+// `tiles`: about how many there are.  Four sequences of 2048, causal, 8 heads of 64, fp32: 161 us for 206; 2048 tokens, 32 heads of
+// 128, bf16: 53 for 63.
+inline Deal folded(Deal d, int heads, int64_t tiles) {
+  const uint32_t cus = 32 * d.per, all = (uint32_t)(heads / d.classes) * d.items;   // CUs of a class
+  if (all > cus && tiles <= 2 * (int64_t)cus * d.classes) d.fold = cus, d.end = std::min(all, 2 * cus);
+  return d;
 }
 inline uint32_t deal_grid(const Deal& d, int heads) {
   const uint64_t n = (uint64_t)(heads / d.classes) * d.items;
   return (uint32_t)((n + d.per - 1) / d.per * 8);
 }
 __device__ __forceinline__ bool dealt(const Deal& d, int heads, uint32_t b, int& head, uint32_t& item) {
-  const uint32_t x = b & 7u, c = x % d.classes, j = (b >> 3) * d.per + x / d.classes, h = j / d.items;
-  if (h >= (uint32_t)(heads / d.classes)) return false;
+  const uint32_t x = b & 7u, c = x % d.classes, each = (uint32_t)(heads / d.classes);
+  uint32_t j = (b >> 3) * d.per + x / d.classes, h;
+  if (j >= each * d.items) return false;
+  if (d.fold > 0) {
+    if (j >= d.fold && j < d.end) j = d.fold + d.end - 1 - j;
+    item = j / each, h = j - item * each;
+  } else {
+    h = j / d.items, item = j - h * d.items;
+  }
   head = (int)(c + d.classes * h);
-  item = j - h * d.items;
   return true;
 }
 
