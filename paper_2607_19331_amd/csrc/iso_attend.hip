@@ -15,11 +15,11 @@ namespace {
 // operand of the product with V where it is.  Q and O stay in registers.
 //
 // What bounds it: D = 128 the matrix instructions, 56% of the cycles at the 1.75 GHz that the card holds under them: four sequences
-// of 4096 tokens, 28 heads over 4, causal, 500 us, 960 TFLOP/s (16 heads of all keys 1040; a large product of the library 1200).
-// D = 64 the exponentials and what goes with them, twice the matrix instructions' cycles (32 heads over 8: 336 us, 820 TFLOP/s).
-// fp32 the matrix rate of its type (a sixteenth of bf16's): 12 heads over 2, four sequences of 1024, 209 us, 62 TFLOP/s with one
-// wave a SIMD, 70% of the cycles.  Few rows: keys are shared out to pieces, see share_out; one token over 77 to 8192 keys for 16
-// sequences, 28 heads, 30 us with the join, 3.5 TB/s, of which 5 are a workgroup's start and 7 the join's launch.
+// of 4096 tokens, 28 heads over 4, causal, 500 us, 960 TFLOP/s (16 heads, all keys seen, 1030; a large product of the library 1200).
+// D = 64 the exponentials and what goes with them, twice the matrix instructions' cycles (32 heads over 8: 330 us, 830 TFLOP/s).
+// fp32 the matrix rate of its type (154 TFLOP/s, a sixteenth of bf16's): 8 heads of 128, one sequence of 8192, all keys seen, 122
+// TFLOP/s with one wave a SIMD; causal, four of 2048, 314 us, 110.  Few rows: keys are shared out to pieces, see share_out; one token over 77 to 8192 keys for 16
+// sequences, 28 heads, 30 us with the join, 3.5 TB/s, of which 5 are a workgroup's start and 6 the join's launch.
 template <int DT, int D>
 __global__ void __launch_bounds__(256, (DT == ISO_F32 && D == 128 ? 1 : 2)) k_attend(AttnArgs A, Deal deal) {
   using P = Panel<DT, D>;
@@ -234,7 +234,7 @@ __global__ void __launch_bounds__(256, (DT == ISO_F32 && D == 128 ? 1 : 2)) k_at
 }
 
 // O = sum of 2^(m_p - m) O_p / sum of 2^(m_p - m) l_p over a row's pieces p, m the largest m_p; half a wave a row, four dimensions a
-// lane.  Its time is latency (the row's sequence, then the pieces, U at once): 6.8 us for 16 tokens of 28 heads in 16 pieces.
+// lane.  Its time is latency (the row's sequence, then the pieces, U at once): 6 us for 16 tokens of 28 heads in up to 13 pieces.
 template <int DT, int U>
 __global__ void __launch_bounds__(256) k_attend_join(AttnArgs A) {
   constexpr int kRows = 32 * kAttnWaves;

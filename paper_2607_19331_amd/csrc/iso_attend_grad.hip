@@ -6,9 +6,9 @@
 // result has one owner who adds in a fixed order: no atomics, the same bits every time.
 //
 // Both are bound by the matrix instructions (bf16, D = 128: busy 61 and 62% of the cycles, at the 1.5 to 1.6 GHz that the card holds
-// under them): two sequences of 8192 tokens, 28 heads over 4, causal, 3.16 ms, 762 TFLOP/s of five products, 1070 of seven, where
-// a large product of the library reaches 1200.  D = 64 (32 heads over 8, 4 x 4096): 1.15 ms, 598.  fp32 (12 over 2, 4 x 1024): 606
-// us, 53, of its matrix rate's 154.
+// under them): two sequences of 8192 tokens, 28 heads over 4, causal, 3.13 ms, 769 TFLOP/s of five products, 1076 of seven, where
+// a large product of the library reaches 1200.  D = 64 (32 heads over 8, 4 x 4096): 1.11 ms, 620.  fp32 (8 heads of 128, 4 x 2048): 1.10
+// ms, 79, 110 of seven, of its matrix rate's 154.
 #include <algorithm>
 
 #include "iso_attend_tiles.h"

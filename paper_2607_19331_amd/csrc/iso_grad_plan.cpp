@@ -230,9 +230,9 @@ constexpr int64_t kFullTiles = 1536;    // three rounds of workgroups, two a CU:
 
 // Tiles of `owners` rows walk over `length` keys on average.  In p pieces a tile's time falls by p, and every row writes and
 // reads p partial sums: the sum of both is least at p = f sqrt(length / owners).  f was measured, 6.5 for rows and 9.1 for keys
-// (which have dK and dV).  Microseconds with f at 12.8, 9, 6.5 and 5: 2048 tokens, 12 heads, forward 43, 44, 42, 42; 512 tokens
-// 18.9, 18.9, 16.9, 17.0; 64 new tokens after 4032 for four sequences, 28 heads, 45, 38, 36, 40; backward with keys' f at 9.1, 6, 4
-// and 2.5: 2048 tokens, 12 heads, 91, 85, 106, 135; 16 samples of 1 to 2048 tokens 313, 347, 460, 458.  Tiles that are mostly
+// (which have dK and dV).  Microseconds with f at 11, 9, 6.5 and 5.5, forward: 2048 tokens, 12 heads, 40, 43, 42, 42; 4096 tokens
+// 92, 94, 83, 82; 512 tokens 19, 18.6, 17.1, 17.1; 64 new tokens after 4032 for four sequences, 28 heads, 37.5, 38.2, 36.4, 36.9; with f at
+// 4.5 39.8.  Backward with keys' f at 9.1 and 6: 2048 tokens, 12 heads, 94 and 90; 16 samples of 1 to 2048 tokens 294 and 308.  Tiles that are mostly
 // empty (one new token a sequence) write little and are bound by what a workgroup waits for at its start and each panel: twice as
 // many pieces, but all of them at once (16 tokens over 77 to 8192 keys, 28 heads: pieces of 256 keys 37.5 us, 512 30.0, 640 30.1).
 Pieces share_out(int64_t owners, int64_t list, int64_t sequences, int64_t heads, double f) {
