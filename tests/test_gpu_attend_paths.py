@@ -84,6 +84,16 @@ def test_partial_sums_stay_in_the_workspace():
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("lens,heads,kv,causal", [([3000, 700, 0, 130], 4, 1, True),          # 94 tiles a sequence and more than 64 places
+                                                  ([2600, 1300, 1000], 8, 8, True),           # 40 tiles a head for 32 CUs: all start at once
+                                                  ([700, 1300, 500], 16, 16, False),          # two heads of 21 tiles each
+                                                  ([1, 900, 2, 900, 3] * 12, 8, 4, True)])    # 60 sequences
+def test_order_of_tiles(dtype, lens, heads, kv, causal):
+    say(f"attend order {dtype} {lens} {heads}/{kv}")
+    run(Case(dtype, lens, lens, heads, kv, 16, causal))
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
 def test_non_finite_values_in_pieces(dtype):
     say(f"attend pieces non-finite {dtype}")
 
