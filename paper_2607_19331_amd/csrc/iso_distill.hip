@@ -3,6 +3,7 @@
 //
 // Bound by memory: 2 (or 4) bytes of a logit read, as many written for a gradient, against one exponential each (two for both in
 // one call).  The list (up to 256 entries, one a thread) is a few microseconds of latency a row, hidden under other rows.
+#include <float.h>
 #include <hip/hip_runtime.h>
 #include <math.h>
 #include <stdint.h>
@@ -18,7 +19,7 @@ namespace iso {
 
 namespace {
 
-constexpr float kLog2e = 1.44269504088896341f;
+constexpr float kLn2 = 0.693147180559945309f;
 
 struct DistillArgs {
   const void* z;
@@ -28,55 +29,67 @@ struct DistillArgs {
   void* grad;
   int64_t tokens, vocab, ld, ld_grad, pad_id;
   int32_t top, id_type, pieces;   // pieces: workgroups a row
-  float inv_t, exp2_t;            // 1 / T and log2(e) / T
-  double t;
-  float* part;                    // maximum and sum of a piece (scaled by 1 / T), tokens x pieces
+  float c;                        // log2(e) / T
+  double t, tc, inv_tc;           // T, T c and its reciprocal
+  float* part;                    // reference and sum of a piece, tokens x pieces
   uint32_t* status;
 };
 
-// Maximum m of some logits, and the sum of exp((z - m) / T) = 2^((z - m) c), c = log2(e) / T.
+// The sum of 2^(z c - m) over some logits, m their largest z c rounded: as m is what is subtracted, its rounding is no error.
 struct Lse {
   float m = -INFINITY, s = 0.0f;
 };
 __device__ __forceinline__ float finite_or_zero(float m) { return m == -INFINITY ? 0.0f : m; }
 // A NaN sum stays one; so does infinity, whose own term is exp(inf - inf).
-__device__ __forceinline__ Lse join(Lse a, Lse b, float c) {
+__device__ __forceinline__ Lse join(Lse a, Lse b) {
   const float m = fmaxf(a.m, b.m), ref = finite_or_zero(m);
-  return Lse{m, a.s * __builtin_amdgcn_exp2f((a.m - ref) * c) + b.s * __builtin_amdgcn_exp2f((b.m - ref) * c)};
+  return Lse{m, a.s * __builtin_amdgcn_exp2f(a.m - ref) + b.s * __builtin_amdgcn_exp2f(b.m - ref)};
 }
 
 // Of a workgroup of N: every wave puts its own into LDS, and after a barrier all of them are joined.
-__device__ __forceinline__ void put_lse(Lse v, float c, float (*lds)[2]) {
+__device__ __forceinline__ void put_lse(Lse v, float (*lds)[2]) {
 #pragma unroll
-  for (int d = 32; d > 0; d >>= 1) v = join(v, Lse{__shfl_xor(v.m, d), __shfl_xor(v.s, d)}, c);
+  for (int d = 32; d > 0; d >>= 1) v = join(v, Lse{__shfl_xor(v.m, d), __shfl_xor(v.s, d)});
   if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6][0] = v.m, lds[threadIdx.x >> 6][1] = v.s;
 }
 template <int N>
-__device__ __forceinline__ Lse get_lse(float c, const float (*lds)[2]) {
-  Lse v{lds[0][0], lds[0][1]};
+__device__ __forceinline__ Lse get_lse(const float (*lds)[2]) {
+  const int i = threadIdx.x & (N / 64 - 1);   // each N / 64 lanes for themselves, all alike
+  Lse v{lds[i][0], lds[i][1]};
 #pragma unroll
-  for (int i = 1; i < N / 64; ++i) v = join(v, Lse{lds[i][0], lds[i][1]}, c);
+  for (int d = N / 128; d > 0; d >>= 1) v = join(v, Lse{__shfl_xor(v.m, d), __shfl_xor(v.s, d)});
   return v;
 }
 template <int N>
-__device__ __forceinline__ Lse block_lse(Lse v, float c, float (*lds)[2]) {
-  put_lse(v, c, lds);
+__device__ __forceinline__ Lse block_lse(Lse v, float (*lds)[2]) {
+  put_lse(v, lds);
   __syncthreads();
-  return get_lse<N>(c, lds);
+  return get_lse<N>(lds);
 }
 
-// Adds values to a maximum and sum, which is scaled once for all of them.
+// Adds values to a sum, which is scaled once for all of them.  They are added up by themselves first: where an entry's logit is in the
+// sum, one by one the others would be lost in its rounding.
 template <int N>
 __device__ __forceinline__ void add_to(Lse& l, const float* v, float c) {
-  float top = l.m;
+  float top = v[0];
 #pragma unroll
-  for (int j = 0; j < N; ++j) top = fmaxf(top, v[j]);
-  const float ref = finite_or_zero(top), ref2 = ref * c;
-  float s = l.s * __builtin_amdgcn_exp2f((l.m - ref) * c);
+  for (int j = 1; j < N; ++j) top = fmaxf(top, v[j]);
+  top = fmaxf(l.m, top * c);
+  const float ref = finite_or_zero(top);
+  float s = 0.0f;
 #pragma unroll
-  for (int j = 0; j < N; ++j) s += __builtin_amdgcn_exp2f(fmaf(v[j], c, -ref2));
-  l = Lse{top, s};
+  for (int j = 0; j < N; ++j) s += __builtin_amdgcn_exp2f(fmaf(v[j], c, -ref));
+  l = Lse{top, fmaf(l.s, __builtin_amdgcn_exp2f(l.m - ref), s)};
 }
+
+// Of one entry of a teacher's list; an infinite or NaN logit (or one whose y c overflows) makes all of the list's shares NaN.
+__device__ __forceinline__ Lse one(float y, float c) {
+  const float m = fminf(fmaxf(y * c, -FLT_MAX), FLT_MAX);
+  return Lse{m, fabsf(y) < INFINITY ? __builtin_amdgcn_exp2f(fmaf(y, c, -m)) : NAN};
+}
+// Its share and the share's logarithm, of a list with m and the reciprocal of its sum.
+__device__ __forceinline__ float share_of(float y, float c, Lse l) { return __builtin_amdgcn_exp2f(fmaf(y, c, -l.m)) * l.s; }
+__device__ __forceinline__ float log_share_of(float y, float c, Lse l) { return fmaf(y, c, -l.m) * kLn2 + logf(l.s); }
 
 __device__ __forceinline__ int64_t id_at(const DistillArgs& A, int64_t i) {
   return A.id_type == ISO_I64 ? gmem((const int64_t*)A.ids)[i] : (int64_t)gmem((const int32_t*)A.ids)[i];
@@ -129,14 +142,10 @@ __device__ __forceinline__ Entry list_of(const DistillArgs& A, int64_t row, List
     }
   }
   // the first four waves hold the entries
-  Lse l{y, r.id >= 0 ? 1.0f : 0.0f};
-  if (r.id >= 0 && !(fabsf(y) < INFINITY)) l.s = NAN;   // an infinite or NaN logit of the teacher
-  l = block_lse<256>(l, A.exp2_t, S.red);
+  Lse l = block_lse<256>(r.id >= 0 ? one(y, A.c) : Lse{}, S.red);
   any = l.s != 0.0f;
-  if (r.id >= 0) {
-    r.log_t = (y - l.m) * A.inv_t - logf(l.s);
-    r.t = __builtin_amdgcn_exp2f(r.log_t * kLog2e);
-  }
+  l.s = 1.0f / l.s;
+  if (r.id >= 0) r.log_t = log_share_of(y, A.c, l), r.t = share_of(y, A.c, l);
   if (e < ISO_DISTILL_MAX_TOP) S.id[e] = r.id, S.t[e] = r.t;
   __syncthreads();
   return r;
@@ -155,6 +164,8 @@ __device__ __forceinline__ void merge(const DistillArgs& A, const ListSpace& S, 
   r.t = t;
 }
 
+__device__ __forceinline__ float weight_of(const DistillArgs& A, int64_t row) { return A.w != nullptr ? gmem(A.w)[row] : 1.0f; }
+
 // The row's loss from its entries, in binary64: the sum of t (log t - z + L) cancels where the student has learnt.
 template <int DT>
 __device__ __forceinline__ void store_loss(const DistillArgs& A, int64_t row, const Entry& r, float z, double lse, bool any, double* lds) {
@@ -165,7 +176,7 @@ __device__ __forceinline__ void store_loss(const DistillArgs& A, int64_t row, co
   if ((threadIdx.x & 63) == 0 && threadIdx.x < 256) lds[threadIdx.x >> 6] = v;
   __syncthreads();
   if (threadIdx.x == 0) {
-    const float w = A.w != nullptr ? gmem(A.w)[row] : 1.0f;
+    const float w = weight_of(A, row);
     v = lds[0] + lds[1] + lds[2] + lds[3];
     gmem(A.loss)[row] = any && w != 0.0f ? (float)(w * A.t * A.t * v) : 0.0f;
     gmem(A.lse)[row] = (float)lse;
@@ -209,46 +220,55 @@ __device__ __forceinline__ Lse row_lse(const DistillArgs& A, int64_t row, int64_
     float v[U * V];
 #pragma unroll
     for (int u = 0; u < U; ++u) unpack_raw<DT>(w[u], v + u * V);
-    add_to<U * V>(l, v, A.exp2_t);
+    add_to<U * V>(l, v, A.c);
   }
   for (; c < hi; c += kStride) {
     float v[V];
     unpack_raw<DT>(load_end<DT>(A.z, base + c, hi - c), v);
-    add_to<V>(l, v, A.exp2_t);
+    add_to<V>(l, v, A.c);
   }
-  return block_lse<N>(l, A.exp2_t, lds);
+  return block_lse<N>(l, lds);
 }
 
-// L of a row, in binary64: the loss takes differences of it.
-__device__ __forceinline__ double lse_of(const DistillArgs& A, Lse l) { return (double)l.m / A.t + log((double)l.s); }
+// L of a row, in binary64: the loss takes differences of it.  m / c is a logit but for m's rounding, which s holds; the logarithm of s
+// is that of a value from 1/2 to 1, which binary32 has to 2^-24, and a multiple of log 2.
+__device__ __forceinline__ double lse_of(const DistillArgs& A, Lse l) {
+  const float low = logf(__builtin_amdgcn_frexp_mantf(l.s));
+  return fma((double)l.m, A.inv_tc, fma((double)__builtin_amdgcn_frexp_expf(l.s), 0.6931471805599453, (double)low));
+}
 
-// A row's factor w T, and whether its gradient is zero.
+// A row's factor w T, whether its gradient is zero, and its L: a probability is less 2^(z c - lse2), lse2 being T c L
+// rounded and less the power of two of what that took.
 struct Factor {
-  float f;
+  float f, less, lse2;
   bool zero;
-  __device__ __forceinline__ Factor(const DistillArgs& A, int64_t row, bool any) {
-    const float w = A.w != nullptr ? gmem(A.w)[row] : 1.0f;
+  __device__ __forceinline__ Factor(const DistillArgs& A, float w, double lse, bool any) {
     f = w * (float)A.t;
     zero = !any || w == 0.0f;
+    const double exact = lse * A.tc;
+    lse2 = (float)exact;
+    less = fabsf(lse2) < INFINITY ? (float)(1.0 + (lse2 - exact) * 0.6931471805599453) : 1.0f;
+  }
+  __device__ __forceinline__ float probability(const DistillArgs& A, float z) const {
+    return less * __builtin_amdgcn_exp2f(fmaf(z, A.c, -lse2));
   }
 };
-
-// The gradients of 16 bytes of logits; lse2 = L log2(e).
+// The gradients of 16 bytes of logits.
 template <int DT>
-__device__ __forceinline__ void grads_of(const DistillArgs& A, float f, u32x4_t w, float lse2, float* v) {
+__device__ __forceinline__ void grads_of(const DistillArgs& A, const Factor& F, u32x4_t w, float* v) {
   unpack_raw<DT>(w, v);
+  const float f = F.f * F.less;
 #pragma unroll
-  for (int j = 0; j < kVec<DT>; ++j) v[j] = f * __builtin_amdgcn_exp2f(fmaf(v[j], A.exp2_t, -lse2));
+  for (int j = 0; j < kVec<DT>; ++j) v[j] = f * __builtin_amdgcn_exp2f(fmaf(v[j], A.c, -F.lse2));
 }
 
 // Entries' own gradients, written after all of the row's: columns [lo, hi).
 template <int DT>
-__device__ __forceinline__ void put_entry(const DistillArgs& A, int64_t row, int64_t lo, int64_t hi, const Factor& F, const Entry& r, float z,
-                                          float lse2) {
+__device__ __forceinline__ void put_entry(const DistillArgs& A, int64_t row, int64_t lo, int64_t hi, const Factor& F, const Entry& r, float z) {
   asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
   __syncthreads();
   if (F.zero || !r.first || r.id < lo || r.id >= hi) return;
-  const float v = F.f * (__builtin_amdgcn_exp2f(fmaf(z, A.exp2_t, -lse2)) - r.t);
+  const float v = F.f * (F.probability(A, z) - r.t);
   const int64_t to = row * A.ld_grad + r.id;
   if constexpr (DT == ISO_BF16) gmem((uint16_t*)A.grad)[to] = (uint16_t)pack_bf16(v, 0.0f);
   else gmem((uint32_t*)A.grad)[to] = bits_from_f32(v);
@@ -256,7 +276,7 @@ __device__ __forceinline__ void put_entry(const DistillArgs& A, int64_t row, int
 
 // The gradient of 16 bytes a lane from column c on, U of them 256 lanes apart, of a row of A.vocab columns.
 template <int DT, int U, bool STREAM>
-__device__ __forceinline__ void put_grads(const DistillArgs& A, int64_t row, int64_t c, const Factor& F, const u32x4_t* w, float lse2) {
+__device__ __forceinline__ void put_grads(const DistillArgs& A, int64_t row, int64_t c, const Factor& F, const u32x4_t* w) {
   constexpr int V = kVec<DT>, kStride = 256 * V;
   const int64_t to = row * A.ld_grad;
 #pragma unroll
@@ -264,7 +284,7 @@ __device__ __forceinline__ void put_grads(const DistillArgs& A, int64_t row, int
     const int64_t at = c + u * kStride;
     if (at >= A.vocab) continue;
     float v[V] = {};
-    if (!F.zero) grads_of<DT>(A, F.f, w[u], lse2, v);
+    if (!F.zero) grads_of<DT>(A, F, w[u], v);
     store_elems<DT, V, STREAM>(A.grad, to + at, v, A.vocab - at);
   }
 }
@@ -348,8 +368,9 @@ __global__ void __launch_bounds__(N) k_distill_held(DistillArgs A) {
       y = raw.y;
     }
   }
-  const float z = r.id >= 0 ? load_z<DT>(A, row * A.ld + r.id) : 0.0f;
-  const float weight = A.w != nullptr ? gmem(A.w)[row] : 1.0f;
+  bits z_bits = 0;   // as they are: made a value here, they would be waited for, and the row with them
+  if (r.id >= 0) z_bits = gmem((const bits*)A.z)[row * A.ld + r.id];
+  float weight = weight_of(A, row);
   // the row, as it comes in, one piece after the other
   Lse l;
 #pragma unroll
@@ -358,38 +379,36 @@ __global__ void __launch_bounds__(N) k_distill_held(DistillArgs A) {
     float v[2 * V];
 #pragma unroll
     for (int u = 0; u < 2; ++u) unpack_raw<DT>(w[p + u], v + u * V);
-    add_to<2 * V>(l, v, A.exp2_t);
+    add_to<2 * V>(l, v, A.c);
   }
-  put_lse(l, A.exp2_t, S.red);
-  Lse t{y, r.id >= 0 ? 1.0f : 0.0f};
-  if (r.id >= 0 && !(fabsf(y) < INFINITY)) t.s = NAN;   // an infinite or NaN logit of the teacher
-  put_lse(t, A.exp2_t, S.list.red);
+  asm volatile("" : "+v"(z_bits), "+v"(weight));
+  const float z = f32_from_bits(DT == ISO_BF16 ? (uint32_t)z_bits << 16 : (uint32_t)z_bits);
+  put_lse(l, S.red);
+  put_lse(r.id >= 0 ? one(y, A.c) : Lse{}, S.list.red);
   if (e < ISO_DISTILL_MAX_TOP) S.list.id[e] = r.id, S.list.t[e] = y;
   S.head[e] = -1;
   __syncthreads();
-  l = get_lse<N>(A.exp2_t, S.red);
-  t = get_lse<256>(A.exp2_t, S.list.red);   // the first four waves hold the entries
+  l = get_lse<N>(S.red);
+  Lse t = get_lse<256>(S.list.red);   // the first four waves hold the entries
   const bool any = t.s != 0.0f;
-  const float log_s = logf(t.s);
-  auto share = [&](float v) { return (v - t.m) * A.inv_t - log_s; };
-  if (r.id >= 0) r.log_t = share(y), r.t = __builtin_amdgcn_exp2f(r.log_t * kLog2e);
+  t.s = 1.0f / t.s;
+  if (r.id >= 0) r.log_t = log_share_of(y, A.c, t), r.t = share_of(y, A.c, t);
   const double lse = lse_of(A, l);
-  const float lse2 = (float)(lse * 1.4426950408889634), f = weight * (float)A.t;
-  const bool zero = !any || weight == 0.0f;
+  const Factor F(A, weight, lse, any);
   double part = r.id >= 0 && r.t != 0.0f ? (double)r.t * ((double)r.log_t - (double)z / A.t + lse) : 0.0;
 #pragma unroll
   for (int d = 32; d > 0; d >>= 1) part += __shfl_xor(part, d);
   if ((e & 63) == 0 && e < 256) S.sums[e >> 6] = part;
-  if (!zero && r.id >= 0) {   // as merge(), but for the logits in LDS; the first of the entries adds in their order
+  if (!F.zero && r.id >= 0) {   // as merge(), but for the logits in LDS; the first of the entries adds in their order
     r.first = true;
     for (int i = 0; i < A.top; ++i)
       if (S.list.id[i] == r.id && i != e) {
         if (i < e) r.first = false;
-        r.t += __builtin_amdgcn_exp2f(share(S.list.t[i]) * kLog2e);
+        r.t += share_of(S.list.t[i], A.c, t);
       }
   }
   if (r.first) {
-    S.value[e] = f * (__builtin_amdgcn_exp2f(fmaf(z, A.exp2_t, -lse2)) - r.t);
+    S.value[e] = F.f * (F.probability(A, z) - r.t);
     S.next[e] = (int16_t)atomicExch(&S.head[r.id / V % N], e);
   }
   // every entry has its logit: the gradient may lie over the logits
@@ -397,7 +416,7 @@ __global__ void __launch_bounds__(N) k_distill_held(DistillArgs A) {
   __syncthreads();
   if (e == 0) {
     part = S.sums[0] + S.sums[1] + S.sums[2] + S.sums[3];
-    gmem(A.loss)[row] = zero ? 0.0f : (float)(weight * A.t * A.t * part);
+    gmem(A.loss)[row] = F.zero ? 0.0f : (float)(weight * A.t * A.t * part);
     gmem(A.lse)[row] = (float)lse;
   }
   const int head = S.head[e];
@@ -410,7 +429,7 @@ __global__ void __launch_bounds__(N) k_distill_held(DistillArgs A) {
     const int32_t left = vocab - p * N * V - (int32_t)mine;
     if (left <= 0) continue;
     float v[V] = {};
-    if (!zero) grads_of<DT>(A, f, w[p], lse2, v);
+    if (!F.zero) grads_of<DT>(A, F, w[p], v);
     if (has >> p & 1u)
       for (int i = head; i >= 0; i = S.next[i]) {
         const int32_t id = S.list.id[i];
@@ -441,9 +460,9 @@ __global__ void __launch_bounds__(256) k_distill_join(DistillArgs A) {
   Lse l;
   for (int i = threadIdx.x; i < A.pieces; i += 256) {
     const auto p = gmem((const float*)A.part) + 2 * (row * A.pieces + i);
-    l = join(l, Lse{p[0], p[1]}, A.exp2_t);
+    l = join(l, Lse{p[0], p[1]});
   }
-  l = block_lse<256>(l, A.exp2_t, S.red);
+  l = block_lse<256>(l, S.red);
   __syncthreads();
   bool any;
   const Entry r = list_of<256>(A, row, S, any);
@@ -471,11 +490,10 @@ __global__ void __launch_bounds__(256) k_distill_grad(DistillArgs A, uint32_t pi
   const bool here = r.id >= lo && r.id < lo + kGradPiece<DT>;
   const float z = here ? load_z<DT>(A, row * A.ld + r.id) : 0.0f;
   if (here) merge(A, S, r);
-  const Factor F(A, row, any);
-  const float lse2 = gmem(A.lse)[row] * kLog2e;
+  const Factor F(A, weight_of(A, row), gmem(A.lse)[row], any);
   before_writes(z);
-  put_grads<DT, 4, STREAM>(A, row, c, F, w, lse2);
-  put_entry<DT>(A, row, lo, lo + kGradPiece<DT>, F, r, z, lse2);
+  put_grads<DT, 4, STREAM>(A, row, c, F, w);
+  put_entry<DT>(A, row, lo, lo + kGradPiece<DT>, F, r, z);
 }
 
 DistillArgs args_of(const iso_distill& d, uint8_t* ws) {
@@ -483,7 +501,7 @@ DistillArgs args_of(const iso_distill& d, uint8_t* ws) {
   A.z = d.logits, A.ids = d.ids, A.y = d.teacher, A.w = d.weight, A.loss = d.loss, A.lse = d.lse, A.grad = d.grad;
   A.tokens = d.tokens, A.vocab = d.vocab, A.ld = d.ld, A.ld_grad = d.ld_grad, A.pad_id = d.pad_id;
   A.top = d.top, A.id_type = d.id_type;
-  A.inv_t = (float)(1.0 / d.temperature), A.exp2_t = (float)(1.4426950408889634 / d.temperature), A.t = d.temperature;
+  A.c = (float)(1.4426950408889634 / d.temperature), A.t = d.temperature, A.tc = A.t * A.c, A.inv_tc = 1.0 / A.tc;
   A.status = (uint32_t*)ws;
   A.part = (float*)(ws + kStatusBytes);
   return A;
