@@ -328,11 +328,12 @@ struct HeldSpace {
   float red[16][2], value[ISO_DISTILL_MAX_TOP];
   double sums[4];
   int16_t next[ISO_DISTILL_MAX_TOP];
+  u32x4_t rest;      // what is left of a row behind its pieces
   int32_t head[N];   // the first of the entries that lie in a lane's columns; -1: none
 };
 
 // Loss and gradient of a row that a workgroup of N holds in registers, PER pieces of 16 bytes a lane: read once, written once
-// (4096 x 152064 bf16: 513 us, 4.9 TB/s, the rate of a plain copy).
+// (4096 x 152064 bf16: 486 us, 5.1 TB/s, the rate of a plain copy).
 // All of a row is under way at once; what a CU does between its loads and its stores, other CUs' loads and stores fill.  Entries
 // change the pieces they lie in before these are stored (a lane has a list of its own): written after them they would have to
 // wait for the stores.  Workgroups that walk over rows and load a piece of the next row where one of this is stored were tried:
@@ -344,18 +345,22 @@ __global__ void __launch_bounds__(N) k_distill_held(DistillArgs A) {
   __shared__ HeldSpace<N> S;
   const int32_t vocab = (int32_t)A.vocab;
   const int e = threadIdx.x;
-  const uint32_t mine = threadIdx.x * V;
+  uint32_t mine = threadIdx.x * V;
   const int64_t row = blockIdx.x;
   if (row == 0 && A.tokens * A.top <= kFewEntries) check_ids(A);
+  // Every lane makes the same loads: the compiler counts them, and the row is summed as it comes in.  What lies behind the row's end is
+  // taken from its last 16 bytes and replaced below, by minus infinity or by what is left of a piece.
+  const bits* const z_row = (const bits*)A.z + row * A.ld;
   u32x4_t w[PER];
-  // the first column of a round is the same in all lanes and goes into the instruction's base
+  const int32_t whole = vocab % V != 0 ? vocab / V * V : -1;
+  if (whole >= 0 && e == whole / V % N) S.rest = load_end<DT>(z_row, whole, vocab - whole);   // and reads it
   RawEntry raw;
   raw.load(A, row);
+  const uint32_t last = (uint32_t)(vocab - V) * sizeof(bits);
 #pragma unroll
   for (int p = 0; p < PER; ++p) {
-    const bits* const at = (const bits*)A.z + row * A.ld + p * N * V;
-    if ((p + 1) * N * V <= vocab) w[p] = load_raw<DT>(at, mine);
-    else w[p] = load_end<DT>(at, mine, vocab - p * N * V - (int32_t)mine);
+    const uint32_t at = min((uint32_t)(p * N * 16 + e * 16), last);   // bytes from a base that is the same in all lanes
+    w[p] = *(global_ptr<const u32x4_any>)(gmem((const uint8_t*)z_row) + at);
   }
   // the list, and the logits of its entries behind the row's own
   Entry r;
@@ -372,13 +377,19 @@ __global__ void __launch_bounds__(N) k_distill_held(DistillArgs A) {
   if (r.id >= 0) z_bits = gmem((const bits*)A.z)[row * A.ld + r.id];
   float weight = weight_of(A, row);
   // the row, as it comes in, one piece after the other
+  constexpr uint32_t kNone = DT == ISO_BF16 ? 0xFF80FF80u : 0xFF800000u;
+  const u32x4_t none = {kNone, kNone, kNone, kNone};
   Lse l;
 #pragma unroll
   for (int p = 0; p < PER; p += 2) {
-    asm volatile("" : "+v"(w[p]), "+v"(w[p + 1]), "+v"(l.s));
+    asm volatile("" : "+v"(w[p]), "+v"(w[p + 1]), "+v"(l.s), "+v"(l.m), "+v"(mine));
     float v[2 * V];
 #pragma unroll
-    for (int u = 0; u < 2; ++u) unpack_raw<DT>(w[p + u], v + u * V);
+    for (int u = 0; u < 2; ++u) {
+      const int32_t c = (p + u) * N * V + (int32_t)mine;
+      if ((p + u + 1) * N * V > vocab && c > vocab - V) w[p + u] = c == whole ? S.rest : none;
+      unpack_raw<DT>(w[p + u], v + u * V);
+    }
     add_to<2 * V>(l, v, A.c);
   }
   asm volatile("" : "+v"(z_bits), "+v"(weight));
@@ -424,7 +435,7 @@ __global__ void __launch_bounds__(N) k_distill_held(DistillArgs A) {
   for (int i = head; i >= 0; i = S.next[i]) has |= 1u << (S.list.id[i] / (N * V));
 #pragma unroll
   for (int p = 0; p < PER; ++p) {
-    asm volatile("" : "+v"(w[p]));   // unpacked again: there are registers for the row, not for its values twice over
+    asm volatile("" : "+v"(w[p]), "+v"(mine));   // unpacked again: there are registers for the row, not for its values twice over
     bits* const at = (bits*)A.grad + row * A.ld_grad + p * N * V;
     const int32_t left = vocab - p * N * V - (int32_t)mine;
     if (left <= 0) continue;
@@ -531,7 +542,7 @@ template <int DT, bool STREAM>
 void loss(DistillArgs A, hipStream_t s) {
   constexpr int V = kVec<DT>;
   const unsigned n = (unsigned)A.tokens;
-  const bool held = A.grad != nullptr && A.vocab <= 1024 * 20 * V;
+  const bool held = A.grad != nullptr && A.vocab >= V && A.vocab <= 1024 * 20 * V;
   const bool shared = A.vocab > (256 << 10) * V / 16 && A.tokens <= 64;
   if (held && !shared) {
     if (A.vocab <= 256 * 4 * V) k_distill_held<DT, 256, 4, STREAM><<<n, 256, 0, s>>>(A);
