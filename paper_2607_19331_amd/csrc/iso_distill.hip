@@ -114,7 +114,7 @@ __global__ void k_distill_clear(uint32_t* status) { *status = 0; }
 // A token's list: thread e (of at least 256) has entry e.
 struct Entry {
   int32_t id = -1;     // -1: none
-  float t = 0.0f;      // its share; that of all entries with the same id where `sum` was called
+  float t = 0.0f;      // its share; that of all entries with the same id after merge()
   float log_t = 0.0f;
   bool first = false;  // the first of the entries with its id
 };
