@@ -255,12 +255,12 @@ struct Item {
   int32_t piece;
 };
 
-// Item `item` of the list of all sequences' items: of tiles of TILE rows (queries times the group) from the last on, or of keys
-// from the first on, either way beginning with those that have most to do under a causal mask.  Up to 64 sequences are taken level by
-// level (tiles that have as many before them, or behind them for keys), so that the last workgroups to start are short whichever
-// sequences are long; more are taken one after the other.  Either way, four sequences of 2048, 8 heads, fp32: 314 and 497 us; 12 heads over
-// 2, bf16: 72 and 85, backward 231 and 245; 16 samples of 1 to 2048 tokens, backward 283 and 305; 64 sequences of one new token (whose
-// search is skipped) 121 and 120.  Every lane of a wave takes part, each with a sequence.
+// Item `item` of the list of all sequences' items, tiles of TILE rows (queries times the group) or of keys, those that have most to do
+// under a causal mask first.  Up to 64 sequences are taken level by level (tiles that have as many before them, or behind them for
+// keys), so that the last workgroups to start are short whichever sequences are long; more are taken one after the other, a workgroup
+// looking no further than its own.  Level by level and one after the other, four sequences of 2048, 8 heads, fp32: 314 and 497 us; 12
+// heads over 2, bf16: 72 and 85, backward 231 and 245; 16 samples of 1 to 2048 tokens, backward 284 and 305; 64 sequences of one new
+// token (whose levels are not searched) 121 and 120.  Every lane of a wave takes part, each with a sequence.
 template <bool KEYS, int TILE>
 __device__ __forceinline__ bool find_item(const AttnArgs& A, const Pieces& p, uint32_t item, Item& found) {
   const int lane = threadIdx.x & 63;
@@ -314,23 +314,17 @@ __device__ __forceinline__ bool find_item(const AttnArgs& A, const Pieces& p, ui
     return true;
   }
   uint32_t before = 0;
-  if (!KEYS) {
-    uint32_t all = 0;
-    for (int32_t s0 = 0; s0 < A.sequences; s0 += 64) look(s0), all += of(up_to(tiles * pieces), 63);
-    if (item >= all) return false;
-    item = all - 1 - item;
-  }
   for (int32_t s0 = 0; s0 < A.sequences; s0 += 64) {
     look(s0);
     const uint32_t sum = up_to(tiles * pieces);
     const uint64_t behind = __ballot(before + sum > item);
     if (behind != 0) {
       const int src = __builtin_ctzll(behind);
-      const uint32_t in = item - before - of(sum - tiles * pieces, src), each = of(pieces, src);
+      const uint32_t in = item - before - of(sum - tiles * pieces, src), tile = in / of(pieces, src);
       take(src);
-      found.tile = in / each;
-      found.piece = (int32_t)(in - found.tile * each);
-      return found.tile < of(tiles, src);
+      found.tile = KEYS ? tile : of(tiles, src) - 1 - tile;
+      found.piece = (int32_t)(in - tile * of(pieces, src));
+      return true;
     }
     before += of(sum, 63);
   }
