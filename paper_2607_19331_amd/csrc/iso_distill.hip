@@ -535,15 +535,15 @@ void gradient(const DistillArgs& A, bool check, hipStream_t s) {
 // Rows with a gradient that fit into a workgroup's registers are read once (k_distill_held), others' loss is formed before their
 // gradient: both in one kernel, with two walks over a row, took 7 to 17% longer (2048 x 152064 fp32: 737 us for 665).  Few long rows
 // are shared out, loss and join and gradient in a launch each; microseconds for rows of 304 KB, shared out and whole, with the
-// gradient 1 token 17, 25; 64 27, 28; 128 39, 29; the loss alone 1 token 13.1, 13.7; 64 13.4, 14.6; 128 20.6, 17.2; rows of 128 KB 18, 19
-// with the gradient and 13, 11 without.  Where there is no more than a row a CU, 1024 threads have it (608 KB, 128 rows: 20 us, with 256
+// gradient 1 token 17, 25; 64 27, 28; 128 39, 29; the loss alone 1 token 13.1, 13.7; 64 13.4, 14.6; 128 20.6, 17.2; rows of 200 KB with
+// the gradient 1 token 17, 22; 64 23, 25; the loss alone 13.5, 10; rows of 100 KB with the gradient 18, 17.  Where there is no more than a row a CU, 1024 threads have it (608 KB, 128 rows: 20 us, with 256
 // threads 33; 512 rows: 59 and 52).
 template <int DT, bool STREAM>
 void loss(DistillArgs A, hipStream_t s) {
   constexpr int V = kVec<DT>;
   const unsigned n = (unsigned)A.tokens;
   const bool held = A.grad != nullptr && A.vocab >= V && A.vocab <= 1024 * 20 * V;
-  const bool shared = A.vocab > (256 << 10) * V / 16 && A.tokens <= 64;
+  const bool shared = A.vocab > ((A.grad != nullptr ? 128 : 256) << 10) * V / 16 && A.tokens <= 64;
   if (held && !shared) {
     if (A.vocab <= 256 * 4 * V) k_distill_held<DT, 256, 4, STREAM><<<n, 256, 0, s>>>(A);
     else if (A.vocab <= 256 * 20 * V) k_distill_held<DT, 256, 20, STREAM><<<n, 256, 0, s>>>(A);
