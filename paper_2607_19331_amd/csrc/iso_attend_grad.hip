@@ -53,10 +53,11 @@ __global__ void __launch_bounds__(256) k_attend_stat(AttnArgs A) {
 // all rows of the wave see, is added with it at the end: sum S k = sum round(S) k + sum (S - round(S)) (k - c) + c sum (S - round(S)),
 // of which the middle is left out.  With a bias of twice the keys' own width the error of dQ is 2.4 thousandths instead of 4.2, of
 // which 1.7 are its own rounding.
-template <int D>
+template <int DT, int D>
 struct Common {
   static constexpr int kKeys = 16;
-  uint32_t lds;      // 512 bytes of the wave
+  static constexpr uint32_t kBytes = 512;   // of LDS, a wave
+  uint32_t lds;
 
   // Of keys [from, to) the first kKeys.  Before the loop and from memory, not from the panels as they come by: branches in the loop
   // cost registers that it has not got.
@@ -87,6 +88,21 @@ struct Common {
         __builtin_amdgcn_sched_barrier(0);
       }
   }
+};
+// fp32 rounds no S: no sum, and no LDS.
+template <int D>
+struct Common<ISO_F32, D> {
+  static constexpr uint32_t kBytes = 0;
+  __device__ __forceinline__ Common(const AttnArgs&, uint32_t, int64_t, int32_t, int32_t, int64_t, int) {}
+  __device__ __forceinline__ void add(f32x16_t (&)[D / 32], float, int) const {}
+};
+
+// Workgroup layout of dq_tile: two panels of keys, two of values, and what a wave keeps for Common.
+template <int DT, int D>
+struct Dq {
+  using P = Panel<DT, D>;
+  static constexpr uint32_t kV = 2 * P::kBytes, kCommon = 4 * P::kBytes;
+  static constexpr uint32_t kLds = kCommon + kAttnWaves * Common<DT, D>::kBytes;
 };
 
 // dQ of a tile: as the forward kernel, 128 rows of a group's list a workgroup and panels of 64 keys and values in LDS twice over; Q and
@@ -125,14 +141,15 @@ __device__ __forceinline__ void dq_tile(const AttnArgs& A, const Deal& deal, uin
   Rows<DT, D> kr(A.k, s.k0 + all.lo, A.ld_k, col, s.nk - all.lo, A.dim, w, lane);
   Rows<DT, D> vr(A.v, s.k0 + all.lo, A.ld_v, col, s.nk - all.lo, A.dim, w, lane);
   const uint32_t lds = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(lds_u8*)smem);
-  constexpr uint32_t kV = 2 * P::kBytes;   // two panels of keys, then two of values
+  using S = Dq<DT, D>;
+  constexpr uint32_t kV = S::kV;
   const Reader<DT, D> rd(lds, lane);
   kr.skip(first), vr.skip(first);
   if (first < last) {
     kr.load(lds, w);
     vr.load(lds + kV, w);
   }
-  const Common<D> common(A, lds + 4 * P::kBytes + w * 512, s.k0, lo_all, DT == ISO_BF16 ? mine.hi_all : lo_all, col, lane);
+  const Common<DT, D> common(A, lds + S::kCommon + w * Common<DT, D>::kBytes, s.k0, lo_all, mine.hi_all, col, lane);
   OwnRow<DT, D> q, g;
   q.load(A.q, to * A.ld_q + (int64_t)h * A.dim, A.dim, half, on);
   g.load(A.dout, to * A.ld_dout + (int64_t)h * A.dim, A.dim, half, on);
@@ -232,7 +249,7 @@ __device__ __forceinline__ void dq_tile(const AttnArgs& A, const Deal& deal, uin
     step(t, 0);
     if (t + 1 < last) step(t + 1, 1);
   }
-  if constexpr (DT == ISO_BF16) common.add(dq, sum_of_halves(lost), half);
+  common.add(dq, sum_of_halves(lost), half);
   asm volatile("s_waitcnt vmcnt(0)" ::: "memory");   // no load may reach LDS after the workgroup's end
 
   if (pieces > 1) {
@@ -605,7 +622,7 @@ hipError_t backward(AttnArgs A, const AttendPlan& plan, uint8_t* ws, hipStream_t
   const Deal dkv = deal_of(A.heads_kv, attend_items(A.tokens_k, list, A.sequences, A.key_pieces));
   const Deal dq = deal_of(A.heads_kv, attend_items(list, A.tokens_k, A.sequences, A.pieces));
   const uint32_t of_keys = keys > 0 ? deal_grid(dkv, A.heads_kv) : 0, of_rows = rows > 0 ? deal_grid(dq, A.heads_kv) : 0;
-  constexpr uint32_t lds = std::max((uint32_t)(4 * Panel<DT, D>::kBytes + (DT == ISO_BF16 ? kAttnWaves * 512 : 0)), Dkv<DT, D>::kLds);
+  constexpr uint32_t lds = std::max(Dq<DT, D>::kLds, Dkv<DT, D>::kLds);
   if (of_keys + of_rows > 0) k_attend_grad<DT, D><<<of_keys + of_rows, 256, lds, s>>>(A, dkv, dq, of_keys);
   const uint32_t join_keys = A.key_pieces.most > 1 ? (uint32_t)((keys + 3) / 4) : 0, join_rows = A.pieces.most > 1 ? (uint32_t)((rows + 7) / 8) : 0;
   if (join_keys + join_rows > 0) k_attend_grad_join<DT><<<join_keys + join_rows, 256, 0, s>>>(A, join_keys);
