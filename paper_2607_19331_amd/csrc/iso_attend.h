@@ -71,12 +71,25 @@ __device__ __forceinline__ bool seq_range(const int32_t* start, int64_t s, int64
   return ok;
 }
 
+// Whether both offsets of a sequence are ranges; if not, it has no rows.
+__device__ __forceinline__ bool seq_of(const AttnArgs& A, int64_t s, Seq& r) {
+  const bool q = seq_range(A.start_q, s, A.tokens_q, r.q0, r.nq), k = seq_range(A.start_k, s, A.tokens_k, r.k0, r.nk);
+  if (!q || !k) r = Seq{0, 0, 0, 0};
+  return q && k;
+}
 __device__ __forceinline__ Seq seq_of(const AttnArgs& A, int64_t s) {
   Seq r;
-  const bool q = seq_range(A.start_q, s, A.tokens_q, r.q0, r.nq), k = seq_range(A.start_k, s, A.tokens_k, r.k0, r.nk);
-  if (!q || !k) r.nq = r.nk = 0;
+  seq_of(A, s, r);
   return r;
 }
+
+// The last rows that sequences have taken: one that begins before them is left out too, so that no two share a row.  That takes offsets
+// that do not ascend, and then some sequence's are no range.
+struct Taken {
+  int64_t q = 0, k = 0;
+  __device__ __forceinline__ bool free(const Seq& s) const { return s.q0 >= q && s.k0 >= k; }
+  __device__ __forceinline__ void add(const Seq& s) { q = max(q, s.q0 + s.nq), k = max(k, s.k0 + s.nk); }
+};
 
 // The keys that query i of the sequence sees: [lo, hi), and the queries that see key j.
 __device__ __forceinline__ void keys_of(const AttnArgs& A, const Seq& s, int64_t i, int32_t& lo, int32_t& hi) {

@@ -18,9 +18,9 @@ namespace iso {
 
 namespace {
 
-// L log2(e) and D of every row, 16 lanes a row, in the order of the groups' lists: a panel's come into LDS with one load.  Bound by
-// memory: O and dO read once (16384 tokens, 28 heads of 128: 57 us, 4.1 TB/s; four rows
-// for each 16 lanes 54).
+// L log2(e) and D of every row, 16 lanes a row, in the order of the groups' lists: a panel's come into LDS with one load.  A row's place
+// there does not depend on its sequence, so that none is looked up; those of rows without one are not used.  Bound by memory: O and dO
+// read once.
 template <int DT>
 __global__ void __launch_bounds__(256) k_attend_stat(AttnArgs A) {
   if (blockIdx.x == gridDim.x - 1) return check_starts(A);
@@ -28,19 +28,17 @@ __global__ void __launch_bounds__(256) k_attend_stat(AttnArgs A) {
   if (t >= A.tokens_q || A.sequences == 0) return;   // without sequences, pointers may be null
   const int h = (int)(at - t * A.heads), head = h / A.group, c = (threadIdx.x & 15) * 8;
   float o[8] = {}, g[8] = {}, sum = 0.0f;
-  if (c < A.dim) {   // under way while the sequence is looked up
+  if (c < A.dim) {
     load_elems<DT, 8>(A.out, t * A.ld_out + (int64_t)h * A.dim + c, o);
     load_elems<DT, 8>(A.dout, t * A.ld_dout + (int64_t)h * A.dim + c, g);
   }
   const float lse = gmem(A.lse)[at];
-  const Seq s = seq_at(A, A.start_q, t);
-  if (t < s.q0 || t >= s.q0 + s.nq) return;
 #pragma unroll
   for (int j = 0; j < 8; ++j) sum = fmaf(o[j], g[j], sum);
 #pragma unroll
   for (int d = 8; d > 0; d >>= 1) sum += __shfl_xor(sum, d);
   if (c == 0) {
-    const int64_t to = list_of(A, s, head) + (t - s.q0) * A.group + h % A.group;
+    const int64_t to = (head * A.tokens_q + t) * A.group + h - head * A.group;
     gmem(A.stat)[to] = lse * kLog2e;
     gmem(A.stat)[A.tokens_q * A.heads + to] = sum;
   }
@@ -575,7 +573,7 @@ __device__ __forceinline__ void dkv_join(const AttnArgs& A, uint32_t block) {
   constexpr int kKeys = 32 * kAttnWaves;
   const int64_t at = (int64_t)block * 4 + (threadIdx.x >> 6), t = at / A.heads_kv;
   if (t >= A.tokens_k) return;
-  const Seq s = seq_at(A, A.start_k, t);
+  const Seq s = seq_at<true>(A, t);
   if (t < s.k0 || t >= s.k0 + s.nk) return;
   const int head = (int)(at - t * A.heads_kv), lane = threadIdx.x & 63, c = 4 * (lane & 31);
   const int32_t key = (int32_t)(t - s.k0), key0 = key / kKeys * kKeys;

@@ -255,6 +255,24 @@ struct Item {
   int32_t piece;
 };
 
+// Sequences that a wave looks at, a lane each, where some offsets do not ascend: those that begin before the end of an earlier range get
+// no rows.  `taken`: by the sequences before these, and then by these too.
+__device__ __forceinline__ void only_free(Seq& mine, bool range, Taken& taken) {
+  const int lane = threadIdx.x & 63;
+  Taken up_to;   // this lane
+  if (range) up_to.add(mine);
+#pragma unroll 1
+  for (int d = 1; d < 64; d <<= 1) {
+    const int64_t q = __shfl_up(up_to.q, d), k = __shfl_up(up_to.k, d);
+    if (lane >= d) up_to.q = max(up_to.q, q), up_to.k = max(up_to.k, k);
+  }
+  Taken before{__shfl_up(up_to.q, 1), __shfl_up(up_to.k, 1)};
+  if (lane == 0) before = Taken{};
+  before.q = max(before.q, taken.q), before.k = max(before.k, taken.k);
+  if (!range || !before.free(mine)) mine = Seq{0, 0, 0, 0};
+  taken = Taken{max(taken.q, __shfl(up_to.q, 63)), max(taken.k, __shfl(up_to.k, 63))};
+}
+
 // Item `item` of the list of all sequences' items, tiles of TILE rows (queries times the group) or of keys, those that have most to do
 // under a causal mask first.  Up to 64 sequences are taken level by level (tiles that have as many before them, or behind them for
 // keys), so that the last workgroups to start are short whichever sequences are long; more are taken one after the other, a workgroup
@@ -266,9 +284,17 @@ __device__ __forceinline__ bool find_item(const AttnArgs& A, const Pieces& p, ui
   const int lane = threadIdx.x & 63;
   Seq mine;
   uint32_t tiles, pieces;
+  bool ascend = true;   // all offsets so far
+  Taken taken;          // by the sequences so far, if not
   auto look = [&](int32_t s0) {
     mine = Seq{0, 0, 0, 0};
-    if (s0 + lane < A.sequences) mine = seq_of(A, s0 + lane);
+    bool range = true;
+    if (s0 + lane < A.sequences) range = seq_of(A, s0 + lane, mine);
+    if (__any(!range) || !ascend) {
+      if (ascend && s0 > 0) taken = Taken{gmem(A.start_q)[s0], gmem(A.start_k)[s0]};
+      ascend = false;
+      only_free(mine, range && s0 + lane < A.sequences, taken);
+    }
     const uint32_t rows = (uint32_t)mine.nq * (uint32_t)A.group, keys = (uint32_t)mine.nk;
     tiles = ((KEYS ? keys : rows) + TILE - 1) / TILE;
     pieces = min((uint32_t)p.most, max(1u, ((KEYS ? rows : keys) + p.keys - 1) / p.keys));
@@ -331,28 +357,48 @@ __device__ __forceinline__ bool find_item(const AttnArgs& A, const Pieces& p, ui
   return false;
 }
 
-// The sequence whose range holds row t; a sequence without rows where there is none.
-__device__ __forceinline__ Seq seq_at(const AttnArgs& A, const int32_t* start, int64_t t) {
+// The sequence that holds row t of q (of k: KEYS); one without rows where there is none.  For the joins, whose sequences are fewer than
+// a thousand (there are no pieces where tiles are many) and whose call has looked at its offsets: where they do not ascend, the
+// sequences are gone through as find_item does.
+template <bool KEYS>
+__device__ __forceinline__ Seq seq_among(const AttnArgs& A, int64_t t) {
+  Taken taken;
+  for (int32_t i = 0; i < A.sequences; ++i) {
+    Seq s;
+    if (!seq_of(A, i, s)) continue;
+    const bool free = taken.free(s);
+    taken.add(s);
+    if (free && (KEYS ? t >= s.k0 && t < s.k0 + s.nk : t >= s.q0 && t < s.q0 + s.nq)) return s;
+  }
+  return Seq{};
+}
+
+template <bool KEYS>
+__device__ __forceinline__ Seq seq_at(const AttnArgs& A, int64_t t) {
   if (A.sequences == 0) return Seq{};
+  const auto start = gmem(KEYS ? A.start_k : A.start_q);
+  const uint32_t status = *gmem((const uint32_t*)A.status);
   int32_t lo = 0, hi = A.sequences - 1;
   while (lo < hi) {   // the first sequence that ends behind t
     const int32_t m = (lo + hi) / 2;
-    if (gmem(start)[m + 1] > t) hi = m;
+    if (start[m + 1] > t) hi = m;
     else lo = m + 1;
   }
-  return seq_of(A, lo);
+  return status == 0 ? seq_of(A, lo) : seq_among<KEYS>(A, t);
 }
 
-// The same where half a wave asks for one row: up to 64 sequences are looked at at once.
-__device__ __forceinline__ Seq seq_at_half(const AttnArgs& A, const int32_t* start, int64_t t) {
-  if (A.sequences > 64) return seq_at(A, start, t);
+// The same where half a wave asks for one row of q: up to 64 sequences are looked at at once.
+__device__ __forceinline__ Seq seq_at_half(const AttnArgs& A, int64_t t) {
+  if (A.sequences > 64) return seq_at<false>(A, t);
   const int lane = threadIdx.x & 31, side = threadIdx.x & 32;
+  const uint32_t status = *gmem((const uint32_t*)A.status);
   uint64_t ends = 0;
 #pragma unroll
   for (int i = 0; i < 2; ++i) {
-    const bool behind = lane + 32 * i < A.sequences && gmem(start)[lane + 32 * i + 1] > t;
+    const bool behind = lane + 32 * i < A.sequences && gmem(A.start_q)[lane + 32 * i + 1] > t;
     ends |= (__ballot(behind) >> side & 0xFFFFFFFFull) << (32 * i);
   }
+  if (status != 0) return seq_among<false>(A, t);
   return ends != 0 ? seq_of(A, __builtin_ctzll(ends)) : Seq{};
 }
 
@@ -388,7 +434,7 @@ struct JoinRow {
   int32_t h, r;   // head, and row of its group's list
   bool on;
   __device__ __forceinline__ JoinRow(const AttnArgs& A, int64_t at_) : at(at_), t(at_ / A.heads), s(), h(0), r(0), on(t < A.tokens_q) {
-    if (on) s = seq_at_half(A, A.start_q, t);
+    if (on) s = seq_at_half(A, t);
     on = on && t >= s.q0 && t < s.q0 + s.nq;
     h = (int32_t)(at - t * A.heads);
     if (on) r = (int32_t)(t - s.q0) * A.group + h % A.group;
