@@ -3,7 +3,6 @@
 //
 // Bound by memory: 2 (or 4) bytes of a logit read, as many written for a gradient, against one exponential each (two for both in
 // one call).  The list (up to 256 entries, one a thread) is a few microseconds of latency a row, hidden under other rows.
-#include <float.h>
 #include <hip/hip_runtime.h>
 #include <math.h>
 #include <stdint.h>
@@ -30,6 +29,7 @@ struct DistillArgs {
   int64_t tokens, vocab, ld, ld_grad, pad_id;
   int32_t top, id_type, pieces;   // pieces: workgroups a row
   float c;                        // log2(e) / T
+  double log2e_t;                 // the same, not rounded to binary32
   double t, tc, inv_tc;           // T, T c and its reciprocal
   float* part;                    // reference and sum of a piece, tokens x pieces
   uint32_t* status;
@@ -40,31 +40,31 @@ struct Lse {
   float m = -INFINITY, s = 0.0f;
 };
 __device__ __forceinline__ float finite_or_zero(float m) { return m == -INFINITY ? 0.0f : m; }
-// A NaN sum stays one; so does infinity, whose own term is exp(inf - inf).
-__device__ __forceinline__ Lse join(Lse a, Lse b) {
+// A NaN sum stays one; so does infinity, whose own term is exp(inf - inf).  c: what differences of m count (a list's, see one()).
+__device__ __forceinline__ Lse join(Lse a, Lse b, float c) {
   const float m = fmaxf(a.m, b.m), ref = finite_or_zero(m);
-  return Lse{m, a.s * __builtin_amdgcn_exp2f(a.m - ref) + b.s * __builtin_amdgcn_exp2f(b.m - ref)};
+  return Lse{m, a.s * __builtin_amdgcn_exp2f((a.m - ref) * c) + b.s * __builtin_amdgcn_exp2f((b.m - ref) * c)};
 }
 
 // Of a workgroup of N: every wave puts its own into LDS, and after a barrier all of them are joined.
-__device__ __forceinline__ void put_lse(Lse v, float (*lds)[2]) {
+__device__ __forceinline__ void put_lse(Lse v, float (*lds)[2], float c = 1.0f) {
 #pragma unroll
-  for (int d = 32; d > 0; d >>= 1) v = join(v, Lse{__shfl_xor(v.m, d), __shfl_xor(v.s, d)});
+  for (int d = 32; d > 0; d >>= 1) v = join(v, Lse{__shfl_xor(v.m, d), __shfl_xor(v.s, d)}, c);
   if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6][0] = v.m, lds[threadIdx.x >> 6][1] = v.s;
 }
 template <int N>
-__device__ __forceinline__ Lse get_lse(const float (*lds)[2]) {
+__device__ __forceinline__ Lse get_lse(const float (*lds)[2], float c = 1.0f) {
   const int i = threadIdx.x & (N / 64 - 1);   // each N / 64 lanes for themselves, all alike
   Lse v{lds[i][0], lds[i][1]};
 #pragma unroll
-  for (int d = N / 128; d > 0; d >>= 1) v = join(v, Lse{__shfl_xor(v.m, d), __shfl_xor(v.s, d)});
+  for (int d = N / 128; d > 0; d >>= 1) v = join(v, Lse{__shfl_xor(v.m, d), __shfl_xor(v.s, d)}, c);
   return v;
 }
 template <int N>
-__device__ __forceinline__ Lse block_lse(Lse v, float (*lds)[2]) {
-  put_lse(v, lds);
+__device__ __forceinline__ Lse block_lse(Lse v, float (*lds)[2], float c = 1.0f) {
+  put_lse(v, lds, c);
   __syncthreads();
-  return get_lse<N>(lds);
+  return get_lse<N>(lds, c);
 }
 
 // Adds values to a sum, which is scaled once for all of them.  They are added up by themselves first: where an entry's logit is in the
@@ -82,14 +82,17 @@ __device__ __forceinline__ void add_to(Lse& l, const float* v, float c) {
   l = Lse{top, fmaf(l.s, __builtin_amdgcn_exp2f(l.m - ref), s)};
 }
 
-// Of one entry of a teacher's list; an infinite or NaN logit (or one whose y c overflows) makes all of the list's shares NaN.
-__device__ __forceinline__ Lse one(float y, float c) {
-  const float m = fminf(fmaxf(y * c, -FLT_MAX), FLT_MAX);
-  return Lse{m, fabsf(y) < INFINITY ? __builtin_amdgcn_exp2f(fmaf(y, c, -m)) : NAN};
+// Of one entry of a teacher's list, m being its logit as it is: differences are taken before they are scaled, so that the lowest and the
+// largest finite logits have their shares.  An infinite or NaN logit makes all of the list's shares NaN.
+__device__ __forceinline__ Lse one(float y) { return Lse{y, fabsf(y) < INFINITY ? 1.0f : NAN}; }
+// Its exponent of 2 (shares from 2^-1000 down are none), of a list with m; its share and the share's logarithm, l having the reciprocal of
+// the sum.  What the exponent's rounding takes, up to 5 2^-24 of a share of 10^-4, goes into a factor.
+__device__ __forceinline__ double below(const DistillArgs& A, float y, Lse l) { return fmax(((double)y - (double)l.m) * A.log2e_t, -1000.0); }
+__device__ __forceinline__ float share_of(const DistillArgs& A, float y, Lse l) {
+  const double x = below(A, y, l);
+  return __builtin_amdgcn_exp2f((float)x) * fmaf((float)(x - (float)x), kLn2, 1.0f) * l.s;
 }
-// Its share and the share's logarithm, of a list with m and the reciprocal of its sum.
-__device__ __forceinline__ float share_of(float y, float c, Lse l) { return __builtin_amdgcn_exp2f(fmaf(y, c, -l.m)) * l.s; }
-__device__ __forceinline__ float log_share_of(float y, float c, Lse l) { return fmaf(y, c, -l.m) * kLn2 + logf(l.s); }
+__device__ __forceinline__ float log_share_of(const DistillArgs& A, float y, Lse l) { return (float)below(A, y, l) * kLn2 + logf(l.s); }
 
 __device__ __forceinline__ int64_t id_at(const DistillArgs& A, int64_t i) {
   return A.id_type == ISO_I64 ? gmem((const int64_t*)A.ids)[i] : (int64_t)gmem((const int32_t*)A.ids)[i];
@@ -142,10 +145,10 @@ __device__ __forceinline__ Entry list_of(const DistillArgs& A, int64_t row, List
     }
   }
   // the first four waves hold the entries
-  Lse l = block_lse<256>(r.id >= 0 ? one(y, A.c) : Lse{}, S.red);
+  Lse l = block_lse<256>(r.id >= 0 ? one(y) : Lse{}, S.red, A.c);
   any = l.s != 0.0f;
   l.s = 1.0f / l.s;
-  if (r.id >= 0) r.log_t = log_share_of(y, A.c, l), r.t = share_of(y, A.c, l);
+  if (r.id >= 0) r.log_t = log_share_of(A, y, l), r.t = share_of(A, y, l);
   if (e < ISO_DISTILL_MAX_TOP) S.id[e] = r.id, S.t[e] = r.t;
   __syncthreads();
   return r;
@@ -395,15 +398,15 @@ __global__ void __launch_bounds__(N) k_distill_held(DistillArgs A) {
   asm volatile("" : "+v"(z_bits), "+v"(weight));
   const float z = f32_from_bits(DT == ISO_BF16 ? (uint32_t)z_bits << 16 : (uint32_t)z_bits);
   put_lse(l, S.red);
-  put_lse(r.id >= 0 ? one(y, A.c) : Lse{}, S.list.red);
+  put_lse(r.id >= 0 ? one(y) : Lse{}, S.list.red, A.c);
   if (e < ISO_DISTILL_MAX_TOP) S.list.id[e] = r.id, S.list.t[e] = y;
   S.head[e] = -1;
   __syncthreads();
   l = get_lse<N>(S.red);
-  Lse t = get_lse<256>(S.list.red);   // the first four waves hold the entries
+  Lse t = get_lse<256>(S.list.red, A.c);   // the first four waves hold the entries
   const bool any = t.s != 0.0f;
   t.s = 1.0f / t.s;
-  if (r.id >= 0) r.log_t = log_share_of(y, A.c, t), r.t = share_of(y, A.c, t);
+  if (r.id >= 0) r.log_t = log_share_of(A, y, t), r.t = share_of(A, y, t);
   const double lse = lse_of(A, l);
   const Factor F(A, weight, lse, any);
   double part = r.id >= 0 && r.t != 0.0f ? (double)r.t * ((double)r.log_t - (double)z / A.t + lse) : 0.0;
@@ -415,7 +418,7 @@ __global__ void __launch_bounds__(N) k_distill_held(DistillArgs A) {
     for (int i = 0; i < A.top; ++i)
       if (S.list.id[i] == r.id && i != e) {
         if (i < e) r.first = false;
-        r.t += share_of(S.list.t[i], A.c, t);
+        r.t += share_of(A, S.list.t[i], t);
       }
   }
   if (r.first) {
@@ -471,7 +474,7 @@ __global__ void __launch_bounds__(256) k_distill_join(DistillArgs A) {
   Lse l;
   for (int i = threadIdx.x; i < A.pieces; i += 256) {
     const auto p = gmem((const float*)A.part) + 2 * (row * A.pieces + i);
-    l = join(l, Lse{p[0], p[1]});
+    l = join(l, Lse{p[0], p[1]}, 1.0f);
   }
   l = block_lse<256>(l, S.red);
   __syncthreads();
@@ -512,7 +515,7 @@ DistillArgs args_of(const iso_distill& d, uint8_t* ws) {
   A.z = d.logits, A.ids = d.ids, A.y = d.teacher, A.w = d.weight, A.loss = d.loss, A.lse = d.lse, A.grad = d.grad;
   A.tokens = d.tokens, A.vocab = d.vocab, A.ld = d.ld, A.ld_grad = d.ld_grad, A.pad_id = d.pad_id;
   A.top = d.top, A.id_type = d.id_type;
-  A.c = (float)(1.4426950408889634 / d.temperature), A.t = d.temperature, A.tc = A.t * A.c, A.inv_tc = 1.0 / A.tc;
+  A.log2e_t = 1.4426950408889634 / d.temperature, A.c = (float)A.log2e_t, A.t = d.temperature, A.tc = A.t * A.c, A.inv_tc = 1.0 / A.tc;
   A.status = (uint32_t*)ws;
   A.part = (float*)(ws + kStatusBytes);
   return A;
