@@ -695,6 +695,8 @@ iso_status iso_attend_grad(const iso_attn* a, int dt, void* ws, size_t ws_bytes,
  *    zero loss and a zero gradient, whatever its logits hold (L is written all the same).  Ids may repeat in a list.
  *  - An id that is neither pad_id nor in [0, vocab) is reported by iso_read_device_status (ISO_ERR_INDEX); its entry
  *    is none.
+ *  - What a token's largest logit may be: up to 10^9 T in magnitude.  Behind that (a row of nothing but a mask's lowest value, say; single
+ *    masked logits of any size are fine) its L, loss and gradient are not finite, unless the token adds nothing.
  *  - logits and grad are of type dt with any row strides.  grad may be logits itself (same stride).
  */
 #define ISO_DISTILL_MAX_TOP 256
@@ -723,7 +725,8 @@ size_t iso_workspace_size_distill(const iso_distill* d);
  * once for all three. */
 iso_status iso_distill_loss(const iso_distill* d, int dt, void* ws, size_t ws_bytes, void* stream);
 
-/* iso_distill_grad -- writes the gradient from the lse that iso_distill_loss left (loss is not used). */
+/* iso_distill_grad -- writes the gradient from the lse that iso_distill_loss left (loss is not used).  lse is binary32: its rounding, up to
+ * 2^-24 |L|, is a relative error of the token's probabilities.  So it is where iso_distill_loss does not hold the row on chip. */
 iso_status iso_distill_grad(const iso_distill* d, int dt, void* ws, size_t ws_bytes, void* stream);
 
 /* round(n * num / den), halves rounded up, in exact integer arithmetic; -1 on bad arguments. */

@@ -35,37 +35,52 @@ struct DistillArgs {
   uint32_t* status;
 };
 
-// The sum of 2^(z c - m) over some logits, m their largest z c rounded: as m is what is subtracted, its rounding is no error.
+// The sum of 2^(z c - m) over some logits, m their largest z c rounded: as m is what is subtracted, its rounding is no error.  It is in the
+// exponent, though, and reaches 2^6 at 2^31; so m is no less than -2^31 (logits behind that, a mask's, have no part in a sum, and a
+// row of nothing else an L of minus infinity), and L is NaN where it is more than 2^31.
+constexpr float kFar = 2147483648.0f;
 struct Lse {
-  float m = -INFINITY, s = 0.0f;
+  float m = -kFar, s = 0.0f;
 };
-__device__ __forceinline__ float finite_or_zero(float m) { return m == -INFINITY ? 0.0f : m; }
-// A NaN sum stays one; so does infinity, whose own term is exp(inf - inf).  c: what differences of m count (a list's, see one()).
-__device__ __forceinline__ Lse join(Lse a, Lse b, float c) {
-  const float m = fmaxf(a.m, b.m), ref = finite_or_zero(m);
+// A NaN sum stays one; so does infinity, whose own term is exp(inf - inf).
+__device__ __forceinline__ Lse join(Lse a, Lse b) {
+  const float m = fmaxf(a.m, b.m);
+  return Lse{m, a.s * __builtin_amdgcn_exp2f(a.m - m) + b.s * __builtin_amdgcn_exp2f(b.m - m)};
+}
+// Of a list, m being its largest logit as it is (minus infinity: none): differences are taken before they are scaled.
+__device__ __forceinline__ Lse join_list(Lse a, Lse b, float c) {
+  const float m = fmaxf(a.m, b.m), ref = m == -INFINITY ? 0.0f : m;
   return Lse{m, a.s * __builtin_amdgcn_exp2f((a.m - ref) * c) + b.s * __builtin_amdgcn_exp2f((b.m - ref) * c)};
 }
 
 // Of a workgroup of N: every wave puts its own into LDS, and after a barrier all of them are joined.
-__device__ __forceinline__ void put_lse(Lse v, float (*lds)[2], float c = 1.0f) {
+template <class J>
+__device__ __forceinline__ void put_lse(Lse v, float (*lds)[2], J join) {
 #pragma unroll
-  for (int d = 32; d > 0; d >>= 1) v = join(v, Lse{__shfl_xor(v.m, d), __shfl_xor(v.s, d)}, c);
+  for (int d = 32; d > 0; d >>= 1) v = join(v, Lse{__shfl_xor(v.m, d), __shfl_xor(v.s, d)});
   if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6][0] = v.m, lds[threadIdx.x >> 6][1] = v.s;
 }
-template <int N>
-__device__ __forceinline__ Lse get_lse(const float (*lds)[2], float c = 1.0f) {
+template <int N, class J>
+__device__ __forceinline__ Lse get_lse(const float (*lds)[2], J join) {
   const int i = threadIdx.x & (N / 64 - 1);   // each N / 64 lanes for themselves, all alike
   Lse v{lds[i][0], lds[i][1]};
 #pragma unroll
-  for (int d = N / 128; d > 0; d >>= 1) v = join(v, Lse{__shfl_xor(v.m, d), __shfl_xor(v.s, d)}, c);
+  for (int d = N / 128; d > 0; d >>= 1) v = join(v, Lse{__shfl_xor(v.m, d), __shfl_xor(v.s, d)});
   return v;
 }
-template <int N>
-__device__ __forceinline__ Lse block_lse(Lse v, float (*lds)[2], float c = 1.0f) {
-  put_lse(v, lds, c);
+template <int N, class J>
+__device__ __forceinline__ Lse block_lse(Lse v, float (*lds)[2], J join) {
+  put_lse(v, lds, join);
   __syncthreads();
-  return get_lse<N>(lds, c);
+  return get_lse<N>(lds, join);
 }
+struct Join {
+  __device__ __forceinline__ Lse operator()(Lse a, Lse b) const { return join(a, b); }
+};
+struct JoinList {
+  float c;
+  __device__ __forceinline__ Lse operator()(Lse a, Lse b) const { return join_list(a, b, c); }
+};
 
 // Adds values to a sum, which is scaled once for all of them.  They are added up by themselves first: where an entry's logit is in the
 // sum, one by one the others would be lost in its rounding.
@@ -75,16 +90,15 @@ __device__ __forceinline__ void add_to(Lse& l, const float* v, float c) {
 #pragma unroll
   for (int j = 1; j < N; ++j) top = fmaxf(top, v[j]);
   top = fmaxf(l.m, top * c);
-  const float ref = finite_or_zero(top);
   float s = 0.0f;
 #pragma unroll
-  for (int j = 0; j < N; ++j) s += __builtin_amdgcn_exp2f(fmaf(v[j], c, -ref));
-  l = Lse{top, fmaf(l.s, __builtin_amdgcn_exp2f(l.m - ref), s)};
+  for (int j = 0; j < N; ++j) s += __builtin_amdgcn_exp2f(fmaf(v[j], c, -top));
+  l = Lse{top, fmaf(l.s, __builtin_amdgcn_exp2f(l.m - top), s)};
 }
 
-// Of one entry of a teacher's list, m being its logit as it is: differences are taken before they are scaled, so that the lowest and the
-// largest finite logits have their shares.  An infinite or NaN logit makes all of the list's shares NaN.
-__device__ __forceinline__ Lse one(float y) { return Lse{y, fabsf(y) < INFINITY ? 1.0f : NAN}; }
+// Of one entry of a teacher's list (or none): the lowest and the largest finite logits have their shares, an infinite or NaN logit makes
+// all of the list's shares NaN.
+__device__ __forceinline__ Lse one(bool has, float y) { return has ? Lse{y, fabsf(y) < INFINITY ? 1.0f : NAN} : Lse{-INFINITY, 0.0f}; }
 // Its exponent of 2 (shares from 2^-1000 down are none), of a list with m; its share and the share's logarithm, l having the reciprocal of
 // the sum.  What the exponent's rounding takes, up to 5 2^-24 of a share of 10^-4, goes into a factor.
 __device__ __forceinline__ double below(const DistillArgs& A, float y, Lse l) { return fmax(((double)y - (double)l.m) * A.log2e_t, -1000.0); }
@@ -145,7 +159,7 @@ __device__ __forceinline__ Entry list_of(const DistillArgs& A, int64_t row, List
     }
   }
   // the first four waves hold the entries
-  Lse l = block_lse<256>(r.id >= 0 ? one(y) : Lse{}, S.red, A.c);
+  Lse l = block_lse<256>(one(r.id >= 0, y), S.red, JoinList{A.c});
   any = l.s != 0.0f;
   l.s = 1.0f / l.s;
   if (r.id >= 0) r.log_t = log_share_of(A, y, l), r.t = share_of(A, y, l);
@@ -230,18 +244,19 @@ __device__ __forceinline__ Lse row_lse(const DistillArgs& A, int64_t row, int64_
     unpack_raw<DT>(load_end<DT>(A.z, base + c, hi - c), v);
     add_to<V>(l, v, A.c);
   }
-  return block_lse<N>(l, lds);
+  return block_lse<N>(l, lds, Join{});
 }
 
 // L of a row, in binary64: the loss takes differences of it.  m / c is a logit but for m's rounding, which s holds; the logarithm of s
 // is that of a value from 1/2 to 1, which binary32 has to 2^-24, and a multiple of log 2.
 __device__ __forceinline__ double lse_of(const DistillArgs& A, Lse l) {
+  if (!(l.m < kFar)) return NAN;
   const float low = logf(__builtin_amdgcn_frexp_mantf(l.s));
   return fma((double)l.m, A.inv_tc, fma((double)__builtin_amdgcn_frexp_expf(l.s), 0.6931471805599453, (double)low));
 }
 
 // A row's factor w T, whether its gradient is zero, and its L: a probability is less 2^(z c - lse2), lse2 being T c L
-// rounded and less the power of two of what that took.
+// rounded and less the power of two of what that took (2^-19 for logits of 10, more than 1 from 10^7 on).
 struct Factor {
   float f, less, lse2;
   bool zero;
@@ -250,7 +265,8 @@ struct Factor {
     zero = !any || w == 0.0f;
     const double exact = lse * A.tc;
     lse2 = (float)exact;
-    less = fabsf(lse2) < INFINITY ? (float)(1.0 + (lse2 - exact) * 0.6931471805599453) : 1.0f;
+    const double took = lse2 - exact;
+    less = !(fabsf(lse2) < INFINITY) ? 1.0f : fabs(took) < 0x1p-12 ? (float)(1.0 + took * 0.6931471805599453) : exp2f((float)took);
   }
   __device__ __forceinline__ float probability(const DistillArgs& A, float z) const {
     return less * __builtin_amdgcn_exp2f(fmaf(z, A.c, -lse2));
@@ -397,13 +413,13 @@ __global__ void __launch_bounds__(N) k_distill_held(DistillArgs A) {
   }
   asm volatile("" : "+v"(z_bits), "+v"(weight));
   const float z = f32_from_bits(DT == ISO_BF16 ? (uint32_t)z_bits << 16 : (uint32_t)z_bits);
-  put_lse(l, S.red);
-  put_lse(r.id >= 0 ? one(y) : Lse{}, S.list.red, A.c);
+  put_lse(l, S.red, Join{});
+  put_lse(one(r.id >= 0, y), S.list.red, JoinList{A.c});
   if (e < ISO_DISTILL_MAX_TOP) S.list.id[e] = r.id, S.list.t[e] = y;
   S.head[e] = -1;
   __syncthreads();
-  l = get_lse<N>(S.red);
-  Lse t = get_lse<256>(S.list.red, A.c);   // the first four waves hold the entries
+  l = get_lse<N>(S.red, Join{});
+  Lse t = get_lse<256>(S.list.red, JoinList{A.c});   // the first four waves hold the entries
   const bool any = t.s != 0.0f;
   t.s = 1.0f / t.s;
   if (r.id >= 0) r.log_t = log_share_of(A, y, t), r.t = share_of(A, y, t);
@@ -474,9 +490,9 @@ __global__ void __launch_bounds__(256) k_distill_join(DistillArgs A) {
   Lse l;
   for (int i = threadIdx.x; i < A.pieces; i += 256) {
     const auto p = gmem((const float*)A.part) + 2 * (row * A.pieces + i);
-    l = join(l, Lse{p[0], p[1]}, 1.0f);
+    l = join(l, Lse{p[0], p[1]});
   }
-  l = block_lse<256>(l, S.red);
+  l = block_lse<256>(l, S.red, Join{});
   __syncthreads();
   bool any;
   const Entry r = list_of<256>(A, row, S, any);
