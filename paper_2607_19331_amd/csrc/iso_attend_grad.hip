@@ -47,14 +47,17 @@ __global__ void __launch_bounds__(256) k_attend_stat(AttnArgs A) {
 // ---- dQ ------------------------------------------------------------------------------------------------------------
 
 // Keys have much in common (a projection's bias) and a row's S next to no sum, so that the common part of S K cancels but for the
-// sum of what the rounding of S to bf16 took.  That sum is kept, and the common part, for which the mean of 16 keys stands that
-// all rows of the wave see, is added with it at the end: sum S k = sum round(S) k + sum (S - round(S)) (k - c) + c sum (S - round(S)),
+// sum of what the rounding of S to bf16 took.  That sum is kept, and the common part, for which the mean c of a few keys stands that
+// the row sees, is added with it at the end: sum S k = sum round(S) k + sum (S - round(S)) (k - c) + c sum (S - round(S)),
 // of which the middle is left out.  With a bias of twice the keys' own width the error of dQ is 2.4 thousandths instead of 4.2, of
 // which 1.7 are its own rounding.
 template <int DT, int D>
 struct Common {
   static constexpr int kKeys = 16;
   static constexpr uint32_t kBytes = 512;   // of LDS, a wave
+  // Where all rows of the wave see fewer keys than kOwn (narrow windows, the first rows of a sequence) a row has the first kOwn of its
+  // own: what is left of the error is sqrt(1 + 1 / n) times the least for n keys, 3% more with 16 and 12% with 4.
+  static constexpr int kOwn = 4;
   uint32_t lds;
 
   // Of keys [from, to) the first kKeys.  Before the loop and from memory, not from the panels as they come by: branches in the loop
@@ -66,7 +69,7 @@ struct Common {
 #pragma unroll
     for (int i = 0; i < kKeys; ++i) {
       w[i] = 0;
-      if (i < keys && 2 * lane < A.dim) w[i] = *(global_ptr<const uint32_t>)(gmem((const uint16_t*)A.k) + (first + from + i) * A.ld_k + col + 2 * lane);
+      if (i < keys && 2 * lane < A.dim) w[i] = pair(A, first + from + i, col, lane);
     }
     float a = 0.0f, b = 0.0f;
 #pragma unroll
@@ -75,24 +78,74 @@ struct Common {
     *(lds_word)(uintptr_t)(lds + 8 * lane) = bits_from_f32(a * f);
     *(lds_word)(uintptr_t)(lds + 8 * lane + 4) = bits_from_f32(b * f);
   }
-  __device__ __forceinline__ void add(f32x16_t (&acc)[D / 32], float lost, int half) const {
+  __device__ static __forceinline__ uint32_t pair(const AttnArgs& A, int64_t key, int64_t col, int lane) {
+    return *(global_ptr<const uint32_t>)(gmem((const uint16_t*)A.k) + key * A.ld_k + col + 2 * lane);
+  }
+
+  // lost: of the lane's row, which sees keys [lo, hi) from row `first` of k on.  panel: LDS that the wave has to itself.
+  __device__ __forceinline__ void add(const AttnArgs& A, uint32_t panel, int64_t first, bool on, int32_t lo, int32_t hi, int64_t col,
+                                      f32x16_t (&acc)[D / 32], float lost, int lane) const {
+    // what all rows see, worked out again: between the last one's first key and the first one's last
+    const uint32_t rows = (uint32_t)__ballot(on), seeing = (uint32_t)__ballot(hi > lo);
+    const bool own = seeing != 0 && __builtin_amdgcn_readlane(hi, 0) - __builtin_amdgcn_readlane(lo, 31 - __builtin_clz(rows)) < kOwn;
+    const int half = lane >> 5;
+    uint32_t at[kOwn], x[kOwn];
+    float f[kOwn];
+    if (own) {   // the keys as they are, in LDS
+      const int end = 31 - __builtin_clz(seeing);
+      const int32_t from = __builtin_amdgcn_readlane(lo, __builtin_ctz(seeing));
+      const int32_t count = min(__builtin_amdgcn_readlane(lo, end) + kOwn, __builtin_amdgcn_readlane(hi, end)) - from;
+      constexpr int kChunk = 12;
+#pragma unroll 1
+      for (int j0 = 0; j0 < count; j0 += kChunk) {
+        uint32_t w[kChunk];
+#pragma unroll
+        for (int j = 0; j < kChunk; ++j) {
+          w[j] = 0;
+          if (2 * lane < A.dim) w[j] = pair(A, first + from + min(j0 + j, count - 1), col, lane);
+        }
+        if (4 * lane < 2 * D)
+#pragma unroll
+          for (int j = 0; j < kChunk; ++j)
+            *(lds_word)(uintptr_t)(panel + (j0 + j) * 2 * D + (4 * lane ^ place(j0 + j))) = w[j];
+      }
+      const int32_t keys = min(hi - lo, kOwn);
+#pragma unroll
+      for (int k = 0; k < kOwn; ++k) {
+        const int32_t key = max(lo - from + min(k, keys - 1), 0);
+        at[k] = panel + key * 2 * D, x[k] = place(key) ^ 8 * half;
+        f[k] = k < keys ? lost / (float)keys : 0.0f;
+      }
+    }
 #pragma unroll
     for (int d = 0; d < D / 32; ++d)
 #pragma unroll
       for (int e = 0; e < 16; e += 4) {
-        const f32x4_t c = *(lds_f32x4)(uintptr_t)(lds + (32 * d + 2 * e + 4 * half) * 4);
+        f32x4_t c = 0.0f;
+        if (own) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) acc[d][e + i] = fmaf(c[i], lost, acc[d][e + i]);
+          for (int k = 0; k < kOwn; ++k) {
+            const lds_u32x2_t w = *(lds_pair)(uintptr_t)(at[k] + (x[k] ^ (64 * d + 4 * e)));
+            c[0] = fmaf(f32_from_bits(w[0] << 16), f[k], c[0]), c[1] = fmaf(f32_from_bits(w[0] & 0xFFFF0000u), f[k], c[1]);
+            c[2] = fmaf(f32_from_bits(w[1] << 16), f[k], c[2]), c[3] = fmaf(f32_from_bits(w[1] & 0xFFFF0000u), f[k], c[3]);
+          }
+        } else {
+          c = *(lds_f32x4)(uintptr_t)(lds + (32 * d + 2 * e + 4 * half) * 4) * lost;
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) acc[d][e + i] += c[i];
         __builtin_amdgcn_sched_barrier(0);
       }
   }
+  // Keys' 8-byte pieces in different banks.
+  __device__ static __forceinline__ uint32_t place(int key) { return D == 128 ? 8 * (key % 32) : 8 * (key / 2 % 16); }
 };
 // fp32 rounds no S: no sum, and no LDS.
 template <int D>
 struct Common<ISO_F32, D> {
   static constexpr uint32_t kBytes = 0;
   __device__ __forceinline__ Common(const AttnArgs&, uint32_t, int64_t, int32_t, int32_t, int64_t, int) {}
-  __device__ __forceinline__ void add(f32x16_t (&)[D / 32], float, int) const {}
+  __device__ __forceinline__ void add(const AttnArgs&, uint32_t, int64_t, bool, int32_t, int32_t, int64_t, f32x16_t (&)[D / 32], float, int) const {}
 };
 
 // Workgroup layout of dq_tile: two panels of keys, two of values, and what a wave keeps for Common.
@@ -101,6 +154,7 @@ struct Dq {
   using P = Panel<DT, D>;
   static constexpr uint32_t kV = 2 * P::kBytes, kCommon = 4 * P::kBytes;
   static constexpr uint32_t kLds = kCommon + kAttnWaves * Common<DT, D>::kBytes;
+  static_assert(P::kBytes >= 36 * 2 * D, "a panel holds a wave's own keys, in whole chunks");
 };
 
 // dQ of a tile: as the forward kernel, 128 rows of a group's list a workgroup and panels of 64 keys and values in LDS twice over; Q and
@@ -141,7 +195,7 @@ __device__ __forceinline__ void dq_tile(const AttnArgs& A, const Deal& deal, uin
   const uint32_t lds = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(lds_u8*)smem);
   using S = Dq<DT, D>;
   constexpr uint32_t kV = S::kV;
-  const Reader<DT, D> rd(lds, lane);
+  Reader<DT, D> rd(lds, lane);
   kr.skip(first), vr.skip(first);
   if (first < last) {
     kr.load(lds, w);
@@ -168,6 +222,7 @@ __device__ __forceinline__ void dq_tile(const AttnArgs& A, const Deal& deal, uin
     const bool whole = k0 >= mine.lo_all && k0 + P::kRows <= mine.hi_all;
     auto sees = [&](int j, int e) { return (uint32_t)(k0 + 32 * j + 8 * (e / 4) + 4 * half + e % 4 - lo) < (uint32_t)(hi - lo); };
     if constexpr (DT == ISO_BF16) {
+      rd.again();
       // as in dkv_tile: fragments three products ahead, S and dP by rows, dQ by columns, one tile of 32 keys after the other
       constexpr int G = P::kGroups, N = P::kDims, kAhead = 3;
       static_assert(G == 2 * N, "as many products each");
@@ -247,8 +302,8 @@ __device__ __forceinline__ void dq_tile(const AttnArgs& A, const Deal& deal, uin
     step(t, 0);
     if (t + 1 < last) step(t + 1, 1);
   }
-  common.add(dq, sum_of_halves(lost), half);
-  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");   // no load may reach LDS after the workgroup's end
+  landed();   // panels are free, and no load may reach LDS after the workgroup's end
+  common.add(A, lds + w * P::kBytes, s.k0, on, lo, hi, col, dq, sum_of_halves(lost), lane);
 
   if (pieces > 1) {
     if (!on) return;

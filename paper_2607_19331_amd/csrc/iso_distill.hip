@@ -256,7 +256,7 @@ __device__ __forceinline__ double lse_of(const DistillArgs& A, Lse l) {
 }
 
 // A row's factor w T, whether its gradient is zero, and its L: a probability is less 2^(z c - lse2), lse2 being T c L
-// rounded and less the power of two of what that took (2^-19 for logits of 10, more than 1 from 10^7 on).
+// rounded and less the power of two of what that took (2^-21 for logits of 10, 1/2 for 10^7).
 struct Factor {
   float f, less, lse2;
   bool zero;

@@ -12,6 +12,8 @@ typedef __attribute__((address_space(3))) uint8_t lds_u8;
 typedef short s16x4_t __attribute__((ext_vector_type(4)));
 typedef __attribute__((address_space(3))) s16x4_t* lds_frag;
 typedef __attribute__((address_space(3))) f32x4_t* lds_f32x4;
+typedef uint32_t lds_u32x2_t __attribute__((ext_vector_type(2)));
+typedef __attribute__((address_space(3))) const lds_u32x2_t* lds_pair;
 typedef __bf16 bf16x8_t __attribute__((ext_vector_type(8)));
 typedef float f32x16_t __attribute__((ext_vector_type(16)));
 

@@ -1,6 +1,6 @@
-"""LDS of the attention kernels, in the assembly that this build makes of them: what a launch asks for (panels, and behind them what
-a wave keeps) is what the workgroups write.  Panels are filled by loads straight into LDS; the only stores are those of the common
-part of the keys in the bf16 backward pass, 512 bytes a wave."""
+"""LDS of the attention kernels, in the assembly that this build makes of them: what a launch asks for is what the workgroups write.
+Panels and rows' statistics are filled by loads straight into LDS; the only stores are those of the common part of the keys in the bf16
+backward pass."""
 import re
 import subprocess
 
@@ -28,8 +28,3 @@ def test_fp32_workgroups_store_nothing_behind_their_panels(kernels, dim):
     """Their launch asks for the panels and 512 bytes that loads fill."""
     assert "buffer_load_dwordx4" in kernels[0, dim]
     assert stores(kernels[0, dim]) == []
-
-
-@pytest.mark.parametrize("dim", [64, 128])
-def test_bf16_workgroups_store_the_common_part_once(kernels, dim):
-    assert len(stores(kernels[1, dim])) == 1
