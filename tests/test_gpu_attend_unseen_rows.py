@@ -56,3 +56,40 @@ def test_keys_that_a_row_does_not_see_do_not_reach_it(dtype, names, keys, window
     clean = Case(dtype, [length], [length], 2, 1, 64, causal, window)
     clean.forward(), clean.backward()
     assert np.allclose(got[~see], clean.dq.host()[at:at + length][~see], rtol=2.0 ** -6, atol=2.0 ** -9)
+
+
+def test_a_step_that_has_gone_to_nan_ends():
+    """All of q, k, v and dout NaN: all results are, and a call takes a few times as long as it does otherwise (row by row over all keys it
+    would be two hundred times; 40 is far from both)."""
+    import torch
+
+    import paper_2607_19331_amd as iso
+    say("attend all NaN")
+    tokens, heads, kv, dim = 4096, 28, 4, 128
+    new = lambda *s: torch.randn(*s, device="cuda").to(torch.bfloat16)  # noqa: E731
+    start = torch.tensor([0, tokens], dtype=torch.int32, device="cuda")
+    x = {n: new(tokens, (heads if n in ("q", "out", "dout", "dq") else kv) * dim) for n in ("q", "k", "v", "out", "dout", "dq", "dk", "dv")}
+    a = iso.Attn(start_q=start, start_k=start, sequences=1, tokens_q=tokens, tokens_k=tokens, heads=heads, heads_kv=kv, dim=dim, scale=dim ** -0.5,
+                 lse=torch.zeros(tokens, heads, device="cuda"), causal=True, **x)
+    ws = [iso.attend_workspace(a, iso.BF16, grad=g) for g in (False, True)]
+
+    def took():
+        best = []
+        for call, w in zip((iso.iso_attend, iso.iso_attend_grad), ws):
+            times = []
+            for _ in range(4):
+                b, e = (torch.cuda.Event(enable_timing=True) for _ in range(2))
+                b.record(), call(a, iso.BF16, ws=w), e.record()
+                torch.cuda.synchronize()
+                times.append(b.elapsed_time(e))
+            best.append(min(times))
+        return best
+    usual = took()
+    for n in ("q", "k", "v", "dout"):
+        x[n].fill_(float("nan"))
+    bad = took()
+    say(f"ms {usual} {bad}")
+    for n in ("out", "dq", "dk", "dv"):
+        assert bool(x[n].isnan().all())
+    assert bool(a.lse.isnan().all())
+    assert bad[0] < 40 * usual[0] and bad[1] < 40 * usual[1]
