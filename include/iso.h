@@ -627,6 +627,7 @@ iso_status iso_ckpt_weight_grad(const iso_weight_grad* g, int n, int dt, int dt_
  *  - Offsets are device memory, sequences + 1 values each, ascending, 0 <= start <= tokens.  A sequence whose
  *    offsets are no range of the rows is left out, and so is one that begins before the end of an earlier range;
  *    iso_read_device_status reports it (ISO_ERR_INDEX), and the other sequences are worked out.
+ *  - Sequences may have no queries (keys of a cache that nobody asks for, with dk = dv = 0) or no keys (padded rows).
  *  - Rows of q, k and v that belong to no sequence are not read, and those of the outputs not written.
  *  - Sizes past the limits below are ISO_ERR_UNSUPPORTED.
  *  - A result depends on the keys (or queries) that are seen and on no others: what non-finite values others

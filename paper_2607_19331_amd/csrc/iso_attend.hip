@@ -12,14 +12,17 @@ namespace {
 // A workgroup has 128 rows of a kv head's list (queries times the group, so that one token a sequence fills tiles too), a wave 32 of
 // them; panels of 64 keys (32 in fp32) and their values lie in LDS twice over, loaded there by the memory unit while the one before
 // is worked on.  X is formed as K Q^T, a row a lane: maximum and sum are a lane's own (and its other half's), and P is the second
-// operand of the product with V where it is.  Q and O stay in registers.
+// operand of the product with V where it is.  Q and O stay in registers.  With bf16, P is rounded to bf16 for that product, whose operands
+// are of one type (P in two parts would be half as many products again); l is the sum of what was not rounded.  Of 2.1 thousandths by
+// which O is off then, 1.6 are its own rounding.
 //
-// What bounds it: D = 128 the matrix instructions, 56% of the cycles at the 1.75 GHz that the card holds under them: four sequences
-// of 4096 tokens, 28 heads over 4, causal, 500 us, 960 TFLOP/s (16 heads, all keys seen, 1030; a large product of the library 1200).
-// D = 64 the exponentials and what goes with them, twice the matrix instructions' cycles (32 heads over 8: 330 us, 830 TFLOP/s).
+// What bounds it: D = 128 the matrix instructions, 55% of the cycles at the 1.75 GHz that the card holds under them: four sequences
+// of 4096 tokens, 28 heads over 4, causal, 500 us, 960 TFLOP/s (16 heads, all keys seen, 1035; a large product of the library 1200).
+// D = 64 the exponentials and what goes with them, twice the matrix instructions' cycles (32 heads over 8: 325 us, 850 TFLOP/s).
 // fp32 the matrix rate of its type (154 TFLOP/s, a sixteenth of bf16's): 8 heads of 128, one sequence of 8192, all keys seen, 122
 // TFLOP/s with one wave a SIMD; causal, four of 2048, 314 us, 110.  Few rows: keys are shared out to pieces, see share_out; one token over 77 to 8192 keys for 16
-// sequences, 28 heads, 30 us with the join, 3.5 TB/s, of which 5 are a workgroup's start and 6 the join's launch.
+// sequences, 28 heads, 30 us with the join, 3.5 TB/s, of which 5 are a workgroup's start and 6 the join's launch.  One wave of four has
+// rows there; in fp32 (139 us, 1.5 TB/s) its matrix instructions bound it.
 template <int DT, int D>
 __global__ void __launch_bounds__(256, (DT == ISO_F32 && D == 128 ? 1 : 2)) k_attend(AttnArgs A, Deal deal) {
   using P = Panel<DT, D>;
@@ -288,7 +291,7 @@ __global__ void __launch_bounds__(256) k_attend_join(AttnArgs A) {
 template <int DT, int D>
 hipError_t forward(const AttnArgs& A, hipStream_t s) {
   Deal deal = deal_of(A.heads_kv, attend_items(A.tokens_q * A.group, A.tokens_k, A.sequences, A.pieces));
-  if (A.pieces.most == 1 && !(DT == ISO_F32 && D == 128)) deal = folded(deal, A.heads_kv, A.tokens_q * A.heads / kAttnTileRows);   // two a CU
+  if (A.pieces.most == 1 && !(DT == ISO_F32 && D == 128)) deal = folded(deal, A.heads_kv, A.tokens_q * A.heads / kAttnTileRows);
   k_attend<DT, D><<<deal_grid(deal, A.heads_kv) + 1, 256, 4 * Panel<DT, D>::kBytes, s>>>(A, deal);   // one looks at the offsets
   const unsigned rows = (unsigned)((A.tokens_q * A.heads + 7) / 8);
   if (A.pieces.most > 4) k_attend_join<DT, 8><<<rows, 256, 0, s>>>(A);

@@ -5,10 +5,13 @@
 // dq have rows and walk over the keys that they see.  That is seven products of rows x keys x dim where one kernel would need five, but each
 // result has one owner who adds in a fixed order: no atomics, the same bits every time.
 //
-// Both are bound by the matrix instructions (bf16, D = 128: busy 61 and 62% of the cycles, at the 1.5 to 1.6 GHz that the card holds
-// under them): two sequences of 8192 tokens, 28 heads over 4, causal, 3.13 ms, 769 TFLOP/s of five products, 1076 of seven, where
-// a large product of the library reaches 1200.  D = 64 (32 heads over 8, 4 x 4096): 1.11 ms, 620.  fp32 (8 heads of 128, 4 x 2048): 1.10
-// ms, 79, 110 of seven, of its matrix rate's 154.
+// Both are bound by the matrix instructions (bf16, D = 128: busy 64% of the cycles, at the 1.5 to 1.6 GHz that the card holds
+// under them): two sequences of 8192 tokens, 28 heads over 4, causal, 3.09 ms, 779 TFLOP/s of five products, 1090 of seven, where
+// a large product of the library reaches 1200.  D = 64 (32 heads over 8, 4 x 4096): 1.08 ms, 634.  fp32 (8 heads of 128, 4 x 2048): 1.10
+// ms, 78, 109 of seven, of its matrix rate's 154.
+//
+// With bf16, P and S are rounded to bf16 for the products with dO, Q and K, whose operands are of one type; P and S themselves and all sums
+// are binary32.  Of 2.3 to 2.4 thousandths by which dQ, dK and dV are off then, 1.7 are their own rounding.
 #include <algorithm>
 
 #include "iso_attend_tiles.h"
@@ -20,7 +23,7 @@ namespace {
 
 // L log2(e) and D of every row, 16 lanes a row, in the order of the groups' lists: a panel's come into LDS with one load.  A row's place
 // there does not depend on its sequence, so that none is looked up; those of rows without one are not used.  Bound by memory: O and dO
-// read once.
+// read once (16384 tokens, 28 heads of 128: 51 us, 4.6 TB/s; 13379 tokens, 12 heads: 17 us, 4.8).
 template <int DT>
 __global__ void __launch_bounds__(256) k_attend_stat(AttnArgs A) {
   if (blockIdx.x == gridDim.x - 1) return check_starts(A);
@@ -222,7 +225,7 @@ __device__ __forceinline__ void dq_tile(const AttnArgs& A, const Deal& deal, uin
     const bool whole = k0 >= mine.lo_all && k0 + P::kRows <= mine.hi_all;
     auto sees = [&](int j, int e) { return (uint32_t)(k0 + 32 * j + 8 * (e / 4) + 4 * half + e % 4 - lo) < (uint32_t)(hi - lo); };
     if constexpr (DT == ISO_BF16) {
-      rd.again();
+      rd.again();   // kept, addresses and what Common::add needs took 20 bytes of scratch in this loop (heads of 128)
       // as in dkv_tile: fragments three products ahead, S and dP by rows, dQ by columns, one tile of 32 keys after the other
       constexpr int G = P::kGroups, N = P::kDims, kAhead = 3;
       static_assert(G == 2 * N, "as many products each");

@@ -225,8 +225,8 @@ namespace {
 constexpr int kPieceKeys = 256;         // fewest keys of a piece
 constexpr int kMostTilePieces = 64;         // of a tile
 constexpr double kSparse = 2.0;
-constexpr int64_t kRound = 512;         // workgroups at once
-constexpr int64_t kFullTiles = 1536;    // three rounds of workgroups, two a CU: heavy tiles first, these balance by themselves
+constexpr int64_t kRound = 512;         // workgroups at once, counted as two a CU (forward with bf16 heads up to 64 runs three)
+constexpr int64_t kFullTiles = 1536;    // three rounds of them: heavy tiles first, these balance by themselves
 
 // Tiles of `owners` rows walk over `length` keys on average.  In p pieces a tile's time falls by p, and every row writes and
 // reads p partial sums: the sum of both is least at p = f sqrt(length / owners).  f was measured, 6.5 for rows and 9.1 for keys
