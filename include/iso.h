@@ -679,7 +679,8 @@ iso_status iso_attend(const iso_attn* a, int dt, void* ws, size_t ws_bytes, void
  * iso_attend_grad -- from out, lse (those of iso_attend) and dout: with P as above, D_i = dout_i.O_i and
  * S_ij = P_ij (dout_i.v_j - D_i),
  *   dv_j = sum_i P_ij dout_i,   dk_j = scale sum_i S_ij q_i,   dq_i = scale sum_j S_ij k_j,
- * the first two over the heads of a group too.  All three are written.  With bf16, P and S are rounded to bf16 in
+ * the first two over the heads of a group too.  All three are written.  lse is binary32: its rounding, up to 2^-24 |L|, is a relative
+ * error of P (scores of thousands are fine, of 10^7 are not).  With bf16, P and S are rounded to bf16 in
  * the products; dq also has the sum of what S lost times the mean of up to 16 keys that the query sees, which takes out
  * most of that error where keys have a common part (a projection's bias).
  */
