@@ -20,9 +20,9 @@ namespace {
 // of 4096 tokens, 28 heads over 4, causal, 500 us, 960 TFLOP/s (16 heads, all keys seen, 1035; a large product of the library 1200).
 // D = 64 the exponentials and what goes with them, twice the matrix instructions' cycles (32 heads over 8: 325 us, 850 TFLOP/s).
 // fp32 the matrix rate of its type (154 TFLOP/s, a sixteenth of bf16's): 8 heads of 128, one sequence of 8192, all keys seen, 122
-// TFLOP/s with one wave a SIMD; causal, four of 2048, 314 us, 110.  Few rows: keys are shared out to pieces, see share_out; one token over 77 to 8192 keys for 16
-// sequences, 28 heads, 30 us with the join, 3.5 TB/s, of which 5 are a workgroup's start and 6 the join's launch.  One wave of four has
-// rows there; in fp32 (139 us, 1.5 TB/s) its matrix instructions bound it.
+// TFLOP/s with one wave a SIMD; causal, four of 2048, 314 us, 110.  Few rows: keys are shared out to pieces, see share_out; one token
+// over 77 to 8192 keys for 16 sequences, 28 heads, 30 us with the join, 3.5 TB/s, of which 5 are a workgroup's start and 6 the join's
+// launch.  One wave of four has rows there; in fp32 (139 us, 1.5 TB/s) its matrix instructions bound it.
 template <int DT, int D>
 __global__ void __launch_bounds__(256, (DT == ISO_F32 && D == 128 ? 1 : 2)) k_attend(AttnArgs A, Deal deal) {
   using P = Panel<DT, D>;

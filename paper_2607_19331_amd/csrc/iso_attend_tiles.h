@@ -223,8 +223,8 @@ inline Deal deal_of(int heads, uint32_t items) {
   return Deal{c, 8 / c, items, 0, 0};
 }
 // Items of falling length that all start at once, counted as two a CU (bf16 heads up to 64 run three): the second half from its end on, so
-// that the shortest go with the longest.  `tiles`: about how many there are.  Four sequences of 2048, causal, 8 heads of 64, fp32: 161 us for 206; 2048 tokens, 32 heads of
-// 128, bf16: 53 for 63.
+// that the shortest go with the longest.  `tiles`: about how many there are.  Four sequences of 2048, causal, 8 heads of 64, fp32:
+// 161 us for 206; 2048 tokens, 32 heads of 128, bf16: 53 for 63.
 inline Deal folded(Deal d, int heads, int64_t tiles) {
   const uint32_t cus = 32 * d.per, all = (uint32_t)(heads / d.classes) * d.items;   // CUs of a class
   if (all > cus && tiles <= 2 * (int64_t)cus * d.classes) d.fold = cus, d.end = std::min(all, 2 * cus);
